@@ -300,6 +300,142 @@ gbla_status gbla_layer_forward(const gbla_layer_shape* shape, const void* x,
                                const int32_t* cu_seqlens, void* workspace,
                                size_t workspace_bytes, float* out, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The decoder's operators: causal linear attention with one decay per key head,
+ * in chunks and token by token, and the norm and rotation of its queries and
+ * keys.  They share the conventions above, with these differences:
+ * - Queries and keys may have different head counts: kv_heads divides heads,
+ *   query head h reads key head h / (heads / kv_heads).  Shapes below write H
+ *   for heads and K for kv_heads.
+ * - Outputs and gradients have the type of the tensor that they belong to
+ *   (shape->dtype for activations, fp32 for states, decays and norm weights).
+ * - Ragged batches may end before the tensors do (cu[N_s] <= T): rows from
+ *   cu[N_s] on are neither read nor written.
+ * - Batches without tokens are accepted (arrays over the tokens may be NULL).
+ * - Tokens of one sequence never reach another's results.  Within a sequence,
+ *   an infinite or NaN value may also reach outputs of earlier tokens that lie
+ *   within the same 64 tokens of a launch's split.
+ * ---------------------------------------------------------------------------
+ */
+
+/* Adjacent channels (2i, 2i + 1) rotate together, instead of (i, i + R/2). */
+enum { GBLA_ROPE_PAIRS = 8 };
+
+typedef struct {
+  int32_t batch;      /* B (dense) or N_s (ragged), >= 1                          */
+  int32_t seqlen;     /* n (dense) or T (ragged), >= 0                            */
+  int32_t heads;      /* H >= 1: heads of q                                      */
+  int32_t kv_heads;   /* K >= 1: heads of k (any ratio to H)                      */
+  int32_t head_dim;   /* d in {32, 64, 128}                                      */
+  int32_t rotary_dim; /* R: the first R channels rotate; a multiple of 8, 0 .. d   */
+  int32_t dtype;      /* gbla_dtype of q, k and their gradients                  */
+  float eps;          /* RMSNorm epsilon, finite and >= 0                        */
+  float theta;        /* base of the rotation's frequencies, finite and > 0      */
+  uint32_t flags;     /* OR of GBLA_NO_NORM and GBLA_ROPE_PAIRS                   */
+} gbla_rope_shape;
+
+/*
+ * RMS norm of every head's queries and keys, then the rotation by position:
+ *   xn = x / sqrt(mean_e x_e^2 + eps) * w[h]             (x under GBLA_NO_NORM)
+ *   angle_i = position * theta^(-2 i / R), i < R / 2
+ *   (a, b) -> (a cos - b sin, a sin + b cos) for the channels (i, i + R/2), or
+ *   (2i, 2i + 1) under GBLA_ROPE_PAIRS; channels from R on keep xn.
+ *   q [B,H,n,d] or [H,T,d], k [B,K,n,d] or [K,T,d]; q_w [H,d], k_w [K,d] fp32
+ *   positions  int32 [B,n] or [T], or NULL: each token's index in its sequence
+ *   q_out, k_out  like q, k; each may be the buffer of its own input
+ * Angles are reduced in 64 bits, so far positions keep fp32's accuracy.
+ * q_w and k_w may be NULL under GBLA_NO_NORM.
+ */
+gbla_status gbla_qk_norm_rope(const gbla_rope_shape* shape, const void* q, const void* k,
+                              const float* q_w, const float* k_w, const int32_t* positions,
+                              const int32_t* cu_seqlens, void* q_out, void* k_out, void* stream);
+
+/* Scratch bytes of gbla_qk_norm_rope_backward; 0 if the shape is not accepted. */
+size_t gbla_qk_norm_rope_backward_workspace_bytes(const gbla_rope_shape* shape);
+
+/*
+ * Gradients of L = sum(q_out * dq_out) + sum(k_out * dk_out):
+ *   dq_out, dk_out  like q, k      dq, dk  like q, k (each may be the buffer of
+ *   its own dq_out / dk_out)       dq_w [H,d], dk_w [K,d] fp32
+ * dq_w and dk_w are sums over all tokens, in an order fixed by the shape; they
+ * are not written (and may be NULL) under GBLA_NO_NORM.
+ */
+gbla_status gbla_qk_norm_rope_backward(const gbla_rope_shape* shape, const void* q, const void* k,
+                                       const float* q_w, const float* k_w,
+                                       const int32_t* positions, const int32_t* cu_seqlens,
+                                       const void* dq_out, const void* dk_out, void* workspace,
+                                       size_t workspace_bytes, void* dq, void* dk, float* dq_w,
+                                       float* dk_w, void* stream);
+
+typedef struct {
+  int32_t batch;      /* B (dense), N_s (ragged) or rows (gbla_decay_step), >= 1   */
+  int32_t seqlen;     /* n (dense) or T (ragged), >= 0; 1 for gbla_decay_step     */
+  int32_t heads;      /* H: heads of q and the output, a multiple of kv_heads     */
+  int32_t kv_heads;   /* K >= 1: heads of k, v, the decays and the states         */
+  int32_t head_dim;   /* d in {32, 64, 128}, of keys and values                  */
+  int32_t max_seqlen; /* ragged: an upper bound of the lengths (>= 0); dense: 0.
+                         It only chooses kernels                                 */
+  int32_t dtype;      /* gbla_dtype of q, k, v, the output and their gradients   */
+  float scale;        /* factor of the output (finite), usually d^-1/2           */
+} gbla_decay_shape;
+
+/* Scratch bytes of gbla_decay_forward / gbla_decay_backward (the larger of the
+ * dense and the ragged reading, for every max_seqlen); 0 if neither is accepted. */
+size_t gbla_decay_workspace_bytes(const gbla_decay_shape* shape);
+size_t gbla_decay_backward_workspace_bytes(const gbla_decay_shape* shape);
+
+/*
+ * Causal linear attention with a decay per key head, g = log_decay[h]:
+ *   S_t = exp(g) S_{t-1} + k_t v_t^T,    o_t = scale * S_t^T q_t
+ * computed in chunks.  S starts from initial_state (zeros if NULL).
+ *   q [B,H,n,d] or [H,T,d]; k, v [B,K,n,d] or [K,T,d]; log_decay [K] fp32,
+ *   g <= 0 (-inf: no memory, o_t = scale (q_t k_t) v_t)
+ *   initial_state  fp32 [N,K,d,d] ([c][e]: key channel, value channel) or NULL
+ *   out            [B,H,n,d] or [H,T,d]
+ *   final_state    fp32 [N,K,d,d] or NULL (not wanted); may be initial_state.
+ *                  An empty sequence's is its initial state.
+ * States are sums in fp32 of products with fp32's accuracy for both types; in
+ * bf16 the products that form the output round their decayed score and the state
+ * to fewer bits before the output is rounded.
+ */
+gbla_status gbla_decay_forward(const gbla_decay_shape* shape, const void* q, const void* k,
+                               const void* v, const float* log_decay,
+                               const float* initial_state, const int32_t* cu_seqlens,
+                               void* workspace, size_t workspace_bytes, void* out,
+                               float* final_state, void* stream);
+
+/*
+ * Gradients of L = sum(out * dout) + sum(final_state * dfinal_state):
+ *   dout            like q            dfinal_state  fp32 [N,K,d,d] or NULL (zeros)
+ *   dq              like q            dk, dv        like k, v (summed over the
+ *                                     query heads that share them)
+ *   dlog_decay      fp32 [K], summed over the batch, or NULL (not wanted)
+ *   dinitial_state  fp32 [N,K,d,d] or NULL (not wanted); may be dfinal_state
+ * Reductions run in an order fixed by the shape: repeated calls give the same
+ * bits.
+ */
+gbla_status gbla_decay_backward(const gbla_decay_shape* shape, const void* q, const void* k,
+                                const void* v, const float* log_decay,
+                                const float* initial_state, const int32_t* cu_seqlens,
+                                const void* dout, const float* dfinal_state, void* workspace,
+                                size_t workspace_bytes, void* dq, void* dk, void* dv,
+                                float* dlog_decay, float* dinitial_state, void* stream);
+
+/*
+ * The same recurrence for one new token of each of shape->batch rows:
+ *   state[s] = exp(g) state[s] + k v^T,   out = scale * state[s]^T q
+ *   q, out [N,H,d]; k, v [N,K,d]; log_decay [K] fp32
+ *   state          fp32 [slots,K,d,d], updated in place
+ *   state_indices  int32 [N], the slot s of each row, or NULL: row n has slot n
+ *                  (slots >= N)
+ * Rows that name the same slot are applied in row order.  A row whose index is
+ * outside [0, slots) is skipped: no state changes and its output row is left.
+ */
+gbla_status gbla_decay_step(const gbla_decay_shape* shape, const void* q, const void* k,
+                            const void* v, const float* log_decay, const int32_t* state_indices,
+                            int32_t slots, float* state, void* out, void* stream);
+
 /* A static, human-readable name of a status code (never NULL). */
 const char* gbla_status_string(gbla_status status);
 

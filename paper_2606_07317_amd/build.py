@@ -19,7 +19,10 @@ SOURCES = [os.path.join(CSRC, "gbla_kernels.hip"), os.path.join(CSRC, "gbla_stre
            os.path.join(CSRC, "gbla_rows.hip"),
            os.path.join(CSRC, "gbla_plan.cpp"), os.path.join(CSRC, "gbla_ext_plan.cpp"),
            os.path.join(CSRC, "gbla_api.cpp"), os.path.join(CSRC, "gbla_ceiling.hip"),
-           os.path.join(CSRC, "gbla_noalloc.hip")]
+           os.path.join(CSRC, "gbla_noalloc.hip"),
+           os.path.join(CSRC, "gbla_rope.hip"), os.path.join(CSRC, "gbla_decay.hip"),
+           os.path.join(CSRC, "gbla_decay_back.hip"), os.path.join(CSRC, "gbla_decay_step.hip"),
+           os.path.join(CSRC, "gbla_decay_plan.cpp"), os.path.join(CSRC, "gbla_decay_api.cpp")]
 
 # Packed fp32 VALU ops are switched off for all device code; hipcc's host
 # pass warns that it does not know the feature, which is harmless.

@@ -1,0 +1,140 @@
+// gbla_decay_plan.cpp -- plans of the decoder's operators: split sizes and
+// workspace layouts, a function of the shape alone.
+#include <math.h>
+#include <stdint.h>
+
+#include "gbla.h"
+#include "gbla_decay.h"
+
+namespace gbla {
+namespace {
+
+constexpr int64_t kMaxGridX = 2147483647LL;
+constexpr int kMaxGridY = 65535;
+
+bool head_dim_ok(int32_t d) { return d == 32 || d == 64 || d == 128; }
+bool dtype_ok(int32_t t) { return t == GBLA_F32 || t == GBLA_BF16; }
+
+// Tokens of a unit: short enough for about `want` workgroups, long enough that
+// the d x d record of a unit stays small beside its tokens.
+int32_t unit_tokens(const DecayPlan& p) {
+  const int64_t want = p.d == 128 ? 512 : 1024;
+  int32_t unit = kMaxUnit;
+  while (unit > 2 * kTile && p.tokens * p.kv_heads < (int64_t)unit * want) unit /= 2;
+  return unit;
+}
+
+// Whether a workgroup walks a whole sequence: where no sequence is longer than a
+// few units, or the (sequence, key head) pairs alone fill the chip.
+bool walk_whole(const DecayPlan& p, int64_t longest) {
+  if (longest <= 4 * kTile || longest <= p.unit) return true;
+  const int64_t pairs = p.d == 128 ? 256 : 512;
+  return longest * pairs <= p.tokens * p.kv_heads;
+}
+
+}  // namespace
+
+gbla_status make_decay_plan(const gbla_decay_shape* s, bool ragged, bool backward, DecayPlan* p) {
+  if (!s || !p) return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->batch < 1 || s->seqlen < 0 || s->heads < 1 || s->kv_heads < 1)
+    return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->heads % s->kv_heads != 0) return GBLA_ERR_INVALID_ARGUMENT;
+  if (!isfinite(s->scale)) return GBLA_ERR_INVALID_ARGUMENT;
+  if (ragged && s->max_seqlen < 0) return GBLA_ERR_INVALID_ARGUMENT;
+  if (!head_dim_ok(s->head_dim) || !dtype_ok(s->dtype)) return GBLA_ERR_UNSUPPORTED;
+  if (s->heads > kMaxGridY) return GBLA_ERR_UNSUPPORTED;
+  DecayPlan q{};
+  q.nseq = s->batch;
+  q.rows = s->seqlen;
+  q.heads = s->heads;
+  q.kv_heads = s->kv_heads;
+  q.group = s->heads / s->kv_heads;
+  q.d = s->head_dim;
+  q.dtype = s->dtype;
+  q.ragged = ragged ? 1 : 0;
+  q.scale = s->scale;
+  q.tokens = ragged ? (int64_t)s->seqlen : (int64_t)s->batch * s->seqlen;
+  q.unit = unit_tokens(q);
+  // sum over the sequences of max(1, ceil(len / unit)) <= tokens / unit + N
+  const int64_t cap = q.tokens / q.unit + q.nseq;
+  if (cap > kMaxGridX) return GBLA_ERR_UNSUPPORTED;
+  if (ragged) {
+    q.units = (int32_t)cap;
+  } else {
+    int64_t each = ((int64_t)q.rows + q.unit - 1) / q.unit;
+    if (each < 1) each = 1;
+    q.units_per_seq = (int32_t)each;
+    q.units = (int32_t)(each * q.nseq);
+  }
+  q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows) ? 1 : 0;
+  q.grid_units = q.single ? q.nseq : q.units;
+  const size_t states = (size_t)cap * q.kv_heads * q.d * q.d * sizeof(float);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes, 256);
+    return at;
+  };
+  q.off_S = take(states);
+  if (backward) {
+    q.off_D = take(states);
+    q.off_dg = take(2 * (size_t)cap * q.kv_heads * 8 * sizeof(double));
+  }
+  q.total_bytes = off;
+  *p = q;
+  return GBLA_OK;
+}
+
+gbla_status make_rope_plan(const gbla_rope_shape* s, bool ragged, bool backward, RopePlan* p) {
+  if (!s || !p) return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->batch < 1 || s->seqlen < 0 || s->heads < 1 || s->kv_heads < 1)
+    return GBLA_ERR_INVALID_ARGUMENT;
+  if (!(s->eps >= 0.0f) || !isfinite(s->eps)) return GBLA_ERR_INVALID_ARGUMENT;
+  if (!(s->theta > 0.0f) || !isfinite(s->theta)) return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->flags & ~(uint32_t)(GBLA_NO_NORM | GBLA_ROPE_PAIRS)) return GBLA_ERR_INVALID_ARGUMENT;
+  if (!head_dim_ok(s->head_dim) || !dtype_ok(s->dtype)) return GBLA_ERR_UNSUPPORTED;
+  if (s->rotary_dim < 0 || s->rotary_dim > s->head_dim || s->rotary_dim % 8 != 0)
+    return GBLA_ERR_UNSUPPORTED;
+  if (s->heads > kMaxGridY || s->kv_heads > kMaxGridY) return GBLA_ERR_UNSUPPORTED;
+  RopePlan q{};
+  q.nseq = s->batch;
+  q.rows = s->seqlen;
+  q.heads = s->heads;
+  q.kv_heads = s->kv_heads;
+  q.d = s->head_dim;
+  q.rotary = s->rotary_dim;
+  q.dtype = s->dtype;
+  q.ragged = ragged ? 1 : 0;
+  q.eps = s->eps;
+  q.flags = s->flags;
+  q.tokens = ragged ? (int64_t)s->seqlen : (int64_t)s->batch * s->seqlen;
+  q.tile = 256 / (q.d / 8);
+  const int64_t tiles = (q.tokens + q.tile - 1) / q.tile;
+  // Workgroups of one pass and up to eight heads; fewer heads while that gives
+  // few workgroups.
+  const int32_t all = q.heads + q.kv_heads;
+  q.heads_each = 8;
+  while (q.heads_each > 1 && tiles * ((all + q.heads_each - 1) / q.heads_each) < 1024)
+    q.heads_each /= 2;
+  q.head_blocks = (all + q.heads_each - 1) / q.heads_each;
+  if (q.head_blocks > kMaxGridY) return GBLA_ERR_UNSUPPORTED;
+  // The backward's workgroups leave a partial sum each: more passes where there
+  // are many, so that few are added up.
+  int64_t passes = 1;
+  if (backward)
+    while (tiles / passes * q.head_blocks > 2048 && passes < 16) passes *= 2;
+  q.passes = (int32_t)passes;
+  const int64_t blocks = (tiles + passes - 1) / passes;
+  if (blocks > kMaxGridX) return GBLA_ERR_UNSUPPORTED;
+  q.blocks = (int32_t)blocks;
+  for (int i = 0; i < q.rotary / 2; ++i)
+    q.turns[i] = pow((double)s->theta, -2.0 * i / q.rotary) / (2.0 * 3.14159265358979323846);
+  *p = q;
+  return GBLA_OK;
+}
+
+size_t rope_partial_bytes(const RopePlan& p) {
+  return align_up((size_t)p.blocks * (p.heads + p.kv_heads) * p.d * sizeof(float), 256);
+}
+
+}  // namespace gbla

@@ -8,6 +8,7 @@ the library is not built this module raises; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -26,6 +27,7 @@ NO_GATE = 1   # uniform key gates; gate_logits may be None
 NO_CONV = 2   # identity Conv1D; conv_w may be None
 NO_NORM = 4   # out = o; out_gate and norm_w may be None
 BLA = NO_GATE | NO_CONV | NO_NORM
+ROPE_PAIRS = 8  # qk_norm_rope: adjacent channels rotate together
 STATUS_NAMES = {0: "GBLA_OK", 1: "GBLA_ERR_INVALID_ARGUMENT", 2: "GBLA_ERR_UNSUPPORTED",
                 3: "GBLA_ERR_MISALIGNED", 4: "GBLA_ERR_WORKSPACE", 5: "GBLA_ERR_HIP"}
 
@@ -48,6 +50,19 @@ class LayerShape(ctypes.Structure):
                 ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("conv_width", ctypes.c_int32), ("max_seqlen", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class RopeShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("theta", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class DecayShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_seqlen", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -93,6 +108,23 @@ def load_library(path: str = LIB_PATH):
     lib.gbla_layer_project.restype = ctypes.c_int
     lib.gbla_layer_forward.argtypes = [LP, P, P, P, P, P, P, sz, P, P]
     lib.gbla_layer_forward.restype = ctypes.c_int
+    RP, DP = ctypes.POINTER(RopeShape), ctypes.POINTER(DecayShape)
+    lib.gbla_qk_norm_rope.argtypes = [RP] + [P] * 9
+    lib.gbla_qk_norm_rope.restype = ctypes.c_int
+    lib.gbla_qk_norm_rope_backward_workspace_bytes.argtypes = [RP]
+    lib.gbla_qk_norm_rope_backward_workspace_bytes.restype = sz
+    lib.gbla_qk_norm_rope_backward.argtypes = [RP] + [P] * 9 + [sz] + [P] * 5
+    lib.gbla_qk_norm_rope_backward.restype = ctypes.c_int
+    lib.gbla_decay_workspace_bytes.argtypes = [DP]
+    lib.gbla_decay_workspace_bytes.restype = sz
+    lib.gbla_decay_backward_workspace_bytes.argtypes = [DP]
+    lib.gbla_decay_backward_workspace_bytes.restype = sz
+    lib.gbla_decay_forward.argtypes = [DP] + [P] * 7 + [sz] + [P] * 3
+    lib.gbla_decay_forward.restype = ctypes.c_int
+    lib.gbla_decay_backward.argtypes = [DP] + [P] * 9 + [sz] + [P] * 6
+    lib.gbla_decay_backward.restype = ctypes.c_int
+    lib.gbla_decay_step.argtypes = [DP] + [P] * 5 + [ctypes.c_int32] + [P] * 3
+    lib.gbla_decay_step.restype = ctypes.c_int
     lib.gbla_status_string.argtypes = [ctypes.c_int]
     lib.gbla_status_string.restype = ctypes.c_char_p
     if path == LIB_PATH:
@@ -486,4 +518,278 @@ def layer_forward(x, conv_x, w_proj, norm_w, eps: float = 1e-6, cu_seqlens=None,
         ctypes.byref(shape), _ptr(x), _ptr(conv_x), _ptr(w_proj), _ptr(norm_w), _ptr(cu_seqlens),
         _ptr(workspace), workspace.numel(), _ptr(out), _stream(stream))
     _raise(st, "gbla_layer_forward")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# The decoder's operators: norm and rotation of queries and keys, and causal
+# linear attention with a decay.
+# ---------------------------------------------------------------------------
+_HERE = contextlib.nullcontext()
+
+
+def _on(device, stream):
+    """A context in which ``device`` is current and ``stream`` (a torch stream, a HIP
+    handle, or None for the device's current one) is its current stream, so that
+    what a call allocates belongs to the stream that it runs on."""
+    if stream is None:
+        return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    if not hasattr(stream, "cuda_stream"):
+        handle = int(stream)
+        stream = (torch.cuda.ExternalStream(handle, device=device) if handle
+                  else torch.cuda.default_stream(device))
+    if stream.device != device:
+        raise ValueError("stream is on %s, the tensors on %s" % (stream.device, device))
+    return torch.cuda.stream(stream)
+
+
+def _like(t, name, shape, dtype, device):
+    """``t`` if it can take an output of this shape and type, else a new tensor."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _check(t, name, dtype, device)
+    if t.shape != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return t
+
+
+def _want(t, name, shape, dtype, device):
+    _check(t, name, dtype, device)
+    if t.shape != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+
+
+def _query_key(q, k, cu_seqlens):
+    """Batch, tokens per head, head counts and head dim of q and k, which may have
+    different head counts."""
+    _check(q, "q")
+    _check(k, "k", q.dtype, q.device)
+    if cu_seqlens is None:
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("dense q and k must be [B, H, n, d]")
+        B, H, n, d = q.shape
+        if k.shape[0] != B or k.shape[2:] != q.shape[2:]:
+            raise ValueError("k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
+        return B, n, H, k.shape[1], d
+    _check(cu_seqlens, "cu_seqlens", torch.int32, q.device)
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+        raise ValueError("cu_seqlens must be [N + 1]")
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("ragged q and k must be [H, T, d]")
+    if k.shape[1:] != q.shape[1:]:
+        raise ValueError("k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
+    return cu_seqlens.numel() - 1, q.shape[1], q.shape[0], k.shape[0], q.shape[2]
+
+
+def rope_shape(q, k, cu_seqlens=None, rotary_dim=None, theta: float = 10000.0, eps: float = 1e-6,
+               flags: int = 0) -> RopeShape:
+    B, n, H, K, d = _query_key(q, k, cu_seqlens)
+    return RopeShape(B, n, H, K, d, d if rotary_dim is None else int(rotary_dim), _dtype_code(q),
+                     float(eps), float(theta), int(flags))
+
+
+def _check_rope(q, k, q_w, k_w, positions, cu_seqlens, shape):
+    dev = q.device
+    if not shape.flags & NO_NORM:
+        _want(q_w, "q_w", (shape.heads, shape.head_dim), torch.float32, dev)
+        _want(k_w, "k_w", (shape.kv_heads, shape.head_dim), torch.float32, dev)
+    if positions is not None:
+        rows = (shape.batch, shape.seqlen) if cu_seqlens is None else (shape.seqlen,)
+        _want(positions, "positions", rows, torch.int32, dev)
+
+
+def qk_norm_rope(q, k, q_w, k_w, positions=None, cu_seqlens=None, rotary_dim=None,
+                 theta: float = 10000.0, eps: float = 1e-6, flags: int = 0, q_out=None, k_out=None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """RMS norm of every head's queries and keys (weights q_w [H, d], k_w [K, d]), then
+    the rotation of their first ``rotary_dim`` channels (default: all) by position;
+    see include/gbla.h.  q [B, H, n, d] or [H, T, d], k with its own head count;
+    ``positions`` int32 [B, n] or [T], by default each token's index in its sequence.
+    ``flags``: NO_NORM (q_w, k_w may be None), ROPE_PAIRS.  Returns the rotated q and
+    k in their type; ``q_out`` / ``k_out`` may be q / k themselves."""
+    shape = rope_shape(q, k, cu_seqlens, rotary_dim, theta, eps, flags)
+    _check_rope(q, k, q_w, k_w, positions, cu_seqlens, shape)
+    dev = q.device
+    with _on(dev, stream):
+        q_out = _like(q_out, "q_out", q.shape, q.dtype, dev)
+        k_out = _like(k_out, "k_out", k.shape, q.dtype, dev)
+        st = load_library().gbla_qk_norm_rope(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_w), _ptr(k_w), _ptr(positions),
+            _ptr(cu_seqlens), _ptr(q_out), _ptr(k_out), torch.cuda.current_stream(dev).cuda_stream)
+    _raise(st, "gbla_qk_norm_rope")
+    return q_out, k_out
+
+
+def qk_norm_rope_backward_workspace_bytes(shape: RopeShape) -> int:
+    n = load_library().gbla_qk_norm_rope_backward_workspace_bytes(ctypes.byref(shape))
+    if n == 0:
+        raise GblaError(1, "gbla_qk_norm_rope_backward_workspace_bytes")
+    return int(n)
+
+
+def qk_norm_rope_backward(q, k, q_w, k_w, dq_out, dk_out, positions=None, cu_seqlens=None,
+                          rotary_dim=None, theta: float = 10000.0, eps: float = 1e-6,
+                          flags: int = 0, workspace=None, grads: Optional[dict] = None,
+                          stream=None) -> dict:
+    """Gradients of sum(q_out * dq_out) + sum(k_out * dk_out) for the inputs of
+    qk_norm_rope: a dict with dq, dk (in q's type) and, unless NO_NORM, dq_w, dk_w
+    (fp32).  ``grads`` may hold outputs under those names; dq / dk may be dq_out /
+    dk_out themselves."""
+    shape = rope_shape(q, k, cu_seqlens, rotary_dim, theta, eps, flags)
+    _check_rope(q, k, q_w, k_w, positions, cu_seqlens, shape)
+    dev = q.device
+    _want(dq_out, "dq_out", q.shape, q.dtype, dev)
+    _want(dk_out, "dk_out", k.shape, q.dtype, dev)
+    need = qk_norm_rope_backward_workspace_bytes(shape)
+    g = dict(grads or {})
+    with _on(dev, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check_ws(workspace, dev, need)
+        g["dq"] = _like(g.get("dq"), "dq", q.shape, q.dtype, dev)
+        g["dk"] = _like(g.get("dk"), "dk", k.shape, q.dtype, dev)
+        if not flags & NO_NORM:
+            g["dq_w"] = _like(g.get("dq_w"), "dq_w", q_w.shape, torch.float32, dev)
+            g["dk_w"] = _like(g.get("dk_w"), "dk_w", k_w.shape, torch.float32, dev)
+        st = load_library().gbla_qk_norm_rope_backward(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_w), _ptr(k_w), _ptr(positions),
+            _ptr(cu_seqlens), _ptr(dq_out), _ptr(dk_out), _ptr(workspace), workspace.numel(),
+            _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g.get("dq_w")), _ptr(g.get("dk_w")),
+            torch.cuda.current_stream(dev).cuda_stream)
+    _raise(st, "gbla_qk_norm_rope_backward")
+    return g
+
+
+def decay_shape(q, k, scale: Optional[float] = None, cu_seqlens=None, max_seqlen=None) -> DecayShape:
+    B, n, H, K, d = _query_key(q, k, cu_seqlens)
+    msl = 0
+    if cu_seqlens is not None:
+        msl = int(max_seqlen) if max_seqlen is not None else n
+    return DecayShape(B, n, H, K, d, msl, _dtype_code(q),
+                      float(d) ** -0.5 if scale is None else float(scale))
+
+
+def decay_workspace_bytes(shape: DecayShape) -> int:
+    n = load_library().gbla_decay_workspace_bytes(ctypes.byref(shape))
+    if n == 0:
+        raise GblaError(1, "gbla_decay_workspace_bytes")
+    return int(n)
+
+
+def decay_backward_workspace_bytes(shape: DecayShape) -> int:
+    n = load_library().gbla_decay_backward_workspace_bytes(ctypes.byref(shape))
+    if n == 0:
+        raise GblaError(1, "gbla_decay_backward_workspace_bytes")
+    return int(n)
+
+
+def _check_decay(q, k, v, log_decay, shape, states):
+    dev = q.device
+    _want(v, "v", k.shape, q.dtype, dev)
+    _want(log_decay, "log_decay", (shape.kv_heads,), torch.float32, dev)
+    for t, name in states:
+        if t is not None:
+            _want(t, name, (shape.batch, shape.kv_heads, shape.head_dim, shape.head_dim),
+                  torch.float32, dev)
+
+
+def decay_attention(q, k, v, log_decay, scale: Optional[float] = None, initial_state=None,
+                    final_state=None, cu_seqlens=None, max_seqlen=None, workspace=None, out=None,
+                    stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Causal linear attention with a decay per key head, S_t = exp(g) S_{t-1} +
+    k_t v_t^T, o_t = scale S_t^T q_t (scale d^-1/2 by default); see include/gbla.h.
+    q [B, H, n, d] or [H, T, d]; k, v with K heads, K dividing H; log_decay [K] fp32,
+    <= 0; ``initial_state`` fp32 [N, K, d, d] or None (zeros).  Returns the output in
+    q's type and the final state: None, or ``final_state`` if that is a tensor (it may
+    be initial_state, updated in place), or a new tensor if it is True.
+    ``max_seqlen`` (ragged) is an upper bound of the lengths; it only chooses kernels."""
+    shape = decay_shape(q, k, scale, cu_seqlens, max_seqlen)
+    given = final_state if isinstance(final_state, torch.Tensor) else None
+    _check_decay(q, k, v, log_decay, shape, ((initial_state, "initial_state"), (given, "final_state")))
+    dev = q.device
+    need = decay_workspace_bytes(shape)
+    with _on(dev, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check_ws(workspace, dev, need)
+        out = _like(out, "out", q.shape, q.dtype, dev)
+        if given is None and final_state:
+            d = shape.head_dim
+            given = torch.empty((shape.batch, shape.kv_heads, d, d), dtype=torch.float32, device=dev)
+        st = load_library().gbla_decay_forward(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(initial_state),
+            _ptr(cu_seqlens), _ptr(workspace), workspace.numel(), _ptr(out), _ptr(given),
+            torch.cuda.current_stream(dev).cuda_stream)
+    _raise(st, "gbla_decay_forward")
+    return out, given
+
+
+def decay_attention_backward(q, k, v, log_decay, dout, scale: Optional[float] = None,
+                             initial_state=None, dfinal_state=None, cu_seqlens=None,
+                             max_seqlen=None, workspace=None, grads: Optional[dict] = None,
+                             decay_grad: bool = True, stream=None) -> dict:
+    """Gradients of sum(out * dout) + sum(final_state * dfinal_state) for the inputs of
+    decay_attention: a dict with dq, dk, dv (in q's type), dlog_decay (fp32 [K]; left out
+    with ``decay_grad`` False, for fixed decays) and, if initial_state is given,
+    dinitial_state (fp32).  ``grads`` may hold outputs under
+    those names; dinitial_state may be dfinal_state itself."""
+    shape = decay_shape(q, k, scale, cu_seqlens, max_seqlen)
+    g = dict(grads or {})
+    _check_decay(q, k, v, log_decay, shape,
+                 ((initial_state, "initial_state"), (dfinal_state, "dfinal_state"),
+                  (g.get("dinitial_state"), "dinitial_state")))
+    dev = q.device
+    _want(dout, "dout", q.shape, q.dtype, dev)
+    need = decay_backward_workspace_bytes(shape)
+    with _on(dev, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check_ws(workspace, dev, need)
+        g["dq"] = _like(g.get("dq"), "dq", q.shape, q.dtype, dev)
+        g["dk"] = _like(g.get("dk"), "dk", k.shape, q.dtype, dev)
+        g["dv"] = _like(g.get("dv"), "dv", k.shape, q.dtype, dev)
+        if decay_grad:
+            g["dlog_decay"] = _like(g.get("dlog_decay"), "dlog_decay", log_decay.shape, torch.float32,
+                                    dev)
+        if initial_state is not None and g.get("dinitial_state") is None:
+            g["dinitial_state"] = torch.empty_like(initial_state)
+        st = load_library().gbla_decay_backward(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(initial_state),
+            _ptr(cu_seqlens), _ptr(dout), _ptr(dfinal_state), _ptr(workspace), workspace.numel(),
+            _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]),
+            _ptr(g["dlog_decay"]) if decay_grad else None, _ptr(g.get("dinitial_state")), torch.cuda.current_stream(dev).cuda_stream)
+    _raise(st, "gbla_decay_backward")
+    return g
+
+
+def decay_step(q, k, v, log_decay, state, state_indices=None, scale: Optional[float] = None,
+               out=None, stream=None) -> torch.Tensor:
+    """decay_attention for one new token of each row: q [N, H, d], k, v [N, K, d],
+    ``state`` fp32 [slots, K, d, d], updated in place.  Row n uses slot
+    state_indices[n] (int32 [N]; without indices slot n).  Rows of one slot are applied
+    in row order; a row whose index is outside the slots is skipped and its output row
+    left as it is.  Returns the output [N, H, d] in q's type."""
+    _check(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q must be [N, H, d]")
+    N, H, d = q.shape
+    dev = q.device
+    if not isinstance(k, torch.Tensor) or k.dim() != 3 or k.shape[0] != N or k.shape[2] != d:
+        raise ValueError("k must be [N, K, d]")
+    K = k.shape[1]
+    _check(k, "k", q.dtype, dev)
+    _want(v, "v", k.shape, q.dtype, dev)
+    _want(log_decay, "log_decay", (K,), torch.float32, dev)
+    _check(state, "state", torch.float32, dev)
+    if state.dim() != 4 or state.shape[1:] != (K, d, d):
+        raise ValueError("state must be [slots, K, d, d]")
+    if state_indices is not None:
+        _want(state_indices, "state_indices", (N,), torch.int32, dev)
+    shape = DecayShape(N, 1, H, K, d, 0, _dtype_code(q), float(d) ** -0.5 if scale is None else float(scale))
+    with _on(dev, stream):
+        out = _like(out, "out", q.shape, q.dtype, dev)
+        st = load_library().gbla_decay_step(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state_indices),
+            state.shape[0], _ptr(state), _ptr(out), torch.cuda.current_stream(dev).cuda_stream)
+    _raise(st, "gbla_decay_step")
     return out
