@@ -27,6 +27,17 @@
 namespace gbla {
 namespace {
 
+// The sizes that each kernel takes.
+template <typename T, int D>
+using RecordSizes = DC<T, D, D, D == 128 ? 8 : 4, 1, false>;
+// At d = 128 a walk is two workgroups, each with half of the value channels: two run on
+// a CU, so that one's matrix products meet the other's vector work.  (One of eight waves,
+// which the barriers keep in step: its time was the sum of the matrix, the vector and the
+// LDS work.)  Two parts of the state and of the scores leave 2^-17 of a term, far below
+// the bf16 rounding of the results that they form.
+template <typename T, int D>
+using WalkSizes = DC<T, D, D == 128 ? 64 : D, 4, 2, true>;
+
 // Records: the sum of a unit's own products, A^T (weights B).
 //   Reverse = false: weights lam^(tokens of the unit after t), for the state after it;
 //   Reverse = true: scale lam^(tokens of the unit up to t), for the gradient of the
@@ -35,31 +46,25 @@ namespace {
 template <typename T, int D, bool Reverse>
 __device__ __forceinline__ void record_unit(const DecayPlan& P, const Span& sp, int h, const T* A,
                                             const T* B, int heads, int group, float g, float* rec,
-                                            unsigned char* ldsA, unsigned char* ldsB) {
-  using C = DC<T, D>;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), gg = lane >> 4;
+                                            unsigned char* ldsA, unsigned char* ldsB, Powers& pw) {
+  using C = RecordSizes<T, D>;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Decay lam(g);
   const float full = lam(kTile);
   const int n = sp.end - sp.begin, tiles = (n + kTile - 1) / kTile, steps = tiles * group;
-  float weight[2][8];
-  State<T, C> S, add;
+  State<T, C> S;
   S.clear();
-  TileLoad<C> la, lb;
+  TileLoad<T, C, D> la, lb;
+  const int64_t row0 = first_row(P, sp, heads, h * group);
   auto fetch = [&](int step) {
-    const int i = step / group, head = h * group + step % group;
+    const int i = step / group;
     const int t = sp.begin + (Reverse ? tiles - 1 - i : i) * kTile;
-    const int64_t row = row_of(P, sp, heads, head, t) * D;
+    const int64_t row = (row0 + (int64_t)(step % group) * P.rows + t) * D;
     la.load(A + row, sp.end - t);
     lb.load(B + row, sp.end - t);
   };
   if (steps > 0) fetch(0);
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int t = 32 * ks + 8 * gg + j;
-      weight[ks][j] = Reverse ? P.scale * lam(t + 1) : lam(kTile - 1 - t);
-    }
+  pw.fill(lam, P.scale);
   for (int step = 0; step < steps; ++step) {
     const int i = step / group, gi = step % group;
     const int live = min(kTile, sp.end - (sp.begin + (Reverse ? tiles - 1 - i : i) * kTile));
@@ -67,88 +72,115 @@ __device__ __forceinline__ void record_unit(const DecayPlan& P, const Span& sp, 
     lb.store(ldsB);
     lds_barrier();
     if (step + 1 < steps) fetch(step + 1);
-    if (gi == 0) add.clear();
-    add.add_products(ldsA, ldsB, weight, w, lane);
-    if (gi == group - 1) S.advance(live == kTile ? full : lam(live), add);
+    const float f = gi > 0 ? 1.0f : live == kTile ? full : lam(live);
+    S.advance(f, ldsA, ldsB, Reverse ? pw.up : pw.down, w, lane);
     lds_barrier();
   }
-  S.store(rec, false, w, lane);
+  S.store(rec, 0, w, lane);
 }
 
 // blockIdx.z = 0: records of the state (k or v by v or k), 1 (backward): of its
 // gradient.
 template <typename T, int D>
-__global__ void __launch_bounds__((DC<T, D>::NT), 1)
+__global__ void __launch_bounds__((RecordSizes<T, D>::NT), 2)
 record_kernel(DecayPlan P, const T* A, const T* B, const T* q, const T* dout,
               const float* log_decay, const int32_t* cu, float* recS, float* recD) {
-  using C = DC<T, D>;
-  __shared__ __attribute__((aligned(16))) unsigned char ldsA[C::kTileBytes], ldsB[C::kTileBytes];
+  using C = RecordSizes<T, D>;
+  __shared__ __attribute__((aligned(512))) unsigned char ldsA[kTile * C::Wide::kPitch],
+      ldsB[kTile * C::Wide::kPitch];
+  __shared__ __attribute__((aligned(16))) Powers pw;
   Span sp;
   if (!find_span<C::NT>(P, cu, blockIdx.x, &sp)) return;
   const int h = blockIdx.y;
   const size_t at = ((size_t)h * P.units + sp.slot) * (D * D);
   if (blockIdx.z == 0) {
     if (sp.last) return;
-    record_unit<T, D, false>(P, sp, h, A, B, P.kv_heads, 1, log_decay[h], recS + at, ldsA, ldsB);
+    record_unit<T, D, false>(P, sp, h, A, B, P.kv_heads, 1, log_decay[h], recS + at, ldsA, ldsB,
+                              pw);
   } else {
     if (sp.idx == 0) return;
-    record_unit<T, D, true>(P, sp, h, q, dout, P.heads, P.group, log_decay[h], recD + at, ldsA, ldsB);
+    record_unit<T, D, true>(P, sp, h, q, dout, P.heads, P.group, log_decay[h], recD + at, ldsA, ldsB,
+                              pw);
   }
 }
 
-// The records become the state before each unit (z even) or the gradient of the
-// state after each unit (z odd), in place: four elements a thread, unit after unit.
+// The records become the state before each unit (the first parts) or the
+// gradient of the state after each unit (the others), in place.  A workgroup takes 256
+// elements; its waves take consecutive quarters of up to 4 * kScanUnits units, whose
+// records they hold in registers: each sums its own, the sums go from wave to wave
+// through LDS, and each carries what enters its quarter over its records.  Bound by
+// memory: both sides of 16 packed sequences (57,511 tokens, d = 128, H = 8, 126 MB of
+// records) 65 us, 3.9 TB/s.
+constexpr int kScanUnits = 8;
 template <int D>
 __global__ void __launch_bounds__(kThreads)
 scan_kernel(DecayPlan P, const float* log_decay, const int32_t* cu, const float* S0, bool transposed,
             float* recS, const float* dfinal, float* recD) {
-  const int s = blockIdx.x, h = blockIdx.y;
-  const bool back = blockIdx.z >= gridDim.z / (recD ? 2 : 1);
-  const int part = back ? blockIdx.z - gridDim.z / 2 : blockIdx.z;
-  int first, len;
-  if (P.ragged) {
-    first = units_before(cu, s, P.unit);
-    len = cu[s + 1] - cu[s];
-  } else {
-    first = s * P.units_per_seq;
-    len = P.rows;
-  }
+  constexpr int W = kThreads / 64, R = kScanUnits, slices = D * D / 256;
+  __shared__ f32x4_t sums[2][W][64];
+  // Neighbouring workgroups take neighbouring slices, so that those in flight read
+  // whole records: slices of one offset in many records lie on few memory channels (with
+  // the slice as the slowest grid index the same took 126 us).
+  const int parts = recD ? 2 * slices : slices, s = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int h = blockIdx.y, lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool back = part >= slices;
+  const int len = P.ragged ? cu[s + 1] - cu[s] : P.rows;
+  const int first = P.ragged ? first_slot(P, cu[s], s) : s * P.units_per_seq;
   const int units = units_of(len, P.unit);
-  const int el = (part * kThreads + threadIdx.x) * 4;
-  if (el >= D * D) return;
+  const int el = ((part - (back ? slices : 0)) * 64 + lane) * 4;
   const Decay lam(log_decay[h]);
   const float full = lam(P.unit);
+  // Unit i of the walk (backwards from the last): its record, and its decay.  Only
+  // the sequence's last unit may be short; forwards nothing is carried over it.
   float* rec = (back ? recD : recS) + ((size_t)h * P.units + first) * (D * D) + el;
+  auto at = [&](int i) {
+    return reinterpret_cast<f32x4_t*>(rec + (int64_t)(back ? units - 1 - i : i) * (D * D));
+  };
+  const float f0 = back ? lam(len - (units - 1) * P.unit) : full;
+  auto carry = [](f32x4_t& x, float f, const f32x4_t& r) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(f, x[e], r[e]);
+  };
   const float* init = back ? dfinal : S0;
   f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
   if (init) {
     const float* m = init + ((int64_t)s * P.kv_heads + h) * (D * D);
     if (transposed && !back) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[r] = m[(el % D + r) * D + el / D];
+      for (int e = 0; e < 4; ++e) x[e] = m[(el % D + e) * D + el / D];
     } else {
       x = *reinterpret_cast<const f32x4_t*>(m + el);
     }
   }
-  // Unit u of the walk: stored in place of its record, then carried over it.  The
-  // first record of a group is loaded while the last group's are carried.
-  constexpr int G = 8;
-  auto at = [&](int i) { return rec + (int64_t)(back ? units - 1 - i : i) * (D * D); };
-  for (int i = 0; i < units; i += G) {
-    f32x4_t r[G];
+  for (int base = 0, flip = 0; base < units; base += W * R, flip ^= 1) {
+    const int here = min(W * R, units - base), each = (here + W - 1) / W;
+    const int i0 = base + w * each, n = max(0, min(each, base + here - i0));
+    f32x4_t r[R], sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < G; ++j)
-      if (i + j < units - 1) r[j] = *reinterpret_cast<const f32x4_t*>(at(i + j));
-#pragma unroll
-    for (int j = 0; j < G; ++j) {
-      if (i + j < units) *reinterpret_cast<f32x4_t*>(at(i + j)) = x;
-      if (i + j < units - 1) {
-        // only the sequence's last unit may be short; backwards it comes first
-        const float f = back && i + j == 0 ? lam(len - (units - 1) * P.unit) : full;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = fmaf(f, x[e], r[j][e]);
-      }
+    for (int j = 0; j < R; ++j) {
+      r[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+      if (j < n && i0 + j < units - 1) r[j] = *at(i0 + j);
     }
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (j < n) carry(sum, i0 + j == 0 ? f0 : full, r[j]);
+    sums[flip][w][lane] = sum;
+    __syncthreads();
+    // what enters the wave's quarter, and the next round
+    f32x4_t enter = x;
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+      if (v == w) enter = x;
+      const int begin = base + v * each, m = max(0, min(each, base + here - begin));
+      if (m > 0) carry(x, begin == 0 ? f0 * lam((m - 1) * P.unit) : lam(m * P.unit), sums[flip][v][lane]);
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (j < n) {
+        *at(i0 + j) = enter;
+        carry(enter, i0 + j == 0 ? f0 : full, r[j]);
+      }
   }
 }
 
@@ -158,19 +190,26 @@ scan_kernel(DecayPlan P, const float* log_decay, const int32_t* cu, const float*
 // states before the units of a single walk are kept in rec, and `dg` takes the parts
 // of the decay's gradient of the pairs whose earlier token lies before the tile,
 // with q the forward's queries in `other`.
-template <typename T, int D, bool Back>
-__global__ void __launch_bounds__((DC<T, D>::NT), 1)
+// Shared: several query heads to a key head.
+template <typename T, int D, bool Back, bool Shared>
+__global__ void __launch_bounds__((WalkSizes<T, D>::NT), (sizeof(T) == 2 && D == 32 ? 4 : 2))
 walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_decay, const float* S0,
             const int32_t* cu, float* rec, T* out, float* final_state, const T* other, double* dg) {
-  using C = DC<T, D>;
-  __shared__ __attribute__((aligned(16))) unsigned char ldsK[C::kTileBytes], ldsV[C::kTileBytes],
-      ldsS[C::NP * C::kPlane];
+  using C = WalkSizes<T, D>;
+  __shared__ __attribute__((aligned(512))) unsigned char ldsK[kTile * C::Wide::kPitch],
+      ldsV[kTile * C::Slim::kPitch], ldsS[C::NP * C::kPlane];
+  __shared__ __attribute__((aligned(16))) Powers pw;
   const int h = blockIdx.y, lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = lane & 15, g = lane >> 4, tw = w & 3, eh = w >> 2;
+  const int n = lane & 15, g = lane >> 4, tw = w;
+  // Halves of one unit eight workgroups apart: on one XCD, whose L2 has what they share.
+  constexpr int halves = D / C::VD;
+  const int unit = halves == 1 ? blockIdx.x : (blockIdx.x >> 4) * 8 + (blockIdx.x & 7);
+  const int e0 = halves == 1 ? 0 : ((blockIdx.x >> 3) & 1) * C::VD;
+  if (halves > 1 && unit >= P.grid_units) return;
   Span sp;
   double dsum = 0.0;
-  const bool found = find_span<C::NT>(P, cu, blockIdx.x, &sp);
+  const bool found = find_span<C::NT>(P, cu, unit, &sp);
   if (found) {
     const int64_t pair = (int64_t)sp.s * P.kv_heads + h;
     const float* init = S0 ? S0 + pair * (D * D) : nullptr;
@@ -178,123 +217,103 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
     float* keep = nullptr;  // records of a single walk
     if (P.single) {
       if (Back && rec)
-        keep = rec + ((size_t)h * P.units + (P.ragged ? sp.row0 / P.unit + sp.s
-                                                       : (int64_t)sp.s * P.units_per_seq)) * (D * D);
+        keep = rec + ((size_t)h * P.units + sp.slot) * (D * D);
     } else {
       init = rec + ((size_t)h * P.units + sp.slot) * (D * D);
       transposed = false;
       if (!S0 && sp.idx == 0) init = nullptr;
     }
-    State<T, C> S, add;
-    if (init) S.load(init, transposed, w, lane);
+    State<T, C> S;
+    if (init) S.load(init, transposed, e0, w, lane);
     else S.clear();
-    bool some = init != nullptr;  // the state is not all zeros
 
-    const int steps = (sp.end - sp.begin + kTile - 1) / kTile * P.group;
-    TileLoad<C> lk, lv;
-    OwnRows<T, C> own;
+    TileLoad<T, C, D> lk;
+    TileLoad<T, C, C::VD> lv;
+    OwnRows<T, C> qq;
+    OwnPieces<T, C> qo;  // of the forward's queries, for the decay's gradient
+    const int64_t krow0 = first_row(P, sp, P.kv_heads, h), qrow0 = first_row(P, sp, P.heads, h * P.group);
     auto fetch_kv = [&](int t) {
-      const int64_t row = row_of(P, sp, P.kv_heads, h, t) * D;
+      const int64_t row = (krow0 + t) * D;
       lk.load(k + row, sp.end - t);
-      lv.load(v + row, sp.end - t);
+      lv.load(v + row + e0, sp.end - t);
     };
     auto fetch_q = [&](int t, int gi) {
-      own.load(q + row_of(P, sp, P.heads, h * P.group + gi, t) * D, sp.end - t, 16 * tw + n, g);
+      const int64_t row = (qrow0 + (int64_t)gi * P.rows + t) * D;
+      qq.load(q + row, sp.end - t, 16 * tw + n, g);
+      if (Back) qo.load(other + row, dg ? sp.end - t : 0, 16 * tw + n, e0, g);
     };
-    if (steps > 0) {
+    if (sp.begin < sp.end) {
       fetch_kv(sp.begin);
       fetch_q(sp.begin, 0);
     }
     const Decay lam(log_decay[h]);
     const float full = lam(kTile);
-    // decays of the wave's scores: [earlier token 16 b + 4 g + i][own token 16 tw + n]
-    float score[4][4], weight[2][8];
     const float into = P.scale * lam(16 * tw + n + 1);
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) score[b][i] = P.scale * lam(max(0, 16 * (tw - b) + n - 4 * g - i));
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) weight[ks][j] = lam(kTile - 1 - (32 * ks + 8 * g + j));
+    Scores<true> scores;
+    scores.fill(lam, P.scale, n, g);
+    pw.fill(lam, P.scale);
 
-    for (int step = 0; step < steps; step += P.group) {
-      const int t0 = sp.begin + step / P.group * kTile;
+    // A step: one query head's tokens of a tile.  Its rows are read before the step and
+    // the next step's as soon as the products with them are under way, under no
+    // condition (past the end they load nothing): the compiler waits for as many loads
+    // as the path with the fewest has in flight, so that a branch around a prefetch
+    // makes every step wait for it.
+    for (int t0 = sp.begin, gi = 0; t0 < sp.end;) {
       const int live = min(kTile, sp.end - t0);
       const bool final = t0 + kTile >= sp.end;
-      if (Back && keep && (t0 - sp.begin) % P.unit == 0)
-        S.store(keep + (int64_t)((t0 - sp.begin) / P.unit) * (D * D), false, w, lane);
-      lk.store(ldsK);
-      lv.store(ldsV);
-      if (some) S.to_planes(ldsS, w, lane);
-      lds_barrier();
-      if (!final) fetch_kv(t0 + kTile);
-      for (int gi = 0; gi < P.group; ++gi) {
-        const OwnRows<T, C> qq = own;
-        if (gi + 1 < P.group) fetch_q(t0, gi + 1);
-        else if (!final) fetch_q(t0 + kTile, 0);
-        const int64_t row = row_of(P, sp, P.heads, h * P.group + gi, t0) * D;
-        f32x4_t acc[C::OB];
+      if (!Shared || gi == 0) {
+        if (Back && keep && ((t0 - sp.begin) & (P.unit - 1)) == 0)
+          S.store(keep + (int64_t)((t0 - sp.begin) / P.unit) * (D * D), e0, w, lane);
+        lk.store(ldsK);
+        lv.store(ldsV);
+        S.to_planes(ldsS, w, lane);
+        lds_barrier();
+        if (!Shared) fetch_kv(t0 + kTile);
+      }
+      const int64_t row = (qrow0 + (int64_t)gi * P.rows + t0) * D;
+      const bool wrap = !Shared || gi + 1 == P.group;
+      const int next_t = wrap ? t0 + kTile : t0, next_gi = wrap ? 0 : gi + 1;
+      {
+        // Scores of the tile's tokens (16 a block), then the state's part of the output,
+        // whose products run while the scores are decayed.
+        f32x4_t p[4], acc[C::OB];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) p[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+            Num<T>::mma(p[b], row_at<T, typename C::Wide>(ldsK, b, n, ks, g), qq.v[ks]);
 #pragma unroll
         for (int o = 0; o < C::OB; ++o) acc[o] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-        if (some) {
 #pragma unroll
-          for (int ks = 0; ks < C::KS; ++ks)
+        for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-            for (int x = C::NP - 1; x >= 0; --x)
-#pragma unroll
-              for (int o = 0; o < C::OB; ++o)
-                Num<T>::mma(acc[o], row_at<T, C>(ldsS + x * C::kPlane, 16 * (eh * C::OB + o) + n, ks, g),
-                            qq.v[ks]);
-#pragma unroll
-          for (int o = 0; o < C::OB; ++o)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[o][r] *= into;
-          if (Back && dg && 16 * tw + n < live) {
-            // sum_t ((t + 1) - (tokens of the unit from the tile on)) q_t dq_t
-            const T* o4 = other + row + (int64_t)(16 * tw + n) * D + 16 * eh * C::OB + 4 * g;
-            float dot = 0.0f;
+          for (int x = C::NP - 1; x >= 0; --x)
 #pragma unroll
             for (int o = 0; o < C::OB; ++o)
+              Num<T>::mma(acc[o], row_at<T, typename C::Wide>(ldsS + x * C::kPlane, o, n, ks, g), qq.v[ks]);
+        const OwnPieces<T, C> qo_now = qo;
+        fetch_q(next_t, next_gi);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float x = sizeof(T) == 2 ? __uint_as_float((uint32_t)o4[16 * o + r] << 16)
-                                               : (float)o4[16 * o + r];
-                dot = fmaf(x, acc[o][r], dot);
-              }
-            const int at = (t0 - sp.begin) % P.unit;
-            const int rest = min(P.unit, sp.end - (t0 - at)) - at;
-            dsum += (double)dot * (double)(16 * tw + n + 1 - rest);
-          }
-        }
-        // scores of the earlier tokens' blocks b <= tw, decayed, as operands
-        float p[4][4];
+        for (int b = 0; b < 4; ++b) scores.apply(p[b], tw - b, n, g);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (b <= tw) {
+        for (int o = 0; o < C::OB; ++o)
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks)
-              Num<T>::mma(x, row_at<T, C>(ldsK, 16 * b + n, ks, g), qq.v[ks]);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            p[b][i] = b < tw || (b == tw && 4 * g + i <= n) ? x[i] * score[b][i] : 0.0f;
+          for (int r = 0; r < 4; ++r) acc[o][r] *= into;
+        if (Back) {
+          // sum_t ((t + 1) - (tokens of the unit from the tile on)) q_t dq_t
+          const int at = ((t0 - sp.begin) & (P.unit - 1));
+          const int rest = min(P.unit, sp.end - (t0 - at)) - at;
+          dsum += (double)qo_now.dot(acc) * (double)(16 * tw + n + 1 - rest);
         }
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          if (2 * ks > tw) continue;
-          const float x[8] = {p[2 * ks][0],     p[2 * ks][1],     p[2 * ks][2],     p[2 * ks][3],
-                              p[2 * ks + 1][0], p[2 * ks + 1][1], p[2 * ks + 1][2], p[2 * ks + 1][3]};
-          Parts<T, 2> pp;
-          pp.set(x);
-#pragma unroll
-          for (int o = 0; o < C::OB; ++o)
-            pp.mma_right(acc[o], col_at<T, C, true>(ldsV, eh * C::OB + o, ks, lane));
-        }
+        for (int x = 0; x < 2; ++x)
+          add_scored<T, C, typename C::Slim, 2>(acc, p[2 * x], p[2 * x + 1], ldsV, x, 0, lane);
+        pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB>();
+        if (Shared && gi == 0) fetch_kv(t0 + kTile);
         const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + row, (uint32_t)(live * C::kRow));
-        const uint32_t at = (uint32_t)((16 * tw + n) * C::kRow + (16 * eh * C::OB + 4 * g) * C::ES);
+        const uint32_t at = (uint32_t)((16 * tw + n) * C::kRow + (e0 + 4 * g) * C::ES);
 #pragma unroll
         for (int o = 0; o < C::OB; ++o) {
           if constexpr (sizeof(T) == 2) {
@@ -306,26 +325,27 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
           }
         }
       }
+      if (Shared && ++gi < P.group) continue;
+      gi = 0;
       if (!final || (final_state && sp.last)) {
-        if (live < kTile)
-#pragma unroll
-          for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) weight[ks][j] = lam(max(0, live - 1 - (32 * ks + 8 * g + j)));
-        add.clear();
-        add.add_products(ldsK, ldsV, weight, w, lane);
-        S.advance(live == kTile ? full : lam(live), add);
-        some = true;
+        S.advance(live == kTile ? full : lam(live), ldsK, ldsV, pw.down + kTile - live, w, lane);
       }
       lds_barrier();
+      t0 += kTile;
     }
-    if (final_state && sp.last) S.store(final_state + pair * (D * D), false, w, lane);
+    if (final_state && sp.last) S.store(final_state + pair * (D * D), e0, w, lane);
   }
   if (Back && dg) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) dsum += __shfl_xor(dsum, o);
-    if (lane == 0) dg[((int64_t)h * P.grid_units + blockIdx.x) * 8 + w] = dsum;
+    if (lane == 0) dg[((int64_t)h * P.grid_units + unit) * 8 + e0 / C::VD * 4 + w] = dsum;
   }
+}
+
+template <typename T, int D>
+dim3 walk_grid(const DecayPlan& p) {
+  const bool whole = WalkSizes<T, D>::VD == D;
+  return dim3(whole ? p.grid_units : (p.grid_units + 7) / 8 * 16, p.kv_heads);
 }
 
 template <typename F>
@@ -349,16 +369,16 @@ gbla_status launch_decay_forward(const DecayPlan& p, const void* q, const void* 
   return by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    const dim3 grid(p.grid_units, p.kv_heads), block(DC<T, D>::NT);
+    const dim3 grid(p.grid_units, p.kv_heads);
     if (!p.single) {
-      hipLaunchKernelGGL((record_kernel<T, D>), grid, block, 0, st, p, (const T*)k, (const T*)v,
+      hipLaunchKernelGGL((record_kernel<T, D>), grid, dim3(RecordSizes<T, D>::NT), 0, st, p, (const T*)k, (const T*)v,
                          (const T*)nullptr, (const T*)nullptr, log_decay, cu, rec, (float*)nullptr);
-      hipLaunchKernelGGL((scan_kernel<D>), dim3(p.nseq, p.kv_heads, D * D / 1024), dim3(kThreads), 0,
+      hipLaunchKernelGGL((scan_kernel<D>), dim3(p.nseq * (D * D / 256), p.kv_heads), dim3(kThreads), 0,
                          st, p, log_decay, cu, S0, false, rec, (const float*)nullptr, (float*)nullptr);
     }
-    hipLaunchKernelGGL((walk_kernel<T, D, false>), grid, block, 0, st, p, (const T*)q, (const T*)k,
-                       (const T*)v, log_decay, S0, cu, rec, (T*)out, final_state, (const T*)nullptr,
-                       (double*)nullptr);
+    const auto walk = p.group > 1 ? walk_kernel<T, D, false, true> : walk_kernel<T, D, false, false>;
+    hipLaunchKernelGGL(walk, (walk_grid<T, D>(p)), dim3((WalkSizes<T, D>::NT)), 0, st, p, (const T*)q, (const T*)k, (const T*)v, log_decay,
+                       S0, cu, rec, (T*)out, final_state, (const T*)nullptr, (double*)nullptr);
   });
 }
 
@@ -374,17 +394,17 @@ gbla_status launch_decay_backward(const DecayPlan& p, const void* q, const void*
   const gbla_status done = by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    const dim3 grid(p.grid_units, p.kv_heads), block(DC<T, D>::NT);
+    const dim3 grid(p.grid_units, p.kv_heads);
     if (!p.single) {
-      hipLaunchKernelGGL((record_kernel<T, D>), dim3(p.grid_units, p.kv_heads, 2), block, 0, st, p,
+      hipLaunchKernelGGL((record_kernel<T, D>), dim3(p.grid_units, p.kv_heads, 2), dim3(RecordSizes<T, D>::NT), 0, st, p,
                          (const T*)v, (const T*)k, (const T*)q, (const T*)dout, log_decay, cu, recS,
                          recD);
-      hipLaunchKernelGGL((scan_kernel<D>), dim3(p.nseq, p.kv_heads, 2 * (D * D / 1024)),
+      hipLaunchKernelGGL((scan_kernel<D>), dim3(p.nseq * (2 * D * D / 256), p.kv_heads),
                          dim3(kThreads), 0, st, p, log_decay, cu, S0, true, recS, dfinal, recD);
     }
-    hipLaunchKernelGGL((walk_kernel<T, D, true>), grid, block, 0, st, p, (const T*)dout,
-                       (const T*)v, (const T*)k, log_decay, S0, cu,
-                       p.single && !dg ? (float*)nullptr : recS, (T*)dq, (float*)nullptr, (const T*)q, dg);
+    const auto walk = p.group > 1 ? walk_kernel<T, D, true, true> : walk_kernel<T, D, true, false>;
+    hipLaunchKernelGGL(walk, (walk_grid<T, D>(p)), dim3((WalkSizes<T, D>::NT)), 0, st, p, (const T*)dout, (const T*)v, (const T*)k,
+                       log_decay, S0, cu, p.single && !dg ? (float*)nullptr : recS, (T*)dq, (float*)nullptr, (const T*)q, dg);
   });
   if (done != GBLA_OK) return done;
   return launch_decay_keys(p, q, k, v, log_decay, S0, cu, dout, dfinal, ws, dk, dv, dlog_decay, dS0,

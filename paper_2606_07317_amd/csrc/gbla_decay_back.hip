@@ -30,13 +30,18 @@ namespace gbla {
 namespace {
 
 template <typename T, int D>
-__global__ void __launch_bounds__((DC<T, D>::NT), 1)
+using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, 2, false>;
+
+// Shared: several query heads to a key head.
+template <typename T, int D, bool Shared>
+__global__ void __launch_bounds__((KeysSizes<T, D>::NT), 2)
 keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_decay,
             const float* S0, const int32_t* cu, const T* dout, const float* dfinal,
             const float* recS, const float* recD, T* dk, T* dv, float* dS0, double* dg) {
-  using C = DC<T, D>;
-  __shared__ __attribute__((aligned(16))) unsigned char ldsQ[C::kTileBytes], ldsO[C::kTileBytes],
-      ldsD[C::NP * C::kPlane];
+  using C = KeysSizes<T, D>;
+  __shared__ __attribute__((aligned(512))) unsigned char ldsQ[kTile * C::Wide::kPitch],
+      ldsO[kTile * C::Wide::kPitch], ldsD[C::NP * C::kPlane];
+  __shared__ __attribute__((aligned(16))) Powers pw;
   const int h = blockIdx.y, lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4, tw = w & 3, eh = w >> 2;
@@ -49,135 +54,130 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
     const float* kept;  // the states before its units, [column of S][row] as dq's walk has them
     if (P.single) {
       init = dfinal ? dfinal + pair * (D * D) : nullptr;
-      kept = recS + ((size_t)h * P.units + (P.ragged ? sp.row0 / P.unit + sp.s
-                                                     : (int64_t)sp.s * P.units_per_seq)) * (D * D);
+      kept = recS + ((size_t)h * P.units + sp.slot) * (D * D);
     } else {
       const size_t at = ((size_t)h * P.units + sp.slot) * (D * D);
       init = dfinal || !sp.last ? recD + at : nullptr;
       kept = recS + at;
     }
-    State<T, C> S, add;
-    if (init) S.load(init, false, w, lane);
+    State<T, C> S;
+    if (init) S.load(init, false, 0, w, lane);
     else S.clear();
-    bool some = init != nullptr;
 
     const int tiles = (sp.end - sp.begin + kTile - 1) / kTile;
-    TileLoad<C> lq, lo;
+    TileLoad<T, C, D> lq, lo;
     OwnRows<T, C> kf, vf;
+    OwnPieces<T, C> kp;
+    const int64_t krow0 = first_row(P, sp, P.kv_heads, h), qrow0 = first_row(P, sp, P.heads, h * P.group);
     auto fetch = [&](int t, int gi) {
-      const int64_t row = row_of(P, sp, P.heads, h * P.group + gi, t) * D;
-      lq.load(q + row, sp.end - t);
-      lo.load(dout + row, sp.end - t);
+      const int64_t row = (qrow0 + (int64_t)gi * P.rows + t) * D;
+      const int live = t < sp.begin ? 0 : sp.end - t;
+      lq.load(q + row, live);
+      lo.load(dout + row, live);
     };
-    if (tiles > 0) fetch(sp.begin + (tiles - 1) * kTile, 0);
+    auto fetch_own = [&](int t) {  // none before the unit
+      const int64_t row = (krow0 + t) * D;
+      const int live = t < sp.begin ? 0 : sp.end - t;
+      kf.load(k + row, live, 16 * tw + n, g);
+      vf.load(v + row, live, 16 * tw + n, g);
+      kp.load(k + row, dg ? live : 0, 16 * tw + n, 16 * eh * C::OB, g);
+    };
+    if (tiles > 0) {
+      fetch(sp.begin + (tiles - 1) * kTile, 0);
+      fetch_own(sp.begin + (tiles - 1) * kTile);
+    }
     const Decay lam(log_decay[h]);
     const float full = lam(kTile);
-    float score[4][4], weight[2][8];
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) score[b][i] = P.scale * lam(max(0, 16 * (b - tw) + 4 * g + i - n));
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) weight[ks][j] = P.scale * lam(32 * ks + 8 * g + j + 1);
+    Scores<false> scores;
+    scores.fill(lam, P.scale, n, g);
+    pw.fill(lam, P.scale);
 
     for (int tile = tiles - 1; tile >= 0; --tile) {
       const int t0 = sp.begin + tile * kTile, live = min(kTile, sp.end - t0);
-      const int64_t krow = row_of(P, sp, P.kv_heads, h, t0) * D;
-      kf.load(k + krow, live, 16 * tw + n, g);
-      vf.load(v + krow, live, 16 * tw + n, g);
+      const int64_t krow = (krow0 + t0) * D;
       f32x4_t ak[C::OB], av[C::OB];
 #pragma unroll
       for (int o = 0; o < C::OB; ++o) ak[o] = av[o] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
       float inner = 0.0f;
-      add.clear();
-      for (int gi = 0; gi < P.group; ++gi) {
+      for (int gi = 0; gi < (Shared ? P.group : 1); ++gi) {
         lq.store(ldsQ);
         lo.store(ldsO);
-        if (gi == 0 && some) S.to_planes(ldsD, w, lane);
+        if (gi == 0) S.to_planes(ldsD, w, lane);
         lds_barrier();
-        if (gi + 1 < P.group) fetch(t0, gi + 1);
-        else if (tile > 0) fetch(t0 - kTile, 0);
-        if (gi == 0 && some) {
-          // D^T k by rows of the planes [column][row], D v by their columns
+        const bool wrap = !Shared || gi + 1 == P.group;
+        fetch(wrap ? t0 - kTile : t0, wrap ? 0 : gi + 1);
+        // The values' gradient, then the keys': scores of the tile's tokens (16 a block),
+        // the part of D, whose products run while the scores are decayed, the products of
+        // the scores.  One after the other, since both at once do not fit the registers.
+        const bool first = !Shared || gi == 0;
+        const float out = first ? lam(max(0, live - 1 - 16 * tw - n)) : 1.0f;
+        f32x4_t x[4], y[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) x[b] = y[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) Num<T>::mma(x[b], row_at<T, typename C::Wide>(ldsQ, b, n, ks, g), kf.v[ks]);
+        if (first) {  // D^T k by rows of the planes [column][row]
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-            for (int x = C::NP - 1; x >= 0; --x)
+            for (int p = C::NP - 1; p >= 0; --p)
 #pragma unroll
-              for (int o = 0; o < C::OB; ++o) {
-                const int blk = eh * C::OB + o;
-                Num<T>::mma(av[o], row_at<T, C>(ldsD + x * C::kPlane, 16 * blk + n, ks, g), kf.v[ks]);
-                Num<T>::mma(ak[o], col_at<T, C, false>(ldsD + x * C::kPlane, blk, ks, lane), vf.v[ks]);
-              }
-          const float out = lam(max(0, live - 1 - 16 * tw - n));
-#pragma unroll
-          for (int o = 0; o < C::OB; ++o)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              ak[o][r] *= out;
-              av[o][r] *= out;
-            }
-          if (dg && 16 * tw + n < live) {
-            const T* k4 = k + krow + (int64_t)(16 * tw + n) * D + 16 * eh * C::OB + 4 * g;
-            float dot = 0.0f;
-#pragma unroll
-            for (int o = 0; o < C::OB; ++o)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float x = sizeof(T) == 2 ? __uint_as_float((uint32_t)k4[16 * o + r] << 16)
-                                               : (float)k4[16 * o + r];
-                dot = fmaf(x, ak[o][r], dot);
-              }
-            // tokens of the unit after token s
-            const int at = (t0 - sp.begin) % P.unit;
-            const int size = min(P.unit, sp.end - (t0 - at));
-            dsum += (double)dot * (double)(size - 1 - at - 16 * tw - n);
-          }
+              for (int o = 0; o < C::OB; ++o)
+                Num<T>::mma(av[o], row_at<T, typename C::Wide>(ldsD + p * C::kPlane, eh * C::OB + o, n, ks, g), kf.v[ks]);
         }
-        float px[4][4], py[4][4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) scores.apply(x[b], b - tw, n, g);
+#pragma unroll
+        for (int o = 0; o < C::OB; ++o)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) av[o][r] *= out;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          add_scored<T, C, typename C::Wide, 2>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, lane);
+        if (!Shared) pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB>();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) Num<T>::mma(y[b], row_at<T, typename C::Wide>(ldsO, b, n, ks, g), vf.v[ks]);
+        if (first) {  // D v by their columns
+#pragma unroll
+          for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+            for (int p = C::NP - 1; p >= 0; --p)
+#pragma unroll
+              for (int o = 0; o < C::OB; ++o)
+                Num<T>::mma(ak[o], col_at<T, typename C::Wide, false>(ldsD + p * C::kPlane, eh * C::OB + o, ks, lane), vf.v[ks]);
+        }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f}, y = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (b >= tw) {
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) {
-              Num<T>::mma(x, row_at<T, C>(ldsQ, 16 * b + n, ks, g), kf.v[ks]);
-              Num<T>::mma(y, row_at<T, C>(ldsO, 16 * b + n, ks, g), vf.v[ks]);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool in = b > tw || (b == tw && 4 * g + i >= n);
-            px[b][i] = in ? x[i] * score[b][i] : 0.0f;
-            py[b][i] = in ? y[i] * score[b][i] : 0.0f;
-            if (dg && in && eh == 0)
-              inner = fmaf(px[b][i] * y[i], (float)(16 * (b - tw) + 4 * g + i - n), inner);
-          }
+          for (int i = 0; i < 4; ++i)  // x is 0 where the order is wrong
+            inner = fmaf(x[b][i] * y[b][i], (float)(16 * (b - tw) + 4 * g + i - n), inner);
+          scores.apply(y[b], b - tw, n, g);
         }
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          if (2 * ks + 1 < tw) continue;
-          const float x[8] = {px[2 * ks][0],     px[2 * ks][1],     px[2 * ks][2],     px[2 * ks][3],
-                              px[2 * ks + 1][0], px[2 * ks + 1][1], px[2 * ks + 1][2], px[2 * ks + 1][3]};
-          const float y[8] = {py[2 * ks][0],     py[2 * ks][1],     py[2 * ks][2],     py[2 * ks][3],
-                              py[2 * ks + 1][0], py[2 * ks + 1][1], py[2 * ks + 1][2], py[2 * ks + 1][3]};
-          Parts<T, 2> xx, yy;
-          xx.set(x);
-          yy.set(y);
+        for (int o = 0; o < C::OB; ++o)
 #pragma unroll
-          for (int o = 0; o < C::OB; ++o) {
-            xx.mma_right(av[o], col_at<T, C, true>(ldsO, eh * C::OB + o, ks, lane));
-            yy.mma_right(ak[o], col_at<T, C, true>(ldsQ, eh * C::OB + o, ks, lane));
-          }
+          for (int r = 0; r < 4; ++r) ak[o][r] *= out;
+        {
+          // tokens of the unit after token s
+          const int at = (t0 - sp.begin) & (P.unit - 1), size = min(P.unit, sp.end - (t0 - at));
+          const float dot = first ? kp.dot(ak) : 0.0f;
+          dsum += (double)dot * (double)(size - 1 - at - 16 * tw - n);
         }
-        add.add_products(ldsQ, ldsO, weight, w, lane);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          add_scored<T, C, typename C::Wide, 2>(ak, y[2 * p], y[2 * p + 1], ldsQ, p, eh * C::OB, lane);
+        if (!Shared) pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB, 4>();
+        __builtin_amdgcn_sched_barrier(0);
+        if (wrap) fetch_own(t0 - kTile);
+        S.advance(gi > 0 ? 1.0f : live == kTile ? full : lam(live), ldsQ, ldsO, pw.up, w, lane);
         lds_barrier();
       }
-      S.advance(live == kTile ? full : lam(live), add);
-      some = true;
-      dsum += (double)inner;
+      if (eh == 0) dsum += (double)inner;
       const __amdgpu_buffer_rsrc_t rk = make_rsrc(dk + krow, (uint32_t)(live * C::kRow));
       const __amdgpu_buffer_rsrc_t rv = make_rsrc(dv + krow, (uint32_t)(live * C::kRow));
       const uint32_t at = (uint32_t)((16 * tw + n) * C::kRow + (16 * eh * C::OB + 4 * g) * C::ES);
@@ -193,21 +193,22 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, av[o]), rv, at + 16 * o * C::ES, 0, 0);
         }
       }
-      if (dg && (t0 - sp.begin) % P.unit == 0) {  // the unit's first tile: <S_in, D_in>
+      if (dg && ((t0 - sp.begin) & (P.unit - 1)) == 0) {  // the unit's first tile: <S_in, D_in>
         const int unit = (t0 - sp.begin) / P.unit;
         const int size = min(P.unit, sp.end - t0);
         if (S0 || sp.idx + unit > 0) {
-          add.load(kept + (int64_t)unit * (D * D), true, w, lane);
+          State<T, C> in;
+          in.load(kept + (int64_t)unit * (D * D), true, 0, w, lane);
           float dot = 0.0f;
 #pragma unroll
-          for (int i = 0; i < C::SB; ++i)
+          for (int i = 0; i < C::SR; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dot = fmaf(add.s[i][r], S.s[i][r], dot);
+            for (int r = 0; r < 4; ++r) dot = fmaf(in.s[i][r], S.s[i][r], dot);
           dsum += (double)dot * (double)size;
         }
       }
     }
-    if (dS0 && sp.begin == 0) S.store(dS0 + pair * (D * D), false, w, lane);
+    if (dS0 && sp.begin == 0) S.store(dS0 + pair * (D * D), 0, w, lane);
   }
   if (dg) {
 #pragma unroll
@@ -242,13 +243,14 @@ void launch_keys(const DecayPlan& p, const void* q, const void* k, const void* v
                  unsigned char* ws, void* dk, void* dv, float* dlog_decay, float* dS0, hipStream_t st) {
   double* dg = dlog_decay ? reinterpret_cast<double*>(ws + p.off_dg) : nullptr;
   double* mine = dg ? dg + (int64_t)p.kv_heads * p.grid_units * 8 : nullptr;
-  hipLaunchKernelGGL((keys_kernel<T, D>), dim3(p.grid_units, p.kv_heads), dim3(DC<T, D>::NT), 0, st, p,
+  const auto keys = p.group > 1 ? keys_kernel<T, D, true> : keys_kernel<T, D, false>;
+  hipLaunchKernelGGL(keys, dim3(p.grid_units, p.kv_heads), dim3((KeysSizes<T, D>::NT)), 0, st, p,
                      (const T*)q, (const T*)k, (const T*)v, log_decay, S0, cu, (const T*)dout, dfinal,
                      reinterpret_cast<const float*>(ws + p.off_S),
                      reinterpret_cast<const float*>(ws + p.off_D), (T*)dk, (T*)dv, dS0, mine);
   if (dg)
     hipLaunchKernelGGL(decay_sum_kernel, dim3(p.kv_heads), dim3(kThreads), 0, st, p.kv_heads,
-                       p.grid_units, DC<T, D>::NW, dg, dlog_decay);
+                       p.grid_units, (KeysSizes<T, D>::NW), dg, dlog_decay);
 }
 
 }  // namespace

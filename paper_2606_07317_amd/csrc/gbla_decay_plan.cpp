@@ -15,21 +15,43 @@ constexpr int kMaxGridY = 65535;
 bool head_dim_ok(int32_t d) { return d == 32 || d == 64 || d == 128; }
 bool dtype_ok(int32_t t) { return t == GBLA_F32 || t == GBLA_BF16; }
 
-// Tokens of a unit: short enough for about `want` workgroups, long enough that
-// the d x d record of a unit stays small beside its tokens.
+// Tokens of a unit (a power of two): short enough for two workgroups a CU, long enough
+// that the d x d record of a unit stays small beside its tokens.  Whole calls in us,
+// units of 256 / 512 / 1024: forward bf16 B = 1, n = 32768, H = 8, d = 64 63 / 53 / 58;
+// packed, 64 sequences, T = 177,929, d = 128, H = 8, K = 2 410 / 404 / -; backward B = 8, n =
+// 2048, H = 16, d = 64 158 / 141 / 139; 16 sequences, T = 57,511, H = 8, d = 128 793 / 691 / -.
 int32_t unit_tokens(const DecayPlan& p) {
-  const int64_t want = p.d == 128 ? 512 : 1024;
   int32_t unit = kMaxUnit;
-  while (unit > 2 * kTile && p.tokens * p.kv_heads < (int64_t)unit * want) unit /= 2;
+  while (unit > 2 * kTile && p.tokens * p.kv_heads < (int64_t)unit * 512) unit /= 2;
   return unit;
 }
 
-// Whether a workgroup walks a whole sequence: where no sequence is longer than a
-// few units, or the (sequence, key head) pairs alone fill the chip.
-bool walk_whole(const DecayPlan& p, int64_t longest) {
-  if (longest <= 4 * kTile || longest <= p.unit) return true;
-  const int64_t pairs = p.d == 128 ? 256 : 512;
-  return longest * pairs <= p.tokens * p.kv_heads;
+// Whether a workgroup walks a whole sequence.  One launch instead of three (three of
+// five): its time is a + b longest while there are few (sequence, key head) pairs, that of
+// the split a' + b' pairs longest, so the single walk wins where
+//   longest (full - tokens of all pairs / longest) <= few,
+// `full` pairs filling the chip at any length and few / full tokens passing for short
+// whatever the pairs.  Single / split in us:
+//   forward bf16 d = 64: B K = 8 n = 257 11 / 13, 384 14 / 13, 1024 32 / 14; 32 n = 384 14 / 14;
+//   128 n = 768 26 / 29, 1024 34 / 33; 256 n = 4096 149 / 201.  d = 32: 8 n = 512 10 / 11, 768
+//   14 / 11; 128 n = 1024 19 / 19.  d = 128: 8 n = 257 17 / 19, 384 20 / 19; 32 n = 512 26 / 26;
+//   128 n = 2048 102 / 128.
+//   forward fp32 d = 32: 8 n = 257 13 / 14; 128 n = 512 20 / 20.  d = 64: 8 n = 192 17 / 20, 257
+//   26 / 20; 128 n = 384 34 / 36, 512 44 / 41.  d = 128: 8 n = 192 26 / 33, 257 43 / 35; 128 n =
+//   2048 275 / 373.
+//   backward bf16 d = 64: 8 n = 192 27 / 26; 128 n = 384 49 / 49; 256 n = 4096 463 / 544.  d = 32:
+//   8 n = 257 22 / 21; 128 n = 512 32 / 31.  d = 128: 32 n = 192 48 / 48; 128 n = 1024 207 / 207.
+//   backward fp32 d = 32: 8 n = 192 27 / 27; 128 n = 257 42 / 42.  d = 64: 8 n = 192 51 / 45; 128
+//   n = 257 84 / 85; 256 n = 2048 515 / 564.  d = 128: 8 n = 192 134 / 105; 128 n = 384 282 / 292.
+bool walk_whole(const DecayPlan& p, int64_t longest, bool backward) {
+  struct Rule {
+    int32_t full, few;
+  };
+  static constexpr Rule rules[2][2][3] = {  // forward, backward; bf16, fp32; d = 32, 64, 128
+      {{{272, 148000}, {192, 61000}, {72, 20000}}, {{262, 68000}, {233, 47000}, {128, 27000}}},
+      {{{226, 48000}, {245, 45000}, {150, 22500}}, {{256, 47000}, {256, 40000}, {190, 27000}}}};
+  const Rule r = rules[backward][p.dtype == GBLA_F32][p.d == 32 ? 0 : p.d == 64 ? 1 : 2];
+  return longest * r.full - p.tokens * p.kv_heads <= r.few;
 }
 
 }  // namespace
@@ -57,7 +79,8 @@ gbla_status make_decay_plan(const gbla_decay_shape* s, bool ragged, bool backwar
   q.unit = unit_tokens(q);
   // sum over the sequences of max(1, ceil(len / unit)) <= tokens / unit + N
   const int64_t cap = q.tokens / q.unit + q.nseq;
-  if (cap > kMaxGridX) return GBLA_ERR_UNSUPPORTED;
+  // grids: units, and the slices of 256 elements of every sequence's state
+  if (cap > kMaxGridX / 2 || (int64_t)q.nseq * (q.d * q.d / 128) > kMaxGridX) return GBLA_ERR_UNSUPPORTED;
   if (ragged) {
     q.units = (int32_t)cap;
   } else {
@@ -66,7 +89,7 @@ gbla_status make_decay_plan(const gbla_decay_shape* s, bool ragged, bool backwar
     q.units_per_seq = (int32_t)each;
     q.units = (int32_t)(each * q.nseq);
   }
-  q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows) ? 1 : 0;
+  q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows, backward) ? 1 : 0;
   q.grid_units = q.single ? q.nseq : q.units;
   const size_t states = (size_t)cap * q.kv_heads * q.d * q.d * sizeof(float);
   size_t off = 0;

@@ -15,8 +15,14 @@
 // sum of one to three bf16 parts (8 significant bits each).  fp32 operands use
 // v_mfma_f32_16x16x4_f32, eight to a K step.
 //
-// Tiles in LDS: [token][D], rows D elements and 16 bytes apart, so that sixteen rows
-// of a 16-byte column start on sixteen different groups of four banks.
+// Tiles in LDS: [token][D].  Two kinds of reads meet there: 16 rows of one 16-byte unit
+// (row_at) and columns (col_at; bf16 by transposed reads of four rows and two units a
+// group of 16 lanes).  The walk's bf16 rows store unit u at u ^ swizzle(r), so that the
+// rows that either reads at once fall on different banks (with rows 16 bytes apart, half
+// of its LDS cycles at d = 128 were conflicts: 239 us, 191 with the swizzle).  The other
+// kernels' rows are 16 bytes apart, since the swizzle's addresses cost registers that
+// they do not have (keys at d = 128 348 us, 466 with it; records 117, 141: one workgroup
+// a CU instead of two), and fp32 rows, whose reads of single values that suits.
 #pragma once
 
 #include <math.h>
@@ -91,29 +97,47 @@ struct Parts {
   }
 };
 
-template <typename T, int DIM>
+// A tile or plane in LDS: rows of W elements, swizzled or 16 bytes apart.
+template <typename T, int W, bool Swizzled>
+struct Lay {
+  static constexpr int ES = (int)sizeof(T);
+  static constexpr int kRow = W * ES;
+  static constexpr bool kSwizzled = Swizzled && ES == 2;
+  static constexpr int kPitch = kRow + (kSwizzled ? 0 : 16);
+  // Rows 0-3 and 4-7, 8-11 and 12-15, 0-3 and 8-11, 4-7 and 12-15 (what a transposed
+  // read takes at once, in either order) get different pairs of units, all sixteen rows
+  // different units; as far as a row has them (W / 8 units).
+  static constexpr int kShift = W == 128 ? 0 : W == 64 ? 1 : 2;
+  static __device__ __forceinline__ int swizzle(int r) {
+    if constexpr (!kSwizzled) return 0;
+    return ((((r ^ ((r >> 1) & 4)) & 7) >> kShift) << 1) | ((r >> 3) & 1);
+  }
+  // Byte offset of the 16-byte unit u of row r.
+  static __device__ __forceinline__ int unit_at(int r, int u) { return r * kPitch + ((u ^ swizzle(r)) << 4); }
+};
+
+// Sizes of a kernel of D channels: a workgroup of NWAVES waves with VD of the value
+// channels, the state in PARTS bf16 parts for its products.
+template <typename T, int DIM, int VDIM, int NWAVES, int PARTS, bool SWIZZLED>
 struct DC {
   static constexpr int D = DIM;
-  static constexpr int EH = D == 128 ? 2 : 1;  // groups of four waves, by the output's channels
-  static constexpr int NW = 4 * EH;
+  static constexpr int VD = VDIM;
+  static constexpr int NW = NWAVES;
+  static constexpr int EH = NW / 4;            // groups of four waves, by the output's channels
   static constexpr int NT = 64 * NW;
   static constexpr int ES = (int)sizeof(T);
   static constexpr int kRow = D * ES;          // bytes of a row in memory
-  static constexpr int kPitch = kRow + 16;     // and in LDS
-  static constexpr int kTileBytes = kTile * kPitch;
   static constexpr int KS = D / 32;            // K steps over channels
-  static constexpr int NB = D / 16;            // 16-channel blocks
-  static constexpr int OB = NB / EH;           // of a wave's output
-  static constexpr int SB = NB * NB / NW;      // state blocks of a wave: one column block,
-                                               // SB row blocks
-  static constexpr int CH = kTile * kRow / 16 / NT;  // 16-byte pieces of a thread per tile
-  // Planes of the state in LDS, [column][row]: two parts leave 2^-18 of a value,
-  // far below the bf16 rounding of the results that they form.
-  static constexpr int NP = ES == 2 ? 2 : 1;
-  static constexpr int kPlane = D * kPitch;
-  // A wave's state blocks: columns 16 cb .., rows 16 (rb + i) .., i < SB.
-  static __device__ __forceinline__ int col_block(int w) { return D == 32 ? (w & 1) : w; }
-  static __device__ __forceinline__ int row_block(int w) { return D == 32 ? (w >> 1) : 0; }
+  static constexpr int OB = VD / 16 / EH;      // 16-channel blocks of a wave's output
+  // A wave's state blocks: one column block, SR row blocks.
+  static constexpr int NBK = D / 16, NBV = VD / 16;
+  static constexpr int SR = NBK * NBV / NW;
+  using Wide = Lay<T, D, SWIZZLED>;                      // tiles of all channels, planes [column][row]
+  using Slim = Lay<T, VD, SWIZZLED>;                     // tiles of the value channels
+  static constexpr int NP = ES == 2 ? PARTS : 1;
+  static constexpr int kPlane = VD * Wide::kPitch;
+  static __device__ __forceinline__ int col_block(int w) { return w % NBV; }
+  static __device__ __forceinline__ int row_block(int w) { return w / NBV * SR; }
 };
 
 // exp(n g) for whole n >= 0: the product n g log2(e) in two parts, so that its
@@ -138,24 +162,28 @@ struct Decay {
 // the next tile's).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// A tile of a thread's 16-byte pieces on its way from memory to LDS; rows from
-// `live` on are zeros.
-template <typename C>
+// W channels of a tile, 16-byte pieces of a thread on their way from memory (rows of
+// C::kRow bytes) to LDS; rows from `live` on are zeros.
+template <typename T, typename C, int W>
 struct TileLoad {
-  u32x4_t x[C::CH];
-  __device__ __forceinline__ void load(const void* row0, int live) {
+  using L = Lay<T, W, C::Wide::kSwizzled>;
+  static constexpr int per = L::kRow / 16, N = kTile * per / C::NT;
+  u32x4_t x[N];
+  __device__ __forceinline__ void load(const void* first, int live) {
     const int rows = live < 0 ? 0 : live > kTile ? kTile : live;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(row0, (uint32_t)(rows * C::kRow));
+    const __amdgpu_buffer_rsrc_t r =
+        make_rsrc(first, rows > 0 ? (uint32_t)((rows - 1) * C::kRow + L::kRow) : 0u);
 #pragma unroll
-    for (int i = 0; i < C::CH; ++i)
-      x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (uint32_t)(i * C::NT + threadIdx.x) * 16u, 0, 0);
+    for (int i = 0; i < N; ++i) {
+      const int at = i * C::NT + threadIdx.x;
+      x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (uint32_t)((at / per) * C::kRow + (at % per) * 16), 0, 0);
+    }
   }
   __device__ __forceinline__ void store(unsigned char* lds) const {
-    constexpr int per = C::kRow / 16;
 #pragma unroll
-    for (int i = 0; i < C::CH; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int at = i * C::NT + threadIdx.x;
-      *reinterpret_cast<u32x4_t*>(lds + (at / per) * C::kPitch + (at % per) * 16) = x[i];
+      *reinterpret_cast<u32x4_t*>(lds + L::unit_at(at / per, at % per)) = x[i];
     }
   }
 };
@@ -181,110 +209,267 @@ struct OwnRows {
   }
 };
 
-// Row `row` of a tile in LDS, channels 32 ks + 8 g + j.
+// The channels of a wave's own rows that its results have: c0 + 16 o + 4 g + r of lane
+// n's row.
 template <typename T, typename C>
-__device__ __forceinline__ typename Num<T>::V8 row_at(const unsigned char* lds, int row, int ks, int g) {
-  const unsigned char* p = lds + row * C::kPitch + (32 * ks + 8 * g) * C::ES;
-  if constexpr (sizeof(T) == 2) return *reinterpret_cast<const u32x4_t*>(p);
-  else return {*reinterpret_cast<const f32x4_t*>(p), *reinterpret_cast<const f32x4_t*>(p + 16)};
-}
-
-// Column 16 cb + n of a tile in LDS, rows 32 ks + .. in split or natural order.
-template <typename T, typename C, bool Split>
-__device__ __forceinline__ typename Num<T>::V8 col_at(const unsigned char* lds, int cb, int ks, int lane) {
-  const int n = lane & 15, g = lane >> 4;
-  const int r0 = 32 * ks + (Split ? 4 : 8) * g, r1 = r0 + (Split ? 16 : 4);
-  if constexpr (sizeof(T) == 2) {
-    const unsigned char* p = lds + (r0 + (n >> 2)) * C::kPitch + (16 * cb + 4 * (n & 3)) * 2;
-    const u32x2_t u = tr_read16(p), w = tr_read16(p + (r1 - r0) * C::kPitch);
-    return (u32x4_t){u[0], u[1], w[0], w[1]};
-  } else {
-    const float* p = reinterpret_cast<const float*>(lds + r0 * C::kPitch) + 16 * cb + n;
-    const float* q = reinterpret_cast<const float*>(lds + r1 * C::kPitch) + 16 * cb + n;
-    constexpr int P = C::kPitch / 4;
-    return {{p[0], p[P], p[2 * P], p[3 * P]}, {q[0], q[P], q[2 * P], q[3 * P]}};
-  }
-}
-
-// A wave's blocks of a state X[row][column] in fp32.
-template <typename T, typename C>
-struct State {
-  f32x4_t s[C::SB];  // block i: rows 16 (rb + i) + 4 g + r, column 16 cb + n
-
-  __device__ __forceinline__ void clear() {
+struct OwnPieces {
+  u32x4_t v[C::OB];
+  __device__ __forceinline__ void load(const void* row0, int live, int row, int c0, int g) {
+    const int rows = live < 0 ? 0 : live > kTile ? kTile : live;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(row0, (uint32_t)(rows * C::kRow));
+    const uint32_t at = (uint32_t)(row * C::kRow + (c0 + 4 * g) * C::ES);
 #pragma unroll
-    for (int i = 0; i < C::SB; ++i) s[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  // from / to memory [row][column] (or [column][row])
-  __device__ __forceinline__ void load(const float* m, bool transposed, int w, int lane) {
-    const int col = 16 * C::col_block(w) + (lane & 15), row = 16 * C::row_block(w) + 4 * (lane >> 4);
-    if (transposed) {
-#pragma unroll
-      for (int i = 0; i < C::SB; ++i)
-        s[i] = *reinterpret_cast<const f32x4_t*>(m + (int64_t)col * C::D + row + 16 * i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::SB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[i][r] = m[(row + 16 * i + r) * C::D + col];
-    }
-  }
-  __device__ __forceinline__ void store(float* m, bool transposed, int w, int lane) const {
-    const int col = 16 * C::col_block(w) + (lane & 15), row = 16 * C::row_block(w) + 4 * (lane >> 4);
-    if (transposed) {
-#pragma unroll
-      for (int i = 0; i < C::SB; ++i)
-        *reinterpret_cast<f32x4_t*>(m + (int64_t)col * C::D + row + 16 * i) = s[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::SB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) m[(row + 16 * i + r) * C::D + col] = s[i][r];
-    }
-  }
-  // into the planes [column][row]
-  __device__ __forceinline__ void to_planes(unsigned char* planes, int w, int lane) const {
-    const int col = 16 * C::col_block(w) + (lane & 15), row = 16 * C::row_block(w) + 4 * (lane >> 4);
-    unsigned char* p = planes + col * C::kPitch + row * C::ES;
-#pragma unroll
-    for (int i = 0; i < C::SB; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<f32x4_t*>(p + 16 * i * C::ES) = s[i];
+    for (int o = 0; o < C::OB; ++o) {
+      if constexpr (sizeof(T) == 2) {
+        const u32x2_t x = __builtin_amdgcn_raw_buffer_load_b64(r, at + 16 * o * C::ES, 0, 0);
+        v[o][0] = x[0];
+        v[o][1] = x[1];
       } else {
-        const uint32_t h0 = pack_bf16x2(s[i][0], s[i][1]), h1 = pack_bf16x2(s[i][2], s[i][3]);
-        *reinterpret_cast<u32x2_t*>(p + 16 * i * C::ES) = (u32x2_t){h0, h1};
-        *reinterpret_cast<u32x2_t*>(p + 16 * i * C::ES + C::kPlane) =
-            (u32x2_t){pack_bf16x2(s[i][0] - bf16_lo(h0), s[i][1] - bf16_hi(h0)),
-                      pack_bf16x2(s[i][2] - bf16_lo(h1), s[i][3] - bf16_hi(h1))};
+        v[o] = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * o * C::ES, 0, 0);
       }
     }
   }
-  // s = f s + x
-  __device__ __forceinline__ void advance(float f, const State& x) {
+  // sum over them of their products with a result
+  __device__ __forceinline__ float dot(const f32x4_t* acc) const {
+    float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < C::SB; ++i)
+    for (int o = 0; o < C::OB; ++o)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[i][r] = fmaf(f, s[i][r], x.s[i][r]);
+      for (int r = 0; r < 4; ++r) {
+        const float x = sizeof(T) == 4 ? __uint_as_float(v[o][r]) : r & 1 ? bf16_hi(v[o][r >> 1]) : bf16_lo(v[o][r >> 1]);
+        sum = fmaf(x, acc[o][r], sum);
+      }
+    return sum;
   }
-  // += A^T (weights B) over a tile's tokens: rows are A's channels, columns B's.
-  // weight[ks][j] belongs to token 32 ks + 8 g + j.  The weighted operand enters in
-  // three parts, so the state has fp32's accuracy.
-  __device__ __forceinline__ void add_products(const unsigned char* A, const unsigned char* B,
-                                               const float (*weight)[8], int w, int lane) {
+};
+
+// Row 16 b + n of a tile in LDS, channels 32 ks + 8 g + j.
+template <typename T, typename L>
+__device__ __forceinline__ typename Num<T>::V8 row_at(const unsigned char* lds, int b, int n, int ks, int g) {
+  const unsigned char* p = lds + 16 * b * L::kPitch;  // row 16 b + n has row n's swizzle
+  if constexpr (sizeof(T) == 2) {
+    return *reinterpret_cast<const u32x4_t*>(p + L::unit_at(n, 4 * ks + g));
+  } else {
+    const f32x4_t* q = reinterpret_cast<const f32x4_t*>(p + L::unit_at(n, 8 * ks + 2 * g));
+    return {q[0], q[1]};
+  }
+}
+
+// Column 16 cb + n of a tile in LDS, rows 32 ks + .. in split or natural order.
+template <typename T, typename L, bool Split>
+__device__ __forceinline__ typename Num<T>::V8 col_at(const unsigned char* lds, int cb, int ks, int lane) {
+  const int n = lane & 15, g = lane >> 4;
+  const unsigned char* p = lds + 32 * ks * L::kPitch;
+  const int r0 = (Split ? 4 : 8) * g;
+  if constexpr (sizeof(T) == 2) {
+    // four rows of 32 bytes a group of 16 lanes, lane n the (n & 3)-th 8 bytes of row
+    // n / 4; 16 rows on the swizzle is the same, 4 rows on one bit of it is the other
+    int at = L::unit_at(r0 + (n >> 2), (n >> 1) & 1) + 8 * (n & 1), next = at;
+    if constexpr (L::kSwizzled) {
+      at ^= cb << 5;
+      next = Split ? at : at ^ (128 >> L::kShift);
+    } else {
+      at += cb << 5;
+      next = at;
+    }
+    const u32x2_t x = tr_read16(p + at), y = tr_read16(p + (Split ? 16 : 4) * L::kPitch + next);
+    return (u32x4_t){x[0], x[1], y[0], y[1]};
+  } else {
+    constexpr int P = L::kPitch / 4, next = (Split ? 16 : 4) * P;
+    const float* q = reinterpret_cast<const float*>(p + r0 * L::kPitch) + 16 * cb + n;
+    return {{q[0], q[P], q[2 * P], q[3 * P]}, {q[next], q[next + P], q[next + 2 * P], q[next + 3 * P]}};
+  }
+}
+
+// Order of N products that each take one operand from LDS (by one read of 16 bytes in
+// bf16, two in fp32), and M more beside which vector work goes on, two at a time with
+// `pair` reads for the two in bf16: eight operands ahead, eight vector instructions after
+// each two of the M.  Left to itself the compiler keeps one or two reads in flight, so
+// that the wave waits for LDS before every product, and puts the vector work behind the
+// products.
+template <typename T, int N, int M, int Pair = 2>
+__device__ __forceinline__ void pipeline() {
+  constexpr int kValu = 0x2, kMfma = 0x8, kRead = 0x100;
+  constexpr bool half = sizeof(T) == 2;
+  constexpr int reads = half ? 1 : 2, mfmas = half ? 1 : 8;
+  constexpr int pair = half ? Pair : Pair == 2 ? 4 : 16;
+  __builtin_amdgcn_sched_group_barrier(kRead, 8 * reads, 0);
 #pragma unroll
-    for (int ks = 0; ks < kTile / 32; ++ks) {
-      float x[8];
-      Num<T>::widen(col_at<T, C, false>(B, C::col_block(w), ks, lane), x);
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, mfmas, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, reads, 0);
+  }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= weight[ks][j];
-      Parts<T, 3> b;
-      b.set(x);
-#pragma unroll
-      for (int i = 0; i < C::SB; ++i)
-        b.mma_right(s[i], col_at<T, C, false>(A, C::row_block(w) + i, ks, lane));
+  for (int i = 0; i < M / 2; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, 2 * mfmas, 0);
+    if (i < M / 2 - 4) __builtin_amdgcn_sched_group_barrier(kRead, pair, 0);
+    __builtin_amdgcn_sched_group_barrier(kValu, 8, 0);
+  }
+}
+
+// Powers of the decay in LDS: up[i] = scale lam^(i+1); down[i] = lam^(63-i), zeros
+// from 64 on, so that down + 64 - L holds the weights lam^(L-1-t) of a tile of L
+// tokens and nothing for the rows behind it.
+struct Powers {
+  float up[kTile];
+  float down[2 * kTile];
+  __device__ __forceinline__ void fill(const Decay& lam, float scale) {
+    const int i = threadIdx.x;
+    if (i < kTile) {
+      up[i] = scale * lam(i + 1);
+      down[i] = lam(kTile - 1 - i);
+      down[kTile + i] = 0.0f;
     }
   }
 };
+
+// A wave's blocks of a state X[row][column] in fp32; the workgroup's columns start at
+// col0 of D.
+template <typename T, typename C>
+struct State {
+  f32x4_t s[C::SR];  // block i: rows 16 (rb + i) + 4 g + r, column 16 cb + n
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < C::SR; ++i) s[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // from / to memory [row][column] (or [column][row])
+  __device__ __forceinline__ void load(const float* m, bool transposed, int col0, int w, int lane) {
+    const int col = col0 + 16 * C::col_block(w) + (lane & 15), row = 16 * C::row_block(w) + 4 * (lane >> 4);
+#pragma unroll
+    for (int i = 0; i < C::SR; ++i) {
+      if (transposed) {
+        s[i] = *reinterpret_cast<const f32x4_t*>(m + col * C::D + row + 16 * i);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[i][r] = m[(row + 16 * i + r) * C::D + col];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float* m, int col0, int w, int lane) const {
+    const int col = col0 + 16 * C::col_block(w) + (lane & 15), row = 16 * C::row_block(w) + 4 * (lane >> 4);
+#pragma unroll
+    for (int i = 0; i < C::SR; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m[(row + 16 * i + r) * C::D + col] = s[i][r];
+  }
+  // into the planes [the workgroup's column][row]
+  __device__ __forceinline__ void to_planes(unsigned char* planes, int w, int lane) const {
+    const int g = lane >> 4, col = 16 * C::col_block(w) + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < C::SR; ++i) {
+      const f32x4_t x = s[i];
+      const int row = 16 * (C::row_block(w) + i) + 4 * g;
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4_t*>(planes + C::Wide::unit_at(col, row >> 2)) = x;
+      } else {
+        unsigned char* p = planes + C::Wide::unit_at(col, row >> 3) + 8 * (g & 1);
+        const uint32_t h0 = pack_bf16x2(x[0], x[1]), h1 = pack_bf16x2(x[2], x[3]);
+        *reinterpret_cast<u32x2_t*>(p) = (u32x2_t){h0, h1};
+        if constexpr (C::NP == 2)
+          *reinterpret_cast<u32x2_t*>(p + C::kPlane) =
+              (u32x2_t){pack_bf16x2(x[0] - bf16_lo(h0), x[1] - bf16_hi(h0)),
+                        pack_bf16x2(x[2] - bf16_lo(h1), x[3] - bf16_hi(h1))};
+      }
+    }
+  }
+  // s = f s + A^T (weight B) over a tile's tokens: rows are A's channels, columns
+  // B's (its value channels), weight[t] token t's.  The weighted operand enters in three
+  // parts and the tile's products are summed by themselves, so the state has fp32's
+  // accuracy.
+  __device__ __forceinline__ void advance(float f, const unsigned char* A, const unsigned char* B,
+                                          const float* weight, int w, int lane) {
+    Parts<T, 3> b[2];
+#pragma unroll
+    for (int ks = 0; ks < kTile / 32; ++ks) {
+      float x[8];
+      Num<T>::widen(col_at<T, typename C::Slim, true>(B, C::col_block(w), ks, lane), x);
+      const float* p = weight + 32 * ks + 4 * (lane >> 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[j] *= p[j];
+        x[4 + j] *= p[16 + j];
+      }
+      b[ks].set(x);
+    }
+    constexpr int G = C::SR < 4 ? C::SR : 4;  // blocks at a time, as independent chains
+#pragma unroll
+    for (int i0 = 0; i0 < C::SR; i0 += G) {
+      f32x4_t x[G];
+#pragma unroll
+      for (int i = 0; i < G; ++i) x[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int ks = 0; ks < kTile / 32; ++ks) {
+        typename Num<T>::V8 a[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+          a[i] = col_at<T, typename C::Wide, true>(A, C::row_block(w) + i0 + i, ks, lane);
+#pragma unroll
+        for (int y = Parts<T, 3>::kN - 1; y >= 0; --y)
+#pragma unroll
+          for (int i = 0; i < G; ++i) Num<T>::mma(x[i], a[i], b[ks].v[y]);
+      }
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[i0 + i][r] = fmaf(f, s[i0 + i][r], x[i][r]);
+    }
+  }
+};
+
+// Decays of a wave's scores: scale lam^(distance) of row 16 b + 4 g + i and the
+// wave's own token 16 tw + n.  Own tokens are the later ones (Later) or the earlier
+// ones; pairs of the wrong order are zero.
+template <bool Later>
+struct Scores {
+  float same[4], next[4], far[2];  // block tw; 16 tokens away; factors for 32 and 48
+  __device__ __forceinline__ void fill(const Decay& lam, float scale, int n, int g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = Later ? n - 4 * g - i : 4 * g + i - n;
+      same[i] = scale * lam(max(0, d));
+      next[i] = scale * lam(16 + d);
+    }
+    far[0] = lam(16);
+    far[1] = lam(32);
+  }
+  // `away`: blocks between the rows' block and the own one, negative where all pairs
+  // are of the wrong order.  Selects only: with branches here the compiler left one to
+  // five wait states between the product that forms x and its first use, where seven
+  // are due (and the results were wrong).
+  __device__ __forceinline__ void apply(f32x4_t& x, int away, int n, int g) const {
+    const float f = away <= 1 ? 1.0f : away == 2 ? far[0] : far[1];
+    const bool near = away == 0, none = away < 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool wrong = Later ? 4 * g + i > n : 4 * g + i < n;
+      const float w = near ? same[i] : next[i] * f;
+      x[i] = none | (near & wrong) ? 0.0f : x[i] * w;
+    }
+  }
+};
+
+// acc += (rows of a tile, K step ks)^T scores, the scores of its two 16-row blocks
+// [rows] x [own tokens], in N parts; the rows' blocks from block `first` on.
+template <typename T, typename C, typename L, int N>
+__device__ __forceinline__ void add_scored(f32x4_t* acc, const f32x4_t& a, const f32x4_t& b,
+                                           const unsigned char* rows, int ks, int first, int lane) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  Parts<T, N> p;
+  p.set(x);
+  typename Num<T>::V8 v[C::OB];
+#pragma unroll
+  for (int o = 0; o < C::OB; ++o) v[o] = col_at<T, L, true>(rows, first + o, ks, lane);
+#pragma unroll
+  for (int y = Parts<T, N>::kN - 1; y >= 0; --y)
+#pragma unroll
+    for (int o = 0; o < C::OB; ++o) Num<T>::mma(acc[o], v[o], p.v[y]);
+}
+
+// The record slot of the first unit of a packed sequence that starts at row c: slots
+// of different sequences never meet (the next starts at least ceil(len / unit) later),
+// and no prefix sum over the lengths is needed.  The last slot is below T / unit + N.
+__device__ __forceinline__ int first_slot(const DecayPlan& P, int c, int s) { return c / P.unit + s; }
 
 // The unit (split) or sequence (single) of a workgroup: tokens [begin, end) of
 // sequence s, whose first row is `row0` of a head's rows.
@@ -297,35 +482,46 @@ struct Span {
 };
 
 // Every thread of the workgroup must call it; false for the whole workgroup where
-// there is none.
+// there is none (a slot that no unit has).
 template <int NT>
 __device__ __forceinline__ bool find_span(const DecayPlan& P, const int32_t* cu, int u, Span* o) {
   if (P.single) {
     o->s = u;
-    o->idx = 0;
   } else if (P.ragged) {
-    if (!locate_unit<NT>(cu, P.nseq, P.unit, u, &o->s, &o->idx)) return false;
+    __shared__ int found;
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    for (int s = threadIdx.x; s < P.nseq; s += NT) {
+      const int c = cu[s], i = u - first_slot(P, c, s);
+      if (i >= 0 && i < units_of((int64_t)cu[s + 1] - c, P.unit)) found = s;
+    }
+    __syncthreads();
+    o->s = __builtin_amdgcn_readfirstlane(found);
+    if (o->s < 0) return false;
   } else {
     o->s = u / P.units_per_seq;
-    o->idx = u - o->s * P.units_per_seq;
   }
   if (P.ragged) {
     o->row0 = cu[o->s];
     o->len = cu[o->s + 1] - cu[o->s];
+    o->slot = first_slot(P, cu[o->s], o->s);
   } else {
     o->row0 = 0;
     o->len = P.rows;
+    o->slot = o->s * P.units_per_seq;
   }
-  o->begin = P.single ? 0 : o->idx * P.unit;
+  o->idx = P.single ? 0 : u - o->slot;
+  o->slot += o->idx;
+  o->begin = o->idx * P.unit;
   o->end = P.single ? o->len : min(o->len, o->begin + P.unit);
   o->last = o->end >= o->len;
-  o->slot = u;
   return true;
 }
 
-// Row of token t of span s in head h (of `heads`), in elements of a [.., D] tensor.
-__device__ __forceinline__ int64_t row_of(const DecayPlan& P, const Span& s, int heads, int h, int t) {
-  return (P.ragged ? (int64_t)h * P.rows + s.row0 : ((int64_t)s.s * heads + h) * P.rows) + t;
+// Row of the first token of span s in head h (of `heads`) of a [.., D] tensor; the rows
+// of head h + 1 are P.rows further.
+__device__ __forceinline__ int64_t first_row(const DecayPlan& P, const Span& s, int heads, int h) {
+  return P.ragged ? (int64_t)h * P.rows + s.row0 : ((int64_t)s.s * heads + h) * P.rows;
 }
 
 }  // namespace gbla
