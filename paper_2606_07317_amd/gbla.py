@@ -543,20 +543,29 @@ def _on(device, stream):
     return torch.cuda.stream(stream)
 
 
-def _like(t, name, shape, dtype, device):
-    """``t`` if it can take an output of this shape and type, else a new tensor."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _check(t, name, dtype, device)
-    if t.shape != tuple(shape):
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    return t
+# The handle of a device's current stream: torch's own shortcut where it has one, since
+# building a Stream object takes longer (1.9 us) than a small kernel's whole call should.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _current(device) -> int:
+    if _raw_stream is not None:
+        return _raw_stream(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _want(t, name, shape, dtype, device):
     _check(t, name, dtype, device)
-    if t.shape != tuple(shape):
+    if t.shape != shape:  # shape: a torch.Size or a tuple
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+
+
+def _like(t, name, x):
+    """``t`` if it can take an output of the shape and type of x, else a new tensor."""
+    if t is None:
+        return torch.empty_like(x)
+    _want(t, name, x.shape, x.dtype, x.device)
+    return t
 
 
 def _query_key(q, k, cu_seqlens):
@@ -611,11 +620,11 @@ def qk_norm_rope(q, k, q_w, k_w, positions=None, cu_seqlens=None, rotary_dim=Non
     _check_rope(q, k, q_w, k_w, positions, cu_seqlens, shape)
     dev = q.device
     with _on(dev, stream):
-        q_out = _like(q_out, "q_out", q.shape, q.dtype, dev)
-        k_out = _like(k_out, "k_out", k.shape, q.dtype, dev)
+        q_out = _like(q_out, "q_out", q)
+        k_out = _like(k_out, "k_out", k)
         st = load_library().gbla_qk_norm_rope(
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_w), _ptr(k_w), _ptr(positions),
-            _ptr(cu_seqlens), _ptr(q_out), _ptr(k_out), torch.cuda.current_stream(dev).cuda_stream)
+            _ptr(cu_seqlens), _ptr(q_out), _ptr(k_out), _current(dev))
     _raise(st, "gbla_qk_norm_rope")
     return q_out, k_out
 
@@ -646,16 +655,16 @@ def qk_norm_rope_backward(q, k, q_w, k_w, dq_out, dk_out, positions=None, cu_seq
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         _check_ws(workspace, dev, need)
-        g["dq"] = _like(g.get("dq"), "dq", q.shape, q.dtype, dev)
-        g["dk"] = _like(g.get("dk"), "dk", k.shape, q.dtype, dev)
+        g["dq"] = _like(g.get("dq"), "dq", q)
+        g["dk"] = _like(g.get("dk"), "dk", k)
         if not flags & NO_NORM:
-            g["dq_w"] = _like(g.get("dq_w"), "dq_w", q_w.shape, torch.float32, dev)
-            g["dk_w"] = _like(g.get("dk_w"), "dk_w", k_w.shape, torch.float32, dev)
+            g["dq_w"] = _like(g.get("dq_w"), "dq_w", q_w)
+            g["dk_w"] = _like(g.get("dk_w"), "dk_w", k_w)
         st = load_library().gbla_qk_norm_rope_backward(
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(q_w), _ptr(k_w), _ptr(positions),
             _ptr(cu_seqlens), _ptr(dq_out), _ptr(dk_out), _ptr(workspace), workspace.numel(),
             _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g.get("dq_w")), _ptr(g.get("dk_w")),
-            torch.cuda.current_stream(dev).cuda_stream)
+            _current(dev))
     _raise(st, "gbla_qk_norm_rope_backward")
     return g
 
@@ -712,14 +721,14 @@ def decay_attention(q, k, v, log_decay, scale: Optional[float] = None, initial_s
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         _check_ws(workspace, dev, need)
-        out = _like(out, "out", q.shape, q.dtype, dev)
+        out = _like(out, "out", q)
         if given is None and final_state:
             d = shape.head_dim
             given = torch.empty((shape.batch, shape.kv_heads, d, d), dtype=torch.float32, device=dev)
         st = load_library().gbla_decay_forward(
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(initial_state),
             _ptr(cu_seqlens), _ptr(workspace), workspace.numel(), _ptr(out), _ptr(given),
-            torch.cuda.current_stream(dev).cuda_stream)
+            _current(dev))
     _raise(st, "gbla_decay_forward")
     return out, given
 
@@ -745,19 +754,18 @@ def decay_attention_backward(q, k, v, log_decay, dout, scale: Optional[float] = 
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         _check_ws(workspace, dev, need)
-        g["dq"] = _like(g.get("dq"), "dq", q.shape, q.dtype, dev)
-        g["dk"] = _like(g.get("dk"), "dk", k.shape, q.dtype, dev)
-        g["dv"] = _like(g.get("dv"), "dv", k.shape, q.dtype, dev)
+        g["dq"] = _like(g.get("dq"), "dq", q)
+        g["dk"] = _like(g.get("dk"), "dk", k)
+        g["dv"] = _like(g.get("dv"), "dv", k)
         if decay_grad:
-            g["dlog_decay"] = _like(g.get("dlog_decay"), "dlog_decay", log_decay.shape, torch.float32,
-                                    dev)
+            g["dlog_decay"] = _like(g.get("dlog_decay"), "dlog_decay", log_decay)
         if initial_state is not None and g.get("dinitial_state") is None:
             g["dinitial_state"] = torch.empty_like(initial_state)
         st = load_library().gbla_decay_backward(
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(initial_state),
             _ptr(cu_seqlens), _ptr(dout), _ptr(dfinal_state), _ptr(workspace), workspace.numel(),
             _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]),
-            _ptr(g["dlog_decay"]) if decay_grad else None, _ptr(g.get("dinitial_state")), torch.cuda.current_stream(dev).cuda_stream)
+            _ptr(g["dlog_decay"]) if decay_grad else None, _ptr(g.get("dinitial_state")), _current(dev))
     _raise(st, "gbla_decay_backward")
     return g
 
@@ -787,9 +795,9 @@ def decay_step(q, k, v, log_decay, state, state_indices=None, scale: Optional[fl
         _want(state_indices, "state_indices", (N,), torch.int32, dev)
     shape = DecayShape(N, 1, H, K, d, 0, _dtype_code(q), float(d) ** -0.5 if scale is None else float(scale))
     with _on(dev, stream):
-        out = _like(out, "out", q.shape, q.dtype, dev)
+        out = _like(out, "out", q)
         st = load_library().gbla_decay_step(
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state_indices),
-            state.shape[0], _ptr(state), _ptr(out), torch.cuda.current_stream(dev).cuda_stream)
+            state.shape[0], _ptr(state), _ptr(out), _current(dev))
     _raise(st, "gbla_decay_step")
     return out
