@@ -9,10 +9,9 @@
 // Every power has an exponent >= 0, so strong decays underflow to 0 and nothing
 // overflows.
 //
-// A workgroup walks the tiles of a unit with the state in registers (four waves; at
-// d = 128 eight, each with half of the output's channels).  Wave w owns tokens
-// 16 (w & 3) .. of a tile for the scores and outputs, and a 16-column block of the
-// state.  Units of one sequence run at the same time: a first launch sums every
+// A workgroup of four waves walks the tiles of a unit with the state in registers.  Wave
+// w owns tokens 16 w .. of a tile for the scores and outputs, and a 16-column block of
+// the state.  Units of one sequence run at the same time: a first launch sums every
 // unit's own k v^T (record_kernel), a second carries the records from unit to unit
 // (scan_kernel), the third walks (walk_kernel).  Sequences of one unit, and batches
 // that fill the chip by themselves, take the third alone.
@@ -34,9 +33,12 @@ using RecordSizes = DC<T, D, D, D == 128 ? 8 : 4, 1, false>;
 // a CU, so that one's matrix products meet the other's vector work.  (One of eight waves,
 // which the barriers keep in step: its time was the sum of the matrix, the vector and the
 // LDS work.)  Two parts of the state and of the scores leave 2^-17 of a term, far below
-// the bf16 rounding of the results that they form.
-template <typename T, int D>
-using WalkSizes = DC<T, D, D == 128 ? 64 : D, 4, 2, true>;
+// the bf16 rounding of the results that they form.  Back, the state's products with the
+// rows also form the decay's gradient, an fp32 sum of both signs: with three parts its
+// error is 0.1e-6 .. 0.5e-6 where it was 1e-6 .. 3e-6, for 2 % of a backward at d = 64 and
+// 6 % at d = 128.
+template <typename T, int D, bool Back>
+using WalkSizes = DC<T, D, D == 128 ? 64 : D, 4, Back ? 3 : 2, true>;
 
 // Records: the sum of a unit's own products, A^T (weights B).
 //   Reverse = false: weights lam^(tokens of the unit after t), for the state after it;
@@ -192,10 +194,10 @@ scan_kernel(DecayPlan P, const float* log_decay, const int32_t* cu, const float*
 // with q the forward's queries in `other`.
 // Shared: several query heads to a key head.
 template <typename T, int D, bool Back, bool Shared>
-__global__ void __launch_bounds__((WalkSizes<T, D>::NT), (sizeof(T) == 2 && D == 32 ? 4 : 2))
+__global__ void __launch_bounds__((WalkSizes<T, D, Back>::NT), (sizeof(T) == 2 && D == 32 ? 4 : 2))
 walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_decay, const float* S0,
             const int32_t* cu, float* rec, T* out, float* final_state, const T* other, double* dg) {
-  using C = WalkSizes<T, D>;
+  using C = WalkSizes<T, D, Back>;
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[kTile * C::Wide::kPitch],
       ldsV[kTile * C::Slim::kPitch], ldsS[C::NP * C::kPlane];
   __shared__ __attribute__((aligned(16))) Powers pw;
@@ -344,7 +346,7 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 
 template <typename T, int D>
 dim3 walk_grid(const DecayPlan& p) {
-  const bool whole = WalkSizes<T, D>::VD == D;
+  const bool whole = WalkSizes<T, D, false>::VD == D;
   return dim3(whole ? p.grid_units : (p.grid_units + 7) / 8 * 16, p.kv_heads);
 }
 
@@ -377,7 +379,7 @@ gbla_status launch_decay_forward(const DecayPlan& p, const void* q, const void* 
                          st, p, log_decay, cu, S0, false, rec, (const float*)nullptr, (float*)nullptr);
     }
     const auto walk = p.group > 1 ? walk_kernel<T, D, false, true> : walk_kernel<T, D, false, false>;
-    hipLaunchKernelGGL(walk, (walk_grid<T, D>(p)), dim3((WalkSizes<T, D>::NT)), 0, st, p, (const T*)q, (const T*)k, (const T*)v, log_decay,
+    hipLaunchKernelGGL(walk, (walk_grid<T, D>(p)), dim3((WalkSizes<T, D, false>::NT)), 0, st, p, (const T*)q, (const T*)k, (const T*)v, log_decay,
                        S0, cu, rec, (T*)out, final_state, (const T*)nullptr, (double*)nullptr);
   });
 }
@@ -403,7 +405,7 @@ gbla_status launch_decay_backward(const DecayPlan& p, const void* q, const void*
                          dim3(kThreads), 0, st, p, log_decay, cu, S0, true, recS, dfinal, recD);
     }
     const auto walk = p.group > 1 ? walk_kernel<T, D, true, true> : walk_kernel<T, D, true, false>;
-    hipLaunchKernelGGL(walk, (walk_grid<T, D>(p)), dim3((WalkSizes<T, D>::NT)), 0, st, p, (const T*)dout, (const T*)v, (const T*)k,
+    hipLaunchKernelGGL(walk, (walk_grid<T, D>(p)), dim3((WalkSizes<T, D, false>::NT)), 0, st, p, (const T*)dout, (const T*)v, (const T*)k,
                        log_decay, S0, cu, p.single && !dg ? (float*)nullptr : recS, (T*)dq, (float*)nullptr, (const T*)q, dg);
   });
   if (done != GBLA_OK) return done;

@@ -29,8 +29,10 @@
 namespace gbla {
 namespace {
 
+// Three parts of D, since its products with the rows form the decay's gradient as well,
+// an fp32 sum of both signs.
 template <typename T, int D>
-using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, 2, false>;
+using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, 3, false>;
 
 // Shared: several query heads to a key head.
 template <typename T, int D, bool Shared>

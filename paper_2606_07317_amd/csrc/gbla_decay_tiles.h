@@ -364,12 +364,13 @@ struct State {
         *reinterpret_cast<f32x4_t*>(planes + C::Wide::unit_at(col, row >> 2)) = x;
       } else {
         unsigned char* p = planes + C::Wide::unit_at(col, row >> 3) + 8 * (g & 1);
-        const uint32_t h0 = pack_bf16x2(x[0], x[1]), h1 = pack_bf16x2(x[2], x[3]);
-        *reinterpret_cast<u32x2_t*>(p) = (u32x2_t){h0, h1};
-        if constexpr (C::NP == 2)
-          *reinterpret_cast<u32x2_t*>(p + C::kPlane) =
-              (u32x2_t){pack_bf16x2(x[0] - bf16_lo(h0), x[1] - bf16_hi(h0)),
-                        pack_bf16x2(x[2] - bf16_lo(h1), x[3] - bf16_hi(h1))};
+        f32x4_t rest = x;
+#pragma unroll
+        for (int j = 0; j < C::NP; ++j) {
+          const uint32_t a = pack_bf16x2(rest[0], rest[1]), b = pack_bf16x2(rest[2], rest[3]);
+          *reinterpret_cast<u32x2_t*>(p + j * C::kPlane) = (u32x2_t){a, b};
+          rest -= (f32x4_t){bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b)};
+        }
       }
     }
   }
