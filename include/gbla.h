@@ -313,6 +313,8 @@ gbla_status gbla_layer_forward(const gbla_layer_shape* shape, const void* x,
  * - Ragged batches may end before the tensors do (cu[N_s] <= T): rows from
  *   cu[N_s] on are neither read nor written.
  * - Batches without tokens are accepted (arrays over the tokens may be NULL).
+ * - Outputs overlap neither inputs nor each other, except where it says so.  Calls
+ *   may share a workspace as long as they run one after the other.
  * - Tokens of one sequence never reach another's results.  Within a sequence,
  *   an infinite or NaN value may also reach outputs of earlier tokens that lie
  *   within the same 64 tokens of a launch's split.

@@ -9,8 +9,11 @@
 namespace gbla {
 namespace {
 
-constexpr int64_t kMaxGridX = 2147483647LL;
+// A grid's first dimension has fewer than 2^32 threads; the workgroups here have up to 512
+// (or two of 256 to a unit) and 256.
+constexpr int64_t kMaxGroups512 = 4294967295LL / 512, kMaxGroups256 = 4294967295LL / 256;
 constexpr int kMaxGridY = 65535;
+constexpr int kMaxPasses = 16;  // of a workgroup of the rotation's backward
 
 bool head_dim_ok(int32_t d) { return d == 32 || d == 64 || d == 128; }
 bool dtype_ok(int32_t t) { return t == GBLA_F32 || t == GBLA_BF16; }
@@ -76,11 +79,11 @@ gbla_status make_decay_plan(const gbla_decay_shape* s, bool ragged, bool backwar
   q.ragged = ragged ? 1 : 0;
   q.scale = s->scale;
   q.tokens = ragged ? (int64_t)s->seqlen : (int64_t)s->batch * s->seqlen;
+  if (q.tokens > kMaxGroups512 * kMaxUnit) return GBLA_ERR_UNSUPPORTED;  // before products with them
   q.unit = unit_tokens(q);
   // sum over the sequences of max(1, ceil(len / unit)) <= tokens / unit + N
   const int64_t cap = q.tokens / q.unit + q.nseq;
-  // grids: units, and the slices of 256 elements of every sequence's state
-  if (cap > kMaxGridX / 2 || (int64_t)q.nseq * (q.d * q.d / 128) > kMaxGridX) return GBLA_ERR_UNSUPPORTED;
+  if (cap > kMaxGroups512 - 8) return GBLA_ERR_UNSUPPORTED;
   if (ragged) {
     q.units = (int32_t)cap;
   } else {
@@ -90,6 +93,8 @@ gbla_status make_decay_plan(const gbla_decay_shape* s, bool ragged, bool backwar
     q.units = (int32_t)(each * q.nseq);
   }
   q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows, backward) ? 1 : 0;
+  // the split's scan has a workgroup for every 256 elements of a sequence's states
+  if ((int64_t)q.nseq * (q.d * q.d / 128) > kMaxGroups256) q.single = 1;
   q.grid_units = q.single ? q.nseq : q.units;
   const size_t states = (size_t)cap * q.kv_heads * q.d * q.d * sizeof(float);
   size_t off = 0;
@@ -133,6 +138,7 @@ gbla_status make_rope_plan(const gbla_rope_shape* s, bool ragged, bool backward,
   q.tokens = ragged ? (int64_t)s->seqlen : (int64_t)s->batch * s->seqlen;
   q.tile = 256 / (q.d / 8);
   const int64_t tiles = (q.tokens + q.tile - 1) / q.tile;
+  if (tiles > kMaxGroups256 * kMaxPasses) return GBLA_ERR_UNSUPPORTED;  // before products with them
   // Workgroups of one pass and up to eight heads; fewer heads while that gives
   // few workgroups.
   const int32_t all = q.heads + q.kv_heads;
@@ -145,10 +151,10 @@ gbla_status make_rope_plan(const gbla_rope_shape* s, bool ragged, bool backward,
   // are many, so that few are added up.
   int64_t passes = 1;
   if (backward)
-    while (tiles / passes * q.head_blocks > 2048 && passes < 16) passes *= 2;
+    while (tiles / passes * q.head_blocks > 2048 && passes < kMaxPasses) passes *= 2;
   q.passes = (int32_t)passes;
   const int64_t blocks = (tiles + passes - 1) / passes;
-  if (blocks > kMaxGridX) return GBLA_ERR_UNSUPPORTED;
+  if (blocks > kMaxGroups256) return GBLA_ERR_UNSUPPORTED;
   q.blocks = (int32_t)blocks;
   for (int i = 0; i < q.rotary / 2; ++i)
     q.turns[i] = pow((double)s->theta, -2.0 * i / q.rotary) / (2.0 * 3.14159265358979323846);
