@@ -555,8 +555,13 @@ def _current(device) -> int:
 
 
 def _want(t, name, shape, dtype, device):
+    """Refuses a tensor that is not what the call takes; shape: a torch.Size or a tuple.
+    ``device`` is one that has been checked already."""
+    if (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.device == device
+            and t.is_contiguous()):
+        return
     _check(t, name, dtype, device)
-    if t.shape != shape:  # shape: a torch.Size or a tuple
+    if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
 
 
@@ -568,26 +573,31 @@ def _like(t, name, x):
     return t
 
 
+def _size_of(t, dim, at) -> int:
+    return t.shape[at] if isinstance(t, torch.Tensor) and t.dim() == dim else 0
+
+
 def _query_key(q, k, cu_seqlens):
     """Batch, tokens per head, head counts and head dim of q and k, which may have
     different head counts."""
     _check(q, "q")
-    _check(k, "k", q.dtype, q.device)
+    dev = q.device
     if cu_seqlens is None:
-        if q.dim() != 4 or k.dim() != 4:
+        if q.dim() != 4:
             raise ValueError("dense q and k must be [B, H, n, d]")
         B, H, n, d = q.shape
-        if k.shape[0] != B or k.shape[2:] != q.shape[2:]:
-            raise ValueError("k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
-        return B, n, H, k.shape[1], d
-    _check(cu_seqlens, "cu_seqlens", torch.int32, q.device)
+        K = _size_of(k, 4, 1)
+        _want(k, "k", (B, K, n, d), q.dtype, dev)
+        return B, n, H, K, d
+    _check(cu_seqlens, "cu_seqlens", torch.int32, dev)
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
         raise ValueError("cu_seqlens must be [N + 1]")
-    if q.dim() != 3 or k.dim() != 3:
+    if q.dim() != 3:
         raise ValueError("ragged q and k must be [H, T, d]")
-    if k.shape[1:] != q.shape[1:]:
-        raise ValueError("k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
-    return cu_seqlens.numel() - 1, q.shape[1], q.shape[0], k.shape[0], q.shape[2]
+    H, T, d = q.shape
+    K = _size_of(k, 3, 0)
+    _want(k, "k", (K, T, d), q.dtype, dev)
+    return cu_seqlens.numel() - 1, T, H, K, d
 
 
 def rope_shape(q, k, cu_seqlens=None, rotary_dim=None, theta: float = 10000.0, eps: float = 1e-6,
@@ -781,16 +791,13 @@ def decay_step(q, k, v, log_decay, state, state_indices=None, scale: Optional[fl
     if q.dim() != 3:
         raise ValueError("q must be [N, H, d]")
     N, H, d = q.shape
-    dev = q.device
-    if not isinstance(k, torch.Tensor) or k.dim() != 3 or k.shape[0] != N or k.shape[2] != d:
-        raise ValueError("k must be [N, K, d]")
-    K = k.shape[1]
-    _check(k, "k", q.dtype, dev)
-    _want(v, "v", k.shape, q.dtype, dev)
+    dev, dtype = q.device, q.dtype
+    K = _size_of(k, 3, 1)
+    _want(k, "k", (N, K, d), dtype, dev)
+    _want(v, "v", (N, K, d), dtype, dev)
     _want(log_decay, "log_decay", (K,), torch.float32, dev)
-    _check(state, "state", torch.float32, dev)
-    if state.dim() != 4 or state.shape[1:] != (K, d, d):
-        raise ValueError("state must be [slots, K, d, d]")
+    slots = _size_of(state, 4, 0)
+    _want(state, "state", (slots, K, d, d), torch.float32, dev)
     if state_indices is not None:
         _want(state_indices, "state_indices", (N,), torch.int32, dev)
     shape = DecayShape(N, 1, H, K, d, 0, _dtype_code(q), float(d) ** -0.5 if scale is None else float(scale))
@@ -798,6 +805,6 @@ def decay_step(q, k, v, log_decay, state, state_indices=None, scale: Optional[fl
         out = _like(out, "out", q)
         st = load_library().gbla_decay_step(
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state_indices),
-            state.shape[0], _ptr(state), _ptr(out), _current(dev))
+            slots, _ptr(state), _ptr(out), _current(dev))
     _raise(st, "gbla_decay_step")
     return out
