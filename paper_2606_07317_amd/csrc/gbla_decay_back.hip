@@ -29,8 +29,8 @@
 namespace gbla {
 namespace {
 
-// Three parts of D, since its products with the rows form the decay's gradient as well,
-// an fp32 sum of both signs.
+// Three parts of D for the keys' gradient, which forms the decay's as well, an fp32 sum
+// of both signs; two for the values', which is rounded to bf16 only.
 template <typename T, int D>
 using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, 3, false>;
 
@@ -41,6 +41,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
             const float* S0, const int32_t* cu, const T* dout, const float* dfinal,
             const float* recS, const float* recD, T* dk, T* dv, float* dS0, double* dg) {
   using C = KeysSizes<T, D>;
+  constexpr int parts = C::NP < 2 ? C::NP : 2;  // for the values' gradient
   __shared__ __attribute__((aligned(512))) unsigned char ldsQ[kTile * C::Wide::kPitch],
       ldsO[kTile * C::Wide::kPitch], ldsD[C::NP * C::kPlane];
   __shared__ __attribute__((aligned(16))) Powers pw;
@@ -124,7 +125,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-            for (int p = C::NP - 1; p >= 0; --p)
+            for (int p = parts - 1; p >= 0; --p)
 #pragma unroll
               for (int o = 0; o < C::OB; ++o)
                 Num<T>::mma(av[o], row_at<T, typename C::Wide>(ldsD + p * C::kPlane, eh * C::OB + o, n, ks, g), kf.v[ks]);
@@ -138,7 +139,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 #pragma unroll
         for (int p = 0; p < 2; ++p)
           add_scored<T, C, typename C::Wide, 2>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, lane);
-        if (!Shared) pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB>();
+        if (!Shared) pipeline<T, 4 * C::KS, C::KS * parts * C::OB>();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < C::KS; ++ks)
