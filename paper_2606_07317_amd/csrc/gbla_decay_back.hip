@@ -95,6 +95,11 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
     scores.fill(lam, P.scale, n, g);
     pw.fill(lam, P.scale);
 
+    // The lane that LDS addresses are made from, anew for each phase of a step: they free
+    // registers, and a backward (B = 8, n = 2048, H = 16, d = 64) takes 134 us for 139.  At
+    // d = 128, where the walk waits for its own products anyway, it takes 719 for 712.
+    auto place = [&] { return D < 128 ? fresh(lane) : lane; };
+
     for (int tile = tiles - 1; tile >= 0; --tile) {
       const int t0 = sp.begin + tile * kTile, live = min(kTile, sp.end - t0);
       const int64_t krow = (krow0 + t0) * D;
@@ -105,7 +110,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
       for (int gi = 0; gi < (Shared ? P.group : 1); ++gi) {
         lq.store(ldsQ);
         lo.store(ldsO);
-        if (gi == 0) S.to_planes(ldsD, w, lane);
+        if (gi == 0) S.to_planes(ldsD, w, place());
         lds_barrier();
         const bool wrap = !Shared || gi + 1 == P.group;
         fetch(wrap ? t0 - kTile : t0, wrap ? 0 : gi + 1);
@@ -117,10 +122,12 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
         f32x4_t x[4], y[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) x[b] = y[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+        int at_lane = place();
 #pragma unroll
         for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) Num<T>::mma(x[b], row_at<T, typename C::Wide>(ldsQ, b, n, ks, g), kf.v[ks]);
+          for (int b = 0; b < 4; ++b)
+            Num<T>::mma(x[b], row_at<T, typename C::Wide>(ldsQ, b, at_lane & 15, ks, at_lane >> 4), kf.v[ks]);
         if (first) {  // D^T k by rows of the planes [column][row]
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
@@ -128,7 +135,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
             for (int p = parts - 1; p >= 0; --p)
 #pragma unroll
               for (int o = 0; o < C::OB; ++o)
-                Num<T>::mma(av[o], row_at<T, typename C::Wide>(ldsD + p * C::kPlane, eh * C::OB + o, n, ks, g), kf.v[ks]);
+                Num<T>::mma(av[o], row_at<T, typename C::Wide>(ldsD + p * C::kPlane, eh * C::OB + o, at_lane & 15, ks, at_lane >> 4), kf.v[ks]);
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) scores.apply(x[b], b - tw, n, g);
@@ -138,13 +145,15 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
           for (int r = 0; r < 4; ++r) av[o][r] *= out;
 #pragma unroll
         for (int p = 0; p < 2; ++p)
-          add_scored<T, C, typename C::Wide, 2>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, lane);
+          add_scored<T, C, typename C::Wide, 2>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, at_lane);
         if (!Shared) pipeline<T, 4 * C::KS, C::KS * parts * C::OB>();
         __builtin_amdgcn_sched_barrier(0);
+        at_lane = place();
 #pragma unroll
         for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) Num<T>::mma(y[b], row_at<T, typename C::Wide>(ldsO, b, n, ks, g), vf.v[ks]);
+          for (int b = 0; b < 4; ++b)
+            Num<T>::mma(y[b], row_at<T, typename C::Wide>(ldsO, b, at_lane & 15, ks, at_lane >> 4), vf.v[ks]);
         if (first) {  // D v by their columns
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
@@ -152,7 +161,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
             for (int p = C::NP - 1; p >= 0; --p)
 #pragma unroll
               for (int o = 0; o < C::OB; ++o)
-                Num<T>::mma(ak[o], col_at<T, typename C::Wide, false>(ldsD + p * C::kPlane, eh * C::OB + o, ks, lane), vf.v[ks]);
+                Num<T>::mma(ak[o], col_at<T, typename C::Wide, false>(ldsD + p * C::kPlane, eh * C::OB + o, ks, at_lane), vf.v[ks]);
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -173,11 +182,11 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
-          add_scored<T, C, typename C::Wide, 2>(ak, y[2 * p], y[2 * p + 1], ldsQ, p, eh * C::OB, lane);
+          add_scored<T, C, typename C::Wide, 2>(ak, y[2 * p], y[2 * p + 1], ldsQ, p, eh * C::OB, at_lane);
         if (!Shared) pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB, 4>();
         __builtin_amdgcn_sched_barrier(0);
         if (wrap) fetch_own(t0 - kTile);
-        S.advance(gi > 0 ? 1.0f : live == kTile ? full : lam(live), ldsQ, ldsO, pw.up, w, lane);
+        S.advance(gi > 0 ? 1.0f : live == kTile ? full : lam(live), ldsQ, ldsO, pw.up, w, place());
         lds_barrier();
       }
       if (eh == 0) dsum += (double)inner;

@@ -243,6 +243,13 @@ struct OwnPieces {
   }
 };
 
+// A value that the compiler takes for a new one: addresses made from it are worked out
+// where they are used, instead of being held in registers all through a loop.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Row 16 b + n of a tile in LDS, channels 32 ks + 8 g + j.
 template <typename T, typename L>
 __device__ __forceinline__ typename Num<T>::V8 row_at(const unsigned char* lds, int b, int n, int ks, int g) {
