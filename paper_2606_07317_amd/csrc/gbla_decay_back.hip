@@ -35,6 +35,11 @@ template <typename T, int D>
 using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, 3, false>;
 
 // Shared: several query heads to a key head.
+// Measured: bf16, B = 8, n = 2048, H = 16, d = 64 62 us (201 MB, 3.2 TB/s); 16 packed
+// sequences, T = 57,511, H = 8, d = 128 360 us, one workgroup a CU by its LDS, matrix
+// instructions under way in 26 % of a SIMD's cycles and LDS reads in 48 %.  A swizzled
+// layout halves that 48 % and takes as long: the work between two barriers is a chain of
+// products, decays and splits that two waves a SIMD do not cover.
 template <typename T, int D, bool Shared>
 __global__ void __launch_bounds__((KeysSizes<T, D>::NT), 2)
 keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_decay,
