@@ -90,11 +90,6 @@ struct Parts {
       }
     }
   }
-  // c += A this, the smaller parts first
-  __device__ __forceinline__ void mma_right(f32x4_t& c, const typename Num<T>::V8& a) const {
-#pragma unroll
-    for (int i = kN - 1; i >= 0; --i) Num<T>::mma(c, a, v[i]);
-  }
 };
 
 // A tile or plane in LDS: rows of W elements, swizzled or 16 bytes apart.
