@@ -491,16 +491,26 @@ __device__ __forceinline__ bool find_span(const DecayPlan& P, const int32_t* cu,
   if (P.single) {
     o->s = u;
   } else if (P.ragged) {
+    // The last sequence whose first slot is at most u (they increase), by rounds of NT
+    // probes each: one round for up to NT sequences.
     __shared__ int found;
-    if (threadIdx.x == 0) found = -1;
-    __syncthreads();
-    for (int s = threadIdx.x; s < P.nseq; s += NT) {
-      const int c = cu[s], i = u - first_slot(P, c, s);
-      if (i >= 0 && i < units_of((int64_t)cu[s + 1] - c, P.unit)) found = s;
+    int lo = 0, count = P.nseq;
+    while (count > 1) {
+      const int step = (count + NT - 1) / NT, end = lo + count;
+      const int at = lo + (int)threadIdx.x * step;
+      if (threadIdx.x == 0) found = lo;
+      __syncthreads();
+      if (at < end && first_slot(P, cu[at], at) <= u &&
+          (at + step >= end || first_slot(P, cu[at + step], at + step) > u))
+        found = at;
+      __syncthreads();
+      const int f = __builtin_amdgcn_readfirstlane(found);
+      __syncthreads();  // read by all before the next round's write
+      count = min(step, end - f);
+      lo = f;
     }
-    __syncthreads();
-    o->s = __builtin_amdgcn_readfirstlane(found);
-    if (o->s < 0) return false;
+    o->s = lo;
+    if (u - first_slot(P, cu[lo], lo) >= units_of((int64_t)cu[lo + 1] - cu[lo], P.unit)) return false;
   } else {
     o->s = u / P.units_per_seq;
   }

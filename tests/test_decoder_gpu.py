@@ -282,6 +282,18 @@ def test_decay_backward(case, tight):
     _check(got["dlog_decay"], dg, dg_size, 1.0, "dlog_decay")
 
 
+# more sequences than a workgroup has threads, a long one (split into units) among them
+_MANY = [([0, 1, 3, 0, 20, 2] * 110)[:count] + [1500, 0, 7] for count in (254, 255, 600)]
+
+
+@pytest.mark.parametrize("lengths", _MANY, ids=lambda x: str(len(x)))
+@pytest.mark.parametrize("dtype,d", [(BF16, 32), (F32, 64)])
+def test_decay_many_sequences(lengths, dtype, d):
+    case = (lengths, True, 1, 1, d, dtype, True, [-0.01])
+    test_decay_forward(case, True)
+    test_decay_backward(case, True)
+
+
 def test_decay_backward_without_the_decay_gradient_and_into_given_outputs():
     t = _decay_case([700], False, 4, 2, 64, BF16, True, [-0.01, -0.1])
     args = _dev(t["q"], t["k"], t["v"], t["g"], t["dout"])
