@@ -33,7 +33,7 @@ struct DecayPlan {
   // Workspace (bytes from its base)
   size_t off_S;   // [K, units, d, d] fp32: the state before each unit
   size_t off_D;   // backward: [K, units, d, d] the gradient of the state after each unit
-  size_t off_dg;  // backward: [2, K, grid_units, 8] double, parts of dlog_decay
+  size_t off_dg;  // backward: [2, K, grid_units, 4 or 8] double, parts of dlog_decay
   size_t total_bytes;
 };
 

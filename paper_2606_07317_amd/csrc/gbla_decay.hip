@@ -349,7 +349,7 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
   if (Back && dg) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) dsum += __shfl_xor(dsum, o);
-    if (lane == 0) dg[((int64_t)h * P.grid_units + unit) * 8 + e0 / C::VD * 4 + w] = dsum;
+    if (lane == 0) dg[(((int64_t)h * P.grid_units + unit) * halves + e0 / C::VD) * C::NW + w] = dsum;
   }
 }
 

@@ -230,28 +230,28 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
   if (dg) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) dsum += __shfl_xor(dsum, o);
-    if (lane == 0) dg[((int64_t)h * P.grid_units + blockIdx.x) * 8 + w] = dsum;
+    if (lane == 0) dg[((int64_t)h * P.grid_units + blockIdx.x) * C::NW + w] = dsum;
   }
 }
 
-// The sum of a key head's parts: [2][K][grid_units][8] doubles, `waves` of each 8
-// in use.
+// The sum of a key head's parts: [2][K][count] doubles (of walk_kernel and keys_kernel, a
+// wave's each).
 __global__ void __launch_bounds__(kThreads)
-decay_sum_kernel(int kv_heads, int units, int waves, const double* dg, float* out) {
-  __shared__ double red[kThreads];
+decay_sum_kernel(int kv_heads, int64_t count, const double* dg, float* out) {
+  __shared__ double red[kThreads / 64];
   const int h = blockIdx.x;
+  const double* a = dg + h * count;
+  const double* b = a + kv_heads * count;
   double sum = 0.0;
-  for (int half = 0; half < 2; ++half) {
-    const double* p = dg + ((int64_t)half * kv_heads + h) * units * 8;
-    for (int i = threadIdx.x; i < units * waves; i += kThreads) sum += p[(int64_t)(i / waves) * 8 + i % waves];
-  }
-  red[threadIdx.x] = sum;
+  for (int64_t i = threadIdx.x; i < count; i += kThreads) sum += a[i] + b[i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
   __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-    __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kThreads / 64; ++i) sum += red[i];
+    out[h] = (float)sum;
   }
-  if (threadIdx.x == 0) out[h] = (float)red[0];
 }
 
 template <typename T, int D>
@@ -259,15 +259,15 @@ void launch_keys(const DecayPlan& p, const void* q, const void* k, const void* v
                  const float* S0, const int32_t* cu, const void* dout, const float* dfinal,
                  unsigned char* ws, void* dk, void* dv, float* dlog_decay, float* dS0, hipStream_t st) {
   double* dg = dlog_decay ? reinterpret_cast<double*>(ws + p.off_dg) : nullptr;
-  double* mine = dg ? dg + (int64_t)p.kv_heads * p.grid_units * 8 : nullptr;
+  const int64_t count = (int64_t)p.grid_units * KeysSizes<T, D>::NW;
+  double* mine = dg ? dg + p.kv_heads * count : nullptr;
   const auto keys = p.group > 1 ? keys_kernel<T, D, true> : keys_kernel<T, D, false>;
   hipLaunchKernelGGL(keys, dim3(p.grid_units, p.kv_heads), dim3((KeysSizes<T, D>::NT)), 0, st, p,
                      (const T*)q, (const T*)k, (const T*)v, log_decay, S0, cu, (const T*)dout, dfinal,
                      reinterpret_cast<const float*>(ws + p.off_S),
                      reinterpret_cast<const float*>(ws + p.off_D), (T*)dk, (T*)dv, dS0, mine);
   if (dg)
-    hipLaunchKernelGGL(decay_sum_kernel, dim3(p.kv_heads), dim3(kThreads), 0, st, p.kv_heads,
-                       p.grid_units, (KeysSizes<T, D>::NW), dg, dlog_decay);
+    hipLaunchKernelGGL(decay_sum_kernel, dim3(p.kv_heads), dim3(kThreads), 0, st, p.kv_heads, count, dg, dlog_decay);
 }
 
 }  // namespace
