@@ -316,8 +316,10 @@ gbla_status gbla_layer_forward(const gbla_layer_shape* shape, const void* x,
  * - Outputs overlap neither inputs nor each other, except where it says so.  Calls
  *   may share a workspace as long as they run one after the other.
  * - Tokens of one sequence never reach another's results.  Within a sequence,
- *   an infinite or NaN value may also reach outputs of earlier tokens that lie
- *   within the same 64 tokens of a launch's split.
+ *   an infinite or NaN value may also reach results that it has no part in: the
+ *   outputs and the gradients of q of earlier tokens, and the gradients of k and v
+ *   of later ones, where both lie in the same block of 64 tokens (counted from the
+ *   sequence's start).
  * ---------------------------------------------------------------------------
  */
 

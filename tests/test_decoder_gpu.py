@@ -366,6 +366,27 @@ def test_decay_sequences_do_not_reach_each_other():
         assert torch.equal(a[[0, 2, 3]], b[[0, 2, 3]])
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n,dtype", [(300, BF16), (900, BF16), (300, F32)])
+def test_decay_nan_stays_behind_its_block_of_tokens(n, dtype, bad):
+    t = _decay_case([n], False, 2, 1, 64, dtype, False, [-0.01])
+    q, k, v, g, do = _dev(t["q"], t["k"], t["v"], t["g"], t["dout"])
+    out, _ = gbla.decay_attention(q, k, v, g)
+    gr = gbla.decay_attention_backward(q, k, v, g, do)
+    v2, do2 = v.clone(), do.clone()
+    v2[:, :, 100] = bad
+    do2[:, :, 100] = bad
+    out2, _ = gbla.decay_attention(q, k, v2, g)
+    assert torch.equal(out[:, :, :64], out2[:, :, :64])
+    assert not torch.isfinite(out2[:, :, 100:]).any()
+    gr2 = gbla.decay_attention_backward(q, k, v, g, do2)
+    for x in ("dk", "dv"):
+        assert torch.equal(gr[x][:, :, 128:], gr2[x][:, :, 128:]), x
+        assert not torch.isfinite(gr2[x][:, :, :101]).any(), x
+    others = [i for i in range(n) if i != 100]
+    assert torch.equal(gr["dq"][:, :, others], gr2["dq"][:, :, others])
+
+
 def test_decay_without_tokens():
     g = torch.tensor([-0.1, -0.2], device="cuda")
     x = torch.empty(3, 2, 0, 64, dtype=BF16, device="cuda")
