@@ -416,8 +416,9 @@ gbla_status gbla_decay_forward(const gbla_decay_shape* shape, const void* q, con
  *                                     query heads that share them)
  *   dlog_decay      fp32 [K], summed over the batch, or NULL (not wanted)
  *   dinitial_state  fp32 [N,K,d,d] or NULL (not wanted); may be dfinal_state
- * Reductions run in an order fixed by the shape: repeated calls give the same
- * bits.
+ * Gradients are sums in fp32 of products with fp32's accuracy for both types, rounded
+ * once to their type.  Reductions run in an order fixed by the shape: repeated calls
+ * give the same bits.
  */
 gbla_status gbla_decay_backward(const gbla_decay_shape* shape, const void* q, const void* k,
                                 const void* v, const float* log_decay,

@@ -32,13 +32,16 @@ using RecordSizes = DC<T, D, D, D == 128 ? 8 : 4, 1, false>;
 // At d = 128 a walk is two workgroups, each with half of the value channels: two run on
 // a CU, so that one's matrix products meet the other's vector work.  (One of eight waves,
 // which the barriers keep in step: its time was the sum of the matrix, the vector and the
-// LDS work.)  Two parts of the state and of the scores leave 2^-17 of a term, far below
-// the bf16 rounding of the results that they form.  Back, the state's products with the
-// rows also form the decay's gradient, an fp32 sum of both signs: with three parts its
-// error is 0.1e-6 .. 0.5e-6 where it was 1e-6 .. 3e-6, for 2 % of a backward at d = 64 and
-// 6 % at d = 128.
+// LDS work.)  In the forward two parts of the state and of the scores leave 2^-17 of a
+// term, below the bf16 rounding of the output that they form; a third costs 8 % of one
+// prompt (n = 32768, d = 64) and 26 % of the packed prompts (d = 128, shared heads).  Back,
+// the sums are gradients' and have fp32's accuracy, by three parts of both: the state's
+// products also form the decay's gradient, an fp32 sum of both signs (its error is 0.1e-6 ..
+// 0.5e-6 where two parts left 1e-6 .. 3e-6).
+template <bool Back>
+constexpr int kWalkParts = Back ? 3 : 2;
 template <typename T, int D, bool Back>
-using WalkSizes = DC<T, D, D == 128 ? 64 : D, 4, Back ? 3 : 2, true>;
+using WalkSizes = DC<T, D, D == 128 ? 64 : D, 4, kWalkParts<Back>, true>;
 
 // Records: the sum of a unit's own products, A^T (weights B).
 //   Reverse = false: weights lam^(tokens of the unit after t), for the state after it;
@@ -320,7 +323,7 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-          add_scored<T, C, typename C::Slim, 2>(acc, p[2 * x], p[2 * x + 1], ldsV, x, 0, lane);
+          add_scored<T, C, typename C::Slim, kWalkParts<Back>>(acc, p[2 * x], p[2 * x + 1], ldsV, x, 0, lane);
         pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB>();
         if (Shared && gi == 0) fetch_kv(t0 + kTile);
         const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + row, (uint32_t)(live * C::kRow));

@@ -29,10 +29,13 @@
 namespace gbla {
 namespace {
 
-// Three parts of D for the keys' gradient, which forms the decay's as well, an fp32 sum
-// of both signs; two for the values', which is rounded to bf16 only.
+// Three parts of D and of the scores, so that the sums have fp32's accuracy before they
+// are rounded once (with two parts of the scores and of the values' D, 2^-17 of a term, three
+// times as many bf16 gradients differed by a last bit from the fp32 sums; the third parts
+// cost 3 % of a backward).
+constexpr int kKeysParts = 3;
 template <typename T, int D>
-using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, 3, false>;
+using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, kKeysParts, false>;
 
 // Shared: several query heads to a key head.
 // Measured: bf16, B = 8, n = 2048, H = 16, d = 64 62 us (201 MB, 3.2 TB/s); 16 packed
@@ -46,7 +49,6 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
             const float* S0, const int32_t* cu, const T* dout, const float* dfinal,
             const float* recS, const float* recD, T* dk, T* dv, float* dS0, double* dg) {
   using C = KeysSizes<T, D>;
-  constexpr int parts = C::NP < 2 ? C::NP : 2;  // for the values' gradient
   __shared__ __attribute__((aligned(512))) unsigned char ldsQ[kTile * C::Wide::kPitch],
       ldsO[kTile * C::Wide::kPitch], ldsD[C::NP * C::kPlane];
   __shared__ __attribute__((aligned(16))) Powers pw;
@@ -137,7 +139,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-            for (int p = parts - 1; p >= 0; --p)
+            for (int p = C::NP - 1; p >= 0; --p)
 #pragma unroll
               for (int o = 0; o < C::OB; ++o)
                 Num<T>::mma(av[o], row_at<T, typename C::Wide>(ldsD + p * C::kPlane, eh * C::OB + o, at_lane & 15, ks, at_lane >> 4), kf.v[ks]);
@@ -150,8 +152,8 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
           for (int r = 0; r < 4; ++r) av[o][r] *= out;
 #pragma unroll
         for (int p = 0; p < 2; ++p)
-          add_scored<T, C, typename C::Wide, 2>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, at_lane);
-        if (!Shared) pipeline<T, 4 * C::KS, C::KS * parts * C::OB>();
+          add_scored<T, C, typename C::Wide, kKeysParts>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, at_lane);
+        if (!Shared) pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB>();
         __builtin_amdgcn_sched_barrier(0);
         at_lane = place();
 #pragma unroll
@@ -187,7 +189,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
-          add_scored<T, C, typename C::Wide, 2>(ak, y[2 * p], y[2 * p + 1], ldsQ, p, eh * C::OB, at_lane);
+          add_scored<T, C, typename C::Wide, kKeysParts>(ak, y[2 * p], y[2 * p + 1], ldsQ, p, eh * C::OB, at_lane);
         if (!Shared) pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB, 4>();
         __builtin_amdgcn_sched_barrier(0);
         if (wrap) fetch_own(t0 - kTile);
