@@ -139,14 +139,17 @@ __device__ __forceinline__ Token token_at(const RopePlan& P, int64_t tok, const 
   return t;
 }
 
-// cos and sin of the lane's four pairs; the identity past the rotary channels.
+// Whether lane t's channels rotate (all of them, or none: R is a multiple of 8).
+__device__ __forceinline__ bool rotates(const RopePlan& P, int t) { return 8 * t < P.rotary; }
+
+// cos and sin of the lane's four pairs.
 __device__ __forceinline__ void angles(const RopePlan& P, int t, int position, float* c, float* s) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     c[i] = 1.0f;
     s[i] = 0.0f;
   }
-  if (8 * t >= P.rotary) return;
+  if (!rotates(P, t)) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const double turn = (double)position * P.turns[4 * t + i];
@@ -171,6 +174,7 @@ rope_kernel(RopePlan P, const T* q, const T* k, const float* q_w, const float* k
   float c[4], s[4];
   angles(P, t, tok.position, c, s);
   const int h0 = blockIdx.y * P.heads_each, h1 = min(h0 + P.heads_each, P.heads + P.kv_heads);
+  const bool turn = rotates(P, t);
   const bool norm = !(P.flags & GBLA_NO_NORM);
   for (int hh = h0; hh < h1; ++hh) {
     const bool isq = hh < P.heads;
@@ -188,10 +192,11 @@ rope_kernel(RopePlan P, const T* q, const T* k, const float* q_w, const float* k
       for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
     }
     float y[8];
+    // by selects: 0 times an infinite or NaN neighbour is no part of a channel that stays
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      y[i] = x[i] * c[i] - x[4 + i] * s[i];
-      y[4 + i] = x[i] * s[i] + x[4 + i] * c[i];
+      y[i] = turn ? x[i] * c[i] - x[4 + i] * s[i] : x[i];
+      y[4 + i] = turn ? x[i] * s[i] + x[4 + i] * c[i] : x[4 + i];
     }
     Row8<T, Pairs>::store(head_row(P, isq ? q_out : k_out, tok, heads, h), t, P.rotary, y);
   }
@@ -208,6 +213,7 @@ rope_back_kernel(RopePlan P, const T* q, const T* k, const float* q_w, const flo
   const int t = threadIdx.x % L, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int all = P.heads + P.kv_heads;
   const int h0 = blockIdx.y * P.heads_each, h1 = min(h0 + P.heads_each, all);
+  const bool turn = rotates(P, t);
   const bool norm = !(P.flags & GBLA_NO_NORM);
   if (norm) {
     for (int i = threadIdx.x; i < kHeadsEach * (kThreads / 64) * D; i += kThreads)
@@ -231,8 +237,8 @@ rope_back_kernel(RopePlan P, const T* q, const T* k, const float* q_w, const flo
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        u[i] = dy[i] * c[i] + dy[4 + i] * s[i];
-        u[4 + i] = dy[4 + i] * c[i] - dy[i] * s[i];
+        u[i] = turn ? dy[i] * c[i] + dy[4 + i] * s[i] : dy[i];
+        u[4 + i] = turn ? dy[4 + i] * c[i] - dy[i] * s[i] : dy[4 + i];
       }
       if (norm) {
         float w[8], ss = 0.0f, uw = 0.0f;
