@@ -124,8 +124,40 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
         // The values' gradient, then the keys': scores of the tile's tokens (16 a block),
         // the part of D, whose products run while the scores are decayed, the products of
         // the scores.  One after the other, since both at once do not fit the registers.
-        const bool first = !Shared || gi == 0;
-        const float out = first ? lam(max(0, live - 1 - 16 * tw - n)) : 1.0f;
+        // With several query heads the part of D is the first head's, and the branch around
+        // it may not lie between a product and its use (the compiler does not count the wait
+        // states of a jump reliably): it comes first then, and its results are scaled inside.
+        // (Written out twice: from lambdas the single head's kernel took more registers, a
+        // backward of 16 packed sequences, T = 57,511, H = 8, d = 128 787 us for 770.)
+        const float out = lam(max(0, live - 1 - 16 * tw - n));
+        if (Shared && gi == 0) {  // D^T k by rows of the planes [column][row], D v by their columns
+          const int at_lane = place();
+#pragma unroll
+          for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+            for (int p = C::NP - 1; p >= 0; --p)
+#pragma unroll
+              for (int o = 0; o < C::OB; ++o)
+                Num<T>::mma(av[o], row_at<T, typename C::Wide>(ldsD + p * C::kPlane, eh * C::OB + o, at_lane & 15, ks, at_lane >> 4), kf.v[ks]);
+#pragma unroll
+          for (int o = 0; o < C::OB; ++o)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) av[o][r] *= out;
+#pragma unroll
+          for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+            for (int p = C::NP - 1; p >= 0; --p)
+#pragma unroll
+              for (int o = 0; o < C::OB; ++o)
+                Num<T>::mma(ak[o], col_at<T, typename C::Wide, false>(ldsD + p * C::kPlane, eh * C::OB + o, ks, at_lane), vf.v[ks]);
+#pragma unroll
+          for (int o = 0; o < C::OB; ++o)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ak[o][r] *= out;
+          // tokens of the unit after token s
+          const int at = (t0 - sp.begin) & (P.unit - 1), size = min(P.unit, sp.end - (t0 - at));
+          dsum += (double)kp.dot(ak) * (double)(size - 1 - at - 16 * tw - n);
+        }
         f32x4_t x[4], y[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) x[b] = y[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
@@ -135,7 +167,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 #pragma unroll
           for (int b = 0; b < 4; ++b)
             Num<T>::mma(x[b], row_at<T, typename C::Wide>(ldsQ, b, at_lane & 15, ks, at_lane >> 4), kf.v[ks]);
-        if (first) {  // D^T k by rows of the planes [column][row]
+        if (!Shared) {  // D^T k by rows of the planes [column][row]
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
@@ -146,10 +178,12 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) scores.apply(x[b], b - tw, n, g);
+        if (!Shared) {
 #pragma unroll
-        for (int o = 0; o < C::OB; ++o)
+          for (int o = 0; o < C::OB; ++o)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) av[o][r] *= out;
+            for (int r = 0; r < 4; ++r) av[o][r] *= out;
+        }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
           add_scored<T, C, typename C::Wide, kKeysParts>(av, x[2 * p], x[2 * p + 1], ldsO, p, eh * C::OB, at_lane);
@@ -161,7 +195,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 #pragma unroll
           for (int b = 0; b < 4; ++b)
             Num<T>::mma(y[b], row_at<T, typename C::Wide>(ldsO, b, at_lane & 15, ks, at_lane >> 4), vf.v[ks]);
-        if (first) {  // D v by their columns
+        if (!Shared) {  // D v by their columns
 #pragma unroll
           for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
@@ -177,15 +211,14 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
             inner = fmaf(x[b][i] * y[b][i], (float)(16 * (b - tw) + 4 * g + i - n), inner);
           scores.apply(y[b], b - tw, n, g);
         }
+        if (!Shared) {
 #pragma unroll
-        for (int o = 0; o < C::OB; ++o)
+          for (int o = 0; o < C::OB; ++o)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) ak[o][r] *= out;
-        {
+            for (int r = 0; r < 4; ++r) ak[o][r] *= out;
           // tokens of the unit after token s
           const int at = (t0 - sp.begin) & (P.unit - 1), size = min(P.unit, sp.end - (t0 - at));
-          const float dot = first ? kp.dot(ak) : 0.0f;
-          dsum += (double)dot * (double)(size - 1 - at - 16 * tw - n);
+          dsum += (double)kp.dot(ak) * (double)(size - 1 - at - 16 * tw - n);
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
