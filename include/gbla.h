@@ -315,11 +315,11 @@ gbla_status gbla_layer_forward(const gbla_layer_shape* shape, const void* x,
  * - Batches without tokens are accepted (arrays over the tokens may be NULL).
  * - Outputs overlap neither inputs nor each other, except where it says so.  Calls
  *   may share a workspace as long as they run one after the other.
- * - Tokens of one sequence never reach another's results.  Within a sequence,
- *   an infinite or NaN value may also reach results that it has no part in: the
- *   outputs and the gradients of q of earlier tokens, and the gradients of k and v
- *   of later ones, where both lie in the same block of 64 tokens (counted from the
- *   sequence's start).
+ * - Tokens of one sequence never reach another's results, and an infinite or NaN value
+ *   reaches only results that it has a part in: the outputs of its token and later
+ *   ones (so whatever stands behind a padded sequence's end is harmless), the
+ *   gradients of q of later tokens, of k and v of earlier ones, by channels as the
+ *   formulas say; the gradient of a head's decay counts every token.
  * ---------------------------------------------------------------------------
  */
 

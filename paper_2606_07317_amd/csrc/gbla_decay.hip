@@ -192,6 +192,43 @@ scan_kernel(DecayPlan P, const float* log_decay, const int32_t* cu, const float*
   }
 }
 
+// A step's outputs pair by pair (see watch): of the lane's token `own` (a row of the
+// tile's queries at `q`) in the channels that it has stored at `out`.
+template <typename T, int D, bool Back>
+__device__ __forceinline__ void walk_again(T* out, const T* q, int own, int live, int g,
+                                           const unsigned char* ldsK, const unsigned char* ldsV,
+                                           const unsigned char* ldsS, const Decay& lam, float scale) {
+  using C = WalkSizes<T, D, Back>;
+  if (own >= live) return;  // not stored
+  own = fresh(own);  // (what is worked out from them stays in here)
+  g = fresh(g);
+  q += own * D;
+  out += own * D;
+#pragma unroll 1
+  for (int o = 0; o < C::OB; ++o) {
+    const int e = 16 * o + 4 * g;
+    if (__ballot(!finite4(out + e)) == 0) continue;
+    f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int c = 0; c < D; ++c) {
+      const float x = widen1(q[c]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum[r] = fmaf(x, plane_at<T, C>(ldsS, c, e + r), sum[r]);
+    }
+    sum *= scale * lam(own + 1);
+#pragma unroll 1
+    for (int s = 0; s <= own; ++s) {
+      const float x = row_dot<D>(
+          g, [&](int c) { return widen1(q[c]); },
+          [&](int c) { return tile_at<T, typename C::Wide>(ldsK, s, c); });
+      const float w = scale * lam(own - s) * x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum[r] = fmaf(w, tile_at<T, typename C::Slim>(ldsV, s, e + r), sum[r]);
+    }
+    mend4(out + e, sum);
+  }
+}
+
 // The walk.  q, out: `heads` heads, k, v: `kv_heads`.  The state before the unit
 // comes from rec (split) or S0 (single; transposed [e][c] for the gradient of q).
 // final_state: written by the sequence's last unit.  Back (the gradient of q): the
@@ -326,6 +363,8 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
           add_scored<T, C, typename C::Slim, kWalkParts<Back>>(acc, p[2 * x], p[2 * x + 1], ldsV, x, 0, lane);
         pipeline<T, 4 * C::KS, C::KS * C::NP * C::OB>();
         if (Shared && gi == 0) fetch_kv(t0 + kTile);
+        float bad = 0.0f;
+        watch<C::OB>(bad, acc);
         const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + row, (uint32_t)(live * C::kRow));
         const uint32_t at = (uint32_t)((16 * tw + n) * C::kRow + (e0 + 4 * g) * C::ES);
 #pragma unroll
@@ -338,6 +377,8 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
                                                    at + 16 * o * C::ES, 0, 0);
           }
         }
+        if (__builtin_expect(seen(bad), 0))
+          walk_again<T, D, Back>(out + row + e0, q + row, 16 * tw + n, live, g, ldsK, ldsV, ldsS, lam, P.scale);
       }
       if (Shared && ++gi < P.group) continue;
       gi = 0;

@@ -37,6 +37,62 @@ constexpr int kKeysParts = 3;
 template <typename T, int D>
 using KeysSizes = DC<T, D, D, D == 128 ? 8 : 4, kKeysParts, false>;
 
+// What the rows' second pass needs, kept in LDS meanwhile: in scalar registers it leaves the
+// first pass too few (a backward of 16 packed sequences, d = 128 791 us for 756).
+template <typename T>
+struct Rows {
+  const float* init;             // D after the span
+  const T *q, *dout, *k, *v;     // the span's first rows (of the first query head)
+  T *dk, *dv;
+  int64_t head;                  // from one query head's row to the next head's
+  int group, tokens;
+  float scale;
+};
+
+// A tile's gradients pair by pair (see watch): of the lane's token `own` in the channels
+// that it has stored; the tile's rows begin `at` elements after the span's.
+template <typename T, int D>
+__device__ __forceinline__ void keys_again(const Rows<T>& a, int64_t at, int own, int live, int g,
+                                           int eh, const unsigned char* ldsD, const Decay& lam) {
+  using C = KeysSizes<T, D>;
+  if (own >= live) return;  // not stored
+  own = fresh(own);  // (what is worked out from them stays in here)
+  g = fresh(g);
+  // Both gradients by the same code: dv = sum (q k) do + D^T k, dk = sum (do v) q + D v.
+#pragma unroll 1
+  for (int i = 0; i < 2 * C::OB; ++i) {
+    const bool values = i < C::OB;
+    const T* left = (values ? a.q : a.dout) + at;
+    const T* right = (values ? a.dout : a.q) + at;
+    const T* mine = (values ? a.k : a.v) + at + own * D;
+    const int e = 16 * (eh * C::OB + (values ? i : i - C::OB)) + 4 * g;
+    T* to = (values ? a.dv : a.dk) + at + own * D + e;
+    if (__ballot(!finite4(to)) == 0) continue;
+    f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int c = 0; c < D; ++c) {
+      const float x = widen1(mine[c]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        sum[r] = fmaf(x, plane_at<T, C>(ldsD, values ? c : e + r, values ? e + r : c), sum[r]);
+    }
+    sum *= lam(live - 1 - own);
+#pragma unroll 1
+    for (int gi = 0; gi < a.group; ++gi) {
+#pragma unroll 1
+      for (int t = own; t < live; ++t) {
+        const int64_t row = gi * a.head + t * D;
+        const float x = row_dot<D>(
+            g, [&](int c) { return widen1(left[row + c]); }, [&](int c) { return widen1(mine[c]); });
+        const float w = a.scale * lam(t - own) * x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] = fmaf(w, widen1(right[row + e + r]), sum[r]);
+      }
+    }
+    mend4(to, sum);
+  }
+}
+
 // Shared: several query heads to a key head.
 // Measured: bf16, B = 8, n = 2048, H = 16, d = 64 62 us (201 MB, 3.2 TB/s); 16 packed
 // sequences, T = 57,511, H = 8, d = 128 360 us, one workgroup a CU by its LDS, matrix
@@ -52,6 +108,7 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
   __shared__ __attribute__((aligned(512))) unsigned char ldsQ[kTile * C::Wide::kPitch],
       ldsO[kTile * C::Wide::kPitch], ldsD[C::NP * C::kPlane];
   __shared__ __attribute__((aligned(16))) Powers pw;
+  __shared__ Rows<T> rows;
   const int h = blockIdx.y, lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4, tw = w & 3, eh = w >> 2;
@@ -79,6 +136,10 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
     OwnRows<T, C> kf, vf;
     OwnPieces<T, C> kp;
     const int64_t krow0 = first_row(P, sp, P.kv_heads, h), qrow0 = first_row(P, sp, P.heads, h * P.group);
+    if (threadIdx.x == 0)
+      rows = {init, q + (qrow0 + sp.begin) * D, dout + (qrow0 + sp.begin) * D, k + (krow0 + sp.begin) * D,
+              v + (krow0 + sp.begin) * D, dk + (krow0 + sp.begin) * D, dv + (krow0 + sp.begin) * D,
+              (int64_t)P.rows * D, P.group, sp.end - sp.begin, P.scale};
     auto fetch = [&](int t, int gi) {
       const int64_t row = (qrow0 + (int64_t)gi * P.rows + t) * D;
       const int live = t < sp.begin ? 0 : sp.end - t;
@@ -257,6 +318,37 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
 #pragma unroll
             for (int r = 0; r < 4; ++r) dot = fmaf(in.s[i][r], S.s[i][r], dot);
           dsum += (double)dot * (double)size;
+        }
+      }
+    }
+    // The rows again where a value may have reached too far.  That takes a row of q or dout
+    // that is not finite, whose own token's pair (at distance 0) makes the sum for the decay
+    // NaN, or such a D, whose products with k do.
+    const bool mine = __ballot(!isfinite(dsum)) != 0;
+    if (lane == 0) reinterpret_cast<int*>(ldsQ)[w] = mine;
+    lds_barrier();
+    bool again = false;
+#pragma unroll
+    for (int i = 0; i < C::NW; ++i) again |= reinterpret_cast<int*>(ldsQ)[i] != 0;
+    if (__builtin_expect(__ballot(again) != 0, 0)) {
+      const Rows<T> a = rows;
+      if (a.init) S.load(a.init, false, 0, w, lane);
+      else S.clear();
+#pragma unroll 1
+      for (int t0 = (a.tokens - 1) / kTile * kTile; t0 >= 0; t0 -= kTile) {
+        const int live = min(kTile, a.tokens - t0);
+        const int64_t at = (int64_t)t0 * D;
+#pragma unroll 1
+        for (int gi = 0; gi < a.group; ++gi) {
+          lds_barrier();
+          lq.load(a.q + at + gi * a.head, live);
+          lo.load(a.dout + at + gi * a.head, live);
+          lq.store(ldsQ);
+          lo.store(ldsO);
+          if (gi == 0) S.to_planes(ldsD, w, lane);
+          lds_barrier();
+          if (gi == 0) keys_again<T, D>(a, at, 16 * tw + n, live, g, eh, ldsD, lam);
+          S.advance(gi > 0 ? 1.0f : live == kTile ? full : lam(live), ldsQ, ldsO, pw.up, w, lane);
         }
       }
     }

@@ -16,12 +16,6 @@
 namespace gbla {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ float widen1(T x) {
-  if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x << 16);
-  else return x;
-}
-
 constexpr int kGroup = 4;  // query heads of a pass over the registers
 
 template <typename T, int D, int W>

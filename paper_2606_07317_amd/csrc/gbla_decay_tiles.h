@@ -469,6 +469,66 @@ __device__ __forceinline__ void add_scored(f32x4_t* acc, const f32x4_t& a, const
     for (int o = 0; o < C::OB; ++o) Num<T>::mma(acc[o], v[o], p.v[y]);
 }
 
+// Products with an infinite or NaN row of a tile give NaN to tokens that the row has no part
+// in, since a pair of the wrong order enters as 0 times the row.  Results that are not finite
+// are therefore formed again, pair by pair, and take what the recurrence gives; the others
+// stay.  What follows serves that: single elements, in loops that hold few registers, which
+// only such inputs reach (a tile then takes some tens of microseconds).  Looking for them
+// costs 0 to 2 % of a forward and none of a backward.
+
+// z stays 0 while all of x is finite, and is NaN from then on.
+template <int N>
+__device__ __forceinline__ void watch(float& z, const f32x4_t* x) {
+#pragma unroll
+  for (int o = 0; o < N; ++o)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) z = fmaf(x[o][r], 0.0f, z);
+}
+__device__ __forceinline__ bool seen(float z) { return __ballot(z != 0.0f) != 0; }
+template <typename T>
+__device__ __forceinline__ float widen1(T x) {
+  if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x << 16);
+  else return x;
+}
+// The four values that this lane has stored at p: all finite?  y where one is not.
+template <typename T>
+__device__ __forceinline__ bool finite4(const T* p) {
+  return isfinite(widen1(p[0])) && isfinite(widen1(p[1])) && isfinite(widen1(p[2])) && isfinite(widen1(p[3]));
+}
+template <typename T>
+__device__ __forceinline__ void mend4(T* p, const f32x4_t& y) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (isfinite(widen1(p[r]))) continue;
+    if constexpr (sizeof(T) == 2) p[r] = (T)(pack_bf16x2(y[r], 0.0f) & 0xffffu);
+    else p[r] = y[r];
+  }
+}
+// Channel c of row r of a tile in LDS.
+template <typename T, typename L>
+__device__ __forceinline__ float tile_at(const unsigned char* lds, int r, int c) {
+  constexpr int per = 16 / (int)sizeof(T);
+  return widen1(reinterpret_cast<const T*>(lds + L::unit_at(r, c / per))[c % per]);
+}
+// X[row][column] from its planes.
+template <typename T, typename C>
+__device__ __forceinline__ float plane_at(const unsigned char* planes, int row, int col) {
+  const float x = tile_at<T, typename C::Wide>(planes, col, row);
+  float rest = 0.0f;
+#pragma unroll
+  for (int p = C::NP - 1; p > 0; --p) rest += tile_at<T, typename C::Wide>(planes + p * C::kPlane, col, row);
+  return isfinite(x) ? x + rest : x;
+}
+// Sum of the products of two rows' channels; the four lanes of a row (g) take a quarter each.
+template <int D, typename A, typename B>
+__device__ __forceinline__ float row_dot(int g, A a, B b) {
+  float sum = 0.0f;
+#pragma unroll 2
+  for (int c = D / 4 * g; c < D / 4 * (g + 1); ++c) sum = fmaf(a(c), b(c), sum);
+  sum += __shfl_xor(sum, 16);
+  return sum + __shfl_xor(sum, 32);
+}
+
 // The record slot of the first unit of a packed sequence that starts at row c: slots
 // of different sequences never meet (the next starts at least ceil(len / unit) later),
 // and no prefix sum over the lengths is needed.  The last slot is below T / unit + N.
