@@ -199,11 +199,16 @@ __device__ __forceinline__ void walk_again(T* out, const T* q, int own, int live
                                            const unsigned char* ldsK, const unsigned char* ldsV,
                                            const unsigned char* ldsS, const Decay& lam, float scale) {
   using C = WalkSizes<T, D, Back>;
-  if (own >= live) return;  // not stored
   own = fresh(own);  // (what is worked out from them stays in here)
   g = fresh(g);
   q += own * D;
   out += own * D;
+  const int lane = threadIdx.x & 63;
+  const uint64_t bad = __ballot(row_watch<T, D>(C::kRow / 16, [&](int u) {
+    return reinterpret_cast<const T*>(ldsK + C::Wide::unit_at(lane, u));
+  }) != 0.0f);
+  // rows that are not stored; those whose scores are not finite, and so none of their channels
+  if (own >= live || (bad & ((2ull << own) - 1)) != 0 || !shared_row_finite<T, D>(q, g)) return;
 #pragma unroll 1
   for (int o = 0; o < C::OB; ++o) {
     const int e = 16 * o + 4 * g;
@@ -216,6 +221,11 @@ __device__ __forceinline__ void walk_again(T* out, const T* q, int own, int live
       for (int r = 0; r < 4; ++r) sum[r] = fmaf(x, plane_at<T, C>(ldsS, c, e + r), sum[r]);
     }
     sum *= scale * lam(own + 1);
+#pragma unroll 1
+    for (int s = 0; s <= own; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum[r] = fmaf(tile_at<T, typename C::Slim>(ldsV, s, e + r), 0.0f, sum[r]);
+    if (__ballot(wanted4(out + e, sum)) == 0) continue;
 #pragma unroll 1
     for (int s = 0; s <= own; ++s) {
       const float x = row_dot<D>(

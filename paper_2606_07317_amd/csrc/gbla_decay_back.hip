@@ -55,9 +55,20 @@ template <typename T, int D>
 __device__ __forceinline__ void keys_again(const Rows<T>& a, int64_t at, int own, int live, int g,
                                            int eh, const unsigned char* ldsD, const Decay& lam) {
   using C = KeysSizes<T, D>;
-  if (own >= live) return;  // not stored
   own = fresh(own);  // (what is worked out from them stays in here)
   g = fresh(g);
+  const int lane = threadIdx.x & 63;
+  uint64_t bad[2] = {0, 0};  // tokens with a row of q, of dout that is not finite
+#pragma unroll 1
+  for (int gi = 0; gi < a.group; ++gi)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const T* row = (i ? a.dout : a.q) + at + gi * a.head + min(lane, live - 1) * D;
+      bad[i] |= __ballot(row_watch<T, D>(D * C::ES / 16, [&](int u) {
+        return row + u * RowPieces<T, D>::kPer;
+      }) != 0.0f);
+    }
+  if (own >= live) return;  // not stored
   // Both gradients by the same code: dv = sum (q k) do + D^T k, dk = sum (do v) q + D v.
 #pragma unroll 1
   for (int i = 0; i < 2 * C::OB; ++i) {
@@ -68,6 +79,8 @@ __device__ __forceinline__ void keys_again(const Rows<T>& a, int64_t at, int own
     const int e = 16 * (eh * C::OB + (values ? i : i - C::OB)) + 4 * g;
     T* to = (values ? a.dv : a.dk) + at + own * D + e;
     if (__ballot(!finite4(to)) == 0) continue;
+    // scores that are not finite, and so no channel
+    if ((values ? bad[0] : bad[1]) >> own != 0 || !shared_row_finite<T, D>(mine, g)) continue;
     f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int c = 0; c < D; ++c) {
@@ -77,6 +90,13 @@ __device__ __forceinline__ void keys_again(const Rows<T>& a, int64_t at, int own
         sum[r] = fmaf(x, plane_at<T, C>(ldsD, values ? c : e + r, values ? e + r : c), sum[r]);
     }
     sum *= lam(live - 1 - own);
+#pragma unroll 1
+    for (int gi = 0; gi < a.group; ++gi)
+#pragma unroll 1
+      for (int t = own; t < live; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] = fmaf(widen1(right[gi * a.head + t * D + e + r]), 0.0f, sum[r]);
+    if (__ballot(wanted4(to, sum)) == 0) continue;
 #pragma unroll 1
     for (int gi = 0; gi < a.group; ++gi) {
 #pragma unroll 1

@@ -471,10 +471,9 @@ __device__ __forceinline__ void add_scored(f32x4_t* acc, const f32x4_t& a, const
 
 // Products with an infinite or NaN row of a tile give NaN to tokens that the row has no part
 // in, since a pair of the wrong order enters as 0 times the row.  Results that are not finite
-// are therefore formed again, pair by pair, and take what the recurrence gives; the others
+// though all that takes part in them is are therefore formed again, pair by pair; the others
 // stay.  What follows serves that: single elements, in loops that hold few registers, which
-// only such inputs reach (a tile then takes some tens of microseconds).  Looking for them
-// costs 0 to 2 % of a forward and none of a backward.
+// only such inputs reach.  Looking for them costs 0 to 2 % of a forward and none of a backward.
 
 // z stays 0 while all of x is finite, and is NaN from then on.
 template <int N>
@@ -527,6 +526,69 @@ __device__ __forceinline__ float row_dot(int g, A a, B b) {
   for (int c = D / 4 * g; c < D / 4 * (g + 1); ++c) sum = fmaf(a(c), b(c), sum);
   sum += __shfl_xor(sum, 16);
   return sum + __shfl_xor(sum, 32);
+}
+
+// Rows a lane at 16 bytes: a wave holds kRows of them.
+template <typename T, int D>
+struct RowPieces {
+  static constexpr int kPer = 16 / (int)sizeof(T), kLanes = D / kPer, kRows = 64 / kLanes;
+  using Piece = float[kPer];
+  static __device__ __forceinline__ void load(Piece x, const T* p) {
+    const u32x4_t v = load16(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) x[2 * i] = bf16_lo(v[i]), x[2 * i + 1] = bf16_hi(v[i]);
+      else x[i] = __uint_as_float(v[i]);
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, const Piece x) {
+    u32x4_t v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) v[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+      else v[i] = __float_as_uint(x[i]);
+    }
+    *reinterpret_cast<u32x4_t*>(p) = v;
+  }
+  static __device__ __forceinline__ float dot(const Piece a, const Piece b) {
+    float x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x = fmaf(a[i], b[i], x);
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) x += __shfl_xor(x, o);
+    return x;
+  }
+};
+
+// 0 if `count` pieces of 16 bytes of a row are finite, else NaN; at(u): where piece u lies.
+template <typename T, int D, typename At>
+__device__ __forceinline__ float row_watch(int count, At at) {
+  float z = 0.0f;
+#pragma unroll 1
+  for (int u = 0; u < count; ++u) {
+    typename RowPieces<T, D>::Piece x;
+    RowPieces<T, D>::load(x, at(u));
+#pragma unroll
+    for (int i = 0; i < RowPieces<T, D>::kPer; ++i) z = fmaf(x[i], 0.0f, z);
+  }
+  return z;
+}
+// The same for a row in memory that four lanes (g) share.
+template <typename T, int D>
+__device__ __forceinline__ bool shared_row_finite(const T* row, int g) {
+  float z = row_watch<T, D>(RowPieces<T, D>::kLanes / 4,
+                            [&](int u) { return row + D / 4 * g + u * RowPieces<T, D>::kPer; });
+  z += __shfl_xor(z, 16);
+  return z + __shfl_xor(z, 32) == 0.0f;
+}
+// Whether four values (stored at p) are to be formed again: not finite, though what takes part
+// in them (watched by z) is.
+template <typename T>
+__device__ __forceinline__ bool wanted4(const T* p, const f32x4_t& z) {
+  bool any = false;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) any |= !isfinite(widen1(p[r])) && isfinite(z[r]);
+  return any;
 }
 
 // The record slot of the first unit of a packed sequence that starts at row c: slots
