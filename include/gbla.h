@@ -394,7 +394,8 @@ size_t gbla_decay_backward_workspace_bytes(const gbla_decay_shape* shape);
  *   S_t = exp(g) S_{t-1} + k_t v_t^T,    o_t = scale * S_t^T q_t
  * computed in chunks.  S starts from initial_state (zeros if NULL).
  *   q [B,H,n,d] or [H,T,d]; k, v [B,K,n,d] or [K,T,d]; log_decay [K] fp32,
- *   g <= 0 (-inf: no memory, o_t = scale (q_t k_t) v_t)
+ *   g <= 0 (-inf, or so low that exp(g) is 0 in fp32: no memory, o_t = scale
+ *   (q_t k_t) v_t, whatever the states and the other tokens hold)
  *   initial_state  fp32 [N,K,d,d] ([c][e]: key channel, value channel) or NULL
  *   out            [B,H,n,d] or [H,T,d]
  *   final_state    fp32 [N,K,d,d] or NULL (not wanted); may be initial_state.
@@ -414,7 +415,8 @@ gbla_status gbla_decay_forward(const gbla_decay_shape* shape, const void* q, con
  *   dout            like q            dfinal_state  fp32 [N,K,d,d] or NULL (zeros)
  *   dq              like q            dk, dv        like k, v (summed over the
  *                                     query heads that share them)
- *   dlog_decay      fp32 [K], summed over the batch, or NULL (not wanted)
+ *   dlog_decay      fp32 [K], summed over the batch, or NULL (not wanted); 0 for a
+ *                   head without memory
  *   dinitial_state  fp32 [N,K,d,d] or NULL (not wanted); may be dfinal_state
  * Gradients are sums in fp32 of products with fp32's accuracy for both types, rounded
  * once to their type.  Reductions run in an order fixed by the shape: repeated calls

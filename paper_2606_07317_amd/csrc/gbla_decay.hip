@@ -239,6 +239,53 @@ __device__ __forceinline__ void walk_again(T* out, const T* q, int own, int live
   }
 }
 
+// The walk of a head whose decay is 0: o_t = scale (q_t k_t) v_t, and the last token's k v^T as
+// the final state.  By itself, so that 0 times a state's infinities never arises.
+// final_state: the pair's, where the span has to write it.
+template <typename T, int D, int VD>
+__device__ __forceinline__ void walk_forgetful(const DecayPlan& P, const Span& sp, const T* q,
+                                               const T* k, const T* v, int e0, const float* init,
+                                               T* out, float* final_state) {
+  using R = RowPieces<T, D>;
+  constexpr int U = 2;  // tokens of a lane at once
+  const int c0 = (threadIdx.x % R::kLanes) * R::kPer, rows = blockDim.x / R::kLanes;
+  const bool mine = c0 >= e0 && c0 < e0 + VD;
+  // (the bound by the workgroup's first token: the lanes of a row add up their products)
+  for (int t0 = sp.begin; t0 < sp.end; t0 += U * rows) {
+    typename R::Piece kk[U], vv[U];
+    int64_t at[U];
+    bool live[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * rows + (int)threadIdx.x / R::kLanes;
+      live[u] = t < sp.end;
+      at[u] = (int64_t)min(t, sp.end - 1) * D + c0;
+      R::load(kk[u], k + at[u]);
+      R::load(vv[u], v + at[u]);
+    }
+    for (int gi = 0; gi < P.group; ++gi) {
+      const int64_t head = (int64_t)gi * P.rows * D;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        typename R::Piece x;
+        R::load(x, q + head + at[u]);
+        const float p = P.scale * R::dot(x, kk[u]);
+#pragma unroll
+        for (int i = 0; i < R::kPer; ++i) x[i] = p * vv[u][i];
+        if (live[u] && mine) R::store(out + head + at[u], x);
+      }
+    }
+  }
+  if (!final_state) return;
+  for (int i = threadIdx.x; i < D * VD; i += blockDim.x) {
+    const int c = i / VD, e = e0 + i % VD;
+    const int64_t last = (int64_t)(sp.len - 1) * D;
+    final_state[c * D + e] = sp.len > 0 ? widen1(k[last + c]) * widen1(v[last + e])
+                             : init     ? init[c * D + e]
+                                        : 0.0f;
+  }
+}
+
 // The walk.  q, out: `heads` heads, k, v: `kv_heads`.  The state before the unit
 // comes from rec (split) or S0 (single; transposed [e][c] for the gradient of q).
 // final_state: written by the sequence's last unit.  Back (the gradient of q): the
@@ -308,6 +355,12 @@ walk_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
       fetch_q(sp.begin, 0);
     }
     const Decay lam(log_decay[h]);
+    if (lam.forgets()) {
+      walk_forgetful<T, D, C::VD>(P, sp, q + qrow0 * D, k + krow0 * D, v + krow0 * D, e0, init, out + qrow0 * D,
+                                  final_state && sp.last ? final_state + pair * (D * D) : nullptr);
+      if (Back && dg && lane == 0) dg[(((int64_t)h * P.grid_units + unit) * halves + e0 / C::VD) * C::NW + w] = 0.0;
+      return;
+    }
     const float full = lam(kTile);
     const float into = P.scale * lam(16 * tw + n + 1);
     Scores<true> scores;

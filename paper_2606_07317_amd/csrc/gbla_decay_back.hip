@@ -113,6 +113,54 @@ __device__ __forceinline__ void keys_again(const Rows<T>& a, int64_t at, int own
   }
 }
 
+// The gradients of a head whose decay is 0: dv_t = scale (q_t k_t) do_t and dk_t = scale
+// (do_t v_t) q_t, and what the final state's gradient D gives the last token.
+// dS0: the pair's, where the span has to write it; it may be D.
+template <typename T, int D>
+__device__ __forceinline__ void keys_forgetful(const DecayPlan& P, const Span& sp, const Rows<T>& a,
+                                               float* dS0) {
+  using R = RowPieces<T, D>;
+  const int c0 = (threadIdx.x % R::kLanes) * R::kPer, rows = blockDim.x / R::kLanes;
+  const int last = sp.len - 1 - sp.begin;
+  for (int t0 = 0; t0 < a.tokens; t0 += rows) {
+    const int t = t0 + (int)threadIdx.x / R::kLanes;
+    const int64_t at = (int64_t)min(t, a.tokens - 1) * D;
+    typename R::Piece k, v, sk, sv;
+    R::load(k, a.k + at + c0);
+    R::load(v, a.v + at + c0);
+#pragma unroll
+    for (int i = 0; i < R::kPer; ++i) sk[i] = sv[i] = 0.0f;
+    if (t == last && a.init) {
+      for (int e = 0; e < D; ++e) {
+        const float x = widen1(a.v[at + e]), y = widen1(a.k[at + e]);
+#pragma unroll
+        for (int i = 0; i < R::kPer; ++i) {
+          sk[i] = fmaf(a.init[(c0 + i) * D + e], x, sk[i]);
+          sv[i] = fmaf(a.init[e * D + c0 + i], y, sv[i]);
+        }
+      }
+    }
+    for (int gi = 0; gi < a.group; ++gi) {
+      typename R::Piece q, o;
+      R::load(q, a.q + at + gi * a.head + c0);
+      R::load(o, a.dout + at + gi * a.head + c0);
+      const float x = a.scale * R::dot(q, k), y = a.scale * R::dot(o, v);
+#pragma unroll
+      for (int i = 0; i < R::kPer; ++i) {
+        sv[i] = fmaf(x, o[i], sv[i]);
+        sk[i] = fmaf(y, q[i], sk[i]);
+      }
+    }
+    if (t < a.tokens) {
+      R::store(a.dk + at + c0, sk);
+      R::store(a.dv + at + c0, sv);
+    }
+  }
+  __syncthreads();  // D has been read
+  if (dS0)
+    for (int i = threadIdx.x; i < D * D; i += blockDim.x) dS0[i] = sp.len == 0 && a.init ? a.init[i] : 0.0f;
+}
+
 // Shared: several query heads to a key head.
 // Measured: bf16, B = 8, n = 2048, H = 16, d = 64 62 us (201 MB, 3.2 TB/s); 16 packed
 // sequences, T = 57,511, H = 8, d = 128 360 us, one workgroup a CU by its LDS, matrix
@@ -147,6 +195,18 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
       init = dfinal || !sp.last ? recD + at : nullptr;
       kept = recS + at;
     }
+    const int64_t krow0 = first_row(P, sp, P.kv_heads, h), qrow0 = first_row(P, sp, P.heads, h * P.group);
+    {
+      const int64_t ka = (krow0 + sp.begin) * D, qa = (qrow0 + sp.begin) * D;
+      const Rows<T> a = {init, q + qa, dout + qa, k + ka, v + ka, dk + ka, dv + ka,
+                         (int64_t)P.rows * D, P.group, sp.end - sp.begin, P.scale};
+      if (Decay(log_decay[h]).forgets()) {
+        keys_forgetful<T, D>(P, sp, a, dS0 && sp.begin == 0 ? dS0 + pair * (D * D) : nullptr);
+        if (dg && lane == 0) dg[((int64_t)h * P.grid_units + blockIdx.x) * C::NW + w] = 0.0;
+        return;
+      }
+      if (threadIdx.x == 0) rows = a;
+    }
     State<T, C> S;
     if (init) S.load(init, false, 0, w, lane);
     else S.clear();
@@ -155,11 +215,6 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
     TileLoad<T, C, D> lq, lo;
     OwnRows<T, C> kf, vf;
     OwnPieces<T, C> kp;
-    const int64_t krow0 = first_row(P, sp, P.kv_heads, h), qrow0 = first_row(P, sp, P.heads, h * P.group);
-    if (threadIdx.x == 0)
-      rows = {init, q + (qrow0 + sp.begin) * D, dout + (qrow0 + sp.begin) * D, k + (krow0 + sp.begin) * D,
-              v + (krow0 + sp.begin) * D, dk + (krow0 + sp.begin) * D, dv + (krow0 + sp.begin) * D,
-              (int64_t)P.rows * D, P.group, sp.end - sp.begin, P.scale};
     auto fetch = [&](int t, int gi) {
       const int64_t row = (qrow0 + (int64_t)gi * P.rows + t) * D;
       const int live = t < sp.begin ? 0 : sp.end - t;

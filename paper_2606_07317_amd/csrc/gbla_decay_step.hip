@@ -35,6 +35,7 @@ step_kernel(int rows, int heads, int kv_heads, float scale, const T* q, const T*
   if (slot < 0 || slot >= slots) return;
   const Decay decay(log_decay[h]);
   const float lam = decay(1);
+  const bool forgets = decay.forgets();
   float* S = state + ((int64_t)slot * kv_heads + h) * (D * D) + e0 + e;
   f32x4_t s[N];
 #pragma unroll
@@ -62,7 +63,7 @@ step_kernel(int rows, int heads, int kv_heads, float scale, const T* q, const T*
       const int c = c0 + i * R;
       const float kx = c < D ? widen1(kk[c]) : 0.0f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[i][r] = fmaf(kx, vx[r], lam * s[i][r]);
+      for (int r = 0; r < 4; ++r) s[i][r] = fmaf(kx, vx[r], forgets ? 0.0f : lam * s[i][r]);
     }
     for (int g0 = 0; g0 < group; g0 += kGroup) {
       f32x4_t acc[kGroup];

@@ -145,6 +145,10 @@ struct Decay {
     hi = g * l2;
     lo = fmaf(g, l2, -hi) + g * l2lo;
   }
+  // exp(g) is 0: no state goes on, whatever it holds (wave-uniform).
+  __device__ __forceinline__ bool forgets() const {
+    return __builtin_amdgcn_readfirstlane(__float_as_int((*this)(1))) == 0;
+  }
   __device__ __forceinline__ float operator()(int n) const {
     const float f = (float)n, x = f * hi;
     const float r = fmaf(f, hi, -x) + f * lo;
@@ -489,6 +493,11 @@ __device__ __forceinline__ float widen1(T x) {
   if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x << 16);
   else return x;
 }
+template <typename T>
+__device__ __forceinline__ T narrow1(float x) {
+  if constexpr (sizeof(T) == 2) return (T)(pack_bf16x2(x, 0.0f) & 0xffffu);
+  else return x;
+}
 // The four values that this lane has stored at p: all finite?  y where one is not.
 template <typename T>
 __device__ __forceinline__ bool finite4(const T* p) {
@@ -497,11 +506,8 @@ __device__ __forceinline__ bool finite4(const T* p) {
 template <typename T>
 __device__ __forceinline__ void mend4(T* p, const f32x4_t& y) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (isfinite(widen1(p[r]))) continue;
-    if constexpr (sizeof(T) == 2) p[r] = (T)(pack_bf16x2(y[r], 0.0f) & 0xffffu);
-    else p[r] = y[r];
-  }
+  for (int r = 0; r < 4; ++r)
+    if (!isfinite(widen1(p[r]))) p[r] = narrow1<T>(y[r]);
 }
 // Channel c of row r of a tile in LDS.
 template <typename T, typename L>
@@ -528,7 +534,7 @@ __device__ __forceinline__ float row_dot(int g, A a, B b) {
   return sum + __shfl_xor(sum, 32);
 }
 
-// Rows a lane at 16 bytes: a wave holds kRows of them.
+// Rows a lane at 16 bytes: a wave holds kRows of them.  For the heads without memory.
 template <typename T, int D>
 struct RowPieces {
   static constexpr int kPer = 16 / (int)sizeof(T), kLanes = D / kPer, kRows = 64 / kLanes;

@@ -171,3 +171,67 @@ def test_decay_backward_in_place_where_rows_are_formed_again(dtype, n):
     b = gbla.decay_attention_backward(*args, initial_state=S0, dfinal_state=dS, grads=dict(dinitial_state=dS))
     for name in a:
         assert torch.equal(torch.nan_to_num(a[name]), torch.nan_to_num(b[name])), name
+
+
+# ---------------------------------------------------------------------------
+# A decay of 0: tokens and states have no part in anything after them.
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("value", [None, INF, NAN])
+@pytest.mark.parametrize("g", [-INF, -200.0])
+@pytest.mark.parametrize("case", DECAY, ids=_IDS)
+def test_decay_of_zero_forgets(case, g, value):
+    """One head without memory (the last) beside ones with: its results are each token's own."""
+    lengths, ragged, H, K, d, dtype = case
+    where = [("v", 20, 5), ("k", 21, 6), ("q", 22, 7), ("dout", 23, 8), ("S0", 0, 3), ("dS", 0, 9)]
+    t = _case(*case)
+    t, clean = _bad(t, lengths, ragged, where, value) if value is not None else (t, t)
+    log_decay = t["g"].clone()
+    log_decay[-1] = g
+    dev = lambda x: None if x is None else x.cuda()
+    args = [dev(x) for x in (t["q"], t["k"], t["v"], log_decay)]
+    how = dict(initial_state=dev(t["S0"]), cu_seqlens=dev(t["cu"]))
+    out, S = gbla.decay_attention(*args, final_state=True, **how)
+    got = gbla.decay_attention_backward(*args, dev(t["dout"]), dfinal_state=dev(t["dS"]), **how)
+    scale, G = d ** -0.5, H // K
+    outs = [_pieces(x, lengths, ragged) for x in (t["q"], t["k"], t["v"], t["dout"], out, got["dq"], got["dk"], got["dv"])]
+    cleans = [_pieces(clean[n], lengths, ragged) for n in ("q", "k", "v", "dout")]
+    for s, ((q, k, v, do, y, dq, dk, dv), z) in enumerate(zip(zip(*outs), zip(*cleans))):
+        def own(q, k, v, do, dS, S0):
+            q, do, k, v = q[-G:].double(), do[-G:].double(), k[-1].double(), v[-1].double()
+            a, b = scale * (q * k).sum(-1, keepdim=True), scale * (do * v).sum(-1, keepdim=True)
+            gk, gv = (b * q).sum(0), (a * do).sum(0)
+            if len(k):
+                gk[-1] += dS.double() @ v[-1]
+                gv[-1] += dS.double().T @ k[-1]
+            final = k[-1][:, None] * v[-1] if len(k) else S0.double()
+            return a * v, b * k, gk, gv, final, torch.zeros(d, d).double() if len(k) else dS.double()
+        want = own(q, k, v, do, t["dS"][s, -1], t["S0"][s, -1])
+        plain = own(*z, clean["dS"][s, -1], clean["S0"][s, -1])
+        size = own(*(x.abs() for x in z), clean["dS"][s, -1].abs(), clean["S0"][s, -1].abs())
+        c = (2 * d + 144) * 2 * U
+        for i, (name, x) in enumerate((("out", y[-G:]), ("dq", dq[-G:]), ("dk", dk[-1]), ("dv", dv[-1]),
+                                       ("final_state", S[s, -1]), ("dinitial_state", got["dinitial_state"][s, -1]))):
+            _same_places(x, want[i], plain[i], size[i], c, name)
+    assert got["dlog_decay"][-1] == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("g", [-INF, -200.0])
+def test_step_with_a_decay_of_zero_forgets(g, d, dtype):
+    gen = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn(3, h, d, generator=gen).to(dtype) for h in (4, 2, 2))
+    state = torch.randn(2, 2, d, d, generator=gen)
+    state[1] = INF
+    state[0, 1, 2] = NAN
+    S = state.cuda()
+    out = gbla.decay_step(q.cuda(), k.cuda(), v.cuda(), torch.tensor([g, g]).cuda(), S,
+                          state_indices=torch.tensor([1, 0, 1], dtype=torch.int32).cuda())
+    x = (q.double().view(3, 2, 2, d) * k.double()[:, :, None]).sum(-1, keepdim=True) * d ** -0.5
+    want = (x * v.double()[:, :, None]).view(3, 4, d)
+    size = ((q.double().view(3, 2, 2, d) * k.double()[:, :, None]).abs().sum(-1, keepdim=True)
+            * d ** -0.5 * v.double()[:, :, None].abs()).view(3, 4, d)
+    _same_places(out, want, want, size, (d + 8) * 2 * U, "out")
+    for slot, n in ((0, 1), (1, 2)):
+        final = k[n].double()[:, :, None] * v[n].double()[:, None]
+        _same_places(S[slot], final, final, final.abs(), 8 * U, "state")
