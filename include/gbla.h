@@ -355,8 +355,11 @@ gbla_status gbla_qk_norm_rope(const gbla_rope_shape* shape, const void* q, const
                               const float* q_w, const float* k_w, const int32_t* positions,
                               const int32_t* cu_seqlens, void* q_out, void* k_out, void* stream);
 
-/* Scratch bytes of gbla_qk_norm_rope_backward; 0 if the shape is not accepted. */
+/* Scratch bytes of gbla_qk_norm_rope_backward; 0 if the shape is not accepted.  The second
+ * is what the ragged reading alone needs: the first covers B * seqlen tokens too, which for
+ * a packed batch of many sequences is many times as much. */
 size_t gbla_qk_norm_rope_backward_workspace_bytes(const gbla_rope_shape* shape);
+size_t gbla_qk_norm_rope_backward_ragged_workspace_bytes(const gbla_rope_shape* shape);
 
 /*
  * Gradients of L = sum(q_out * dq_out) + sum(k_out * dk_out):
@@ -388,6 +391,10 @@ typedef struct {
  * dense and the ragged reading, for every max_seqlen); 0 if neither is accepted. */
 size_t gbla_decay_workspace_bytes(const gbla_decay_shape* shape);
 size_t gbla_decay_backward_workspace_bytes(const gbla_decay_shape* shape);
+/* What the ragged reading alone needs (see gbla_qk_norm_rope_backward_ragged_workspace_bytes);
+ * 0 if it is not accepted. */
+size_t gbla_decay_ragged_workspace_bytes(const gbla_decay_shape* shape);
+size_t gbla_decay_backward_ragged_workspace_bytes(const gbla_decay_shape* shape);
 
 /*
  * Causal linear attention with a decay per key head, g = log_decay[h]:

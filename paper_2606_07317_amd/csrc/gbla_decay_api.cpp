@@ -36,15 +36,19 @@ gbla_status scratch(const void* ws, size_t have, size_t need) {
   return have < need ? GBLA_ERR_WORKSPACE : GBLA_OK;
 }
 
-size_t decay_bytes(const gbla_decay_shape* shape, bool backward) {
-  size_t most = 0;
-  for (int ragged = 0; ragged < 2; ++ragged) {
-    gbla::DecayPlan p;
-    if (gbla::make_decay_plan(shape, ragged != 0, backward, &p) == GBLA_OK && p.total_bytes > most)
-      most = p.total_bytes;
-  }
-  return most;
+size_t decay_bytes(const gbla_decay_shape* shape, bool ragged, bool backward) {
+  gbla::DecayPlan p;
+  return gbla::make_decay_plan(shape, ragged, backward, &p) == GBLA_OK ? p.total_bytes : 0;
 }
+
+size_t rope_bytes(const gbla_rope_shape* shape, bool ragged) {
+  gbla::RopePlan p;
+  if (gbla::make_rope_plan(shape, ragged, true, &p) != GBLA_OK) return 0;
+  const size_t bytes = gbla::rope_partial_bytes(p);
+  return bytes < 256 ? 256 : bytes;
+}
+
+size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 
 #define GBLA_TRY(expr)                  \
   do {                                  \
@@ -69,15 +73,11 @@ gbla_status gbla_qk_norm_rope(const gbla_rope_shape* shape, const void* q, const
 }
 
 size_t gbla_qk_norm_rope_backward_workspace_bytes(const gbla_rope_shape* shape) {
-  size_t most = 0;
-  for (int ragged = 0; ragged < 2; ++ragged) {
-    gbla::RopePlan p;
-    if (gbla::make_rope_plan(shape, ragged != 0, true, &p) != GBLA_OK) continue;
-    size_t bytes = gbla::rope_partial_bytes(p);
-    if (bytes < 256) bytes = 256;
-    if (bytes > most) most = bytes;
-  }
-  return most;
+  return larger(rope_bytes(shape, false), rope_bytes(shape, true));
+}
+
+size_t gbla_qk_norm_rope_backward_ragged_workspace_bytes(const gbla_rope_shape* shape) {
+  return rope_bytes(shape, true);
 }
 
 gbla_status gbla_qk_norm_rope_backward(const gbla_rope_shape* shape, const void* q, const void* k,
@@ -98,11 +98,19 @@ gbla_status gbla_qk_norm_rope_backward(const gbla_rope_shape* shape, const void*
 }
 
 size_t gbla_decay_workspace_bytes(const gbla_decay_shape* shape) {
-  return decay_bytes(shape, false);
+  return larger(decay_bytes(shape, false, false), decay_bytes(shape, true, false));
 }
 
 size_t gbla_decay_backward_workspace_bytes(const gbla_decay_shape* shape) {
-  return decay_bytes(shape, true);
+  return larger(decay_bytes(shape, false, true), decay_bytes(shape, true, true));
+}
+
+size_t gbla_decay_ragged_workspace_bytes(const gbla_decay_shape* shape) {
+  return decay_bytes(shape, true, false);
+}
+
+size_t gbla_decay_backward_ragged_workspace_bytes(const gbla_decay_shape* shape) {
+  return decay_bytes(shape, true, true);
 }
 
 gbla_status gbla_decay_forward(const gbla_decay_shape* shape, const void* q, const void* k,

@@ -111,14 +111,16 @@ def load_library(path: str = LIB_PATH):
     RP, DP = ctypes.POINTER(RopeShape), ctypes.POINTER(DecayShape)
     lib.gbla_qk_norm_rope.argtypes = [RP] + [P] * 9
     lib.gbla_qk_norm_rope.restype = ctypes.c_int
-    lib.gbla_qk_norm_rope_backward_workspace_bytes.argtypes = [RP]
-    lib.gbla_qk_norm_rope_backward_workspace_bytes.restype = sz
+    for name in ("gbla_qk_norm_rope_backward_workspace_bytes",
+                 "gbla_qk_norm_rope_backward_ragged_workspace_bytes"):
+        getattr(lib, name).argtypes = [RP]
+        getattr(lib, name).restype = sz
     lib.gbla_qk_norm_rope_backward.argtypes = [RP] + [P] * 9 + [sz] + [P] * 5
     lib.gbla_qk_norm_rope_backward.restype = ctypes.c_int
-    lib.gbla_decay_workspace_bytes.argtypes = [DP]
-    lib.gbla_decay_workspace_bytes.restype = sz
-    lib.gbla_decay_backward_workspace_bytes.argtypes = [DP]
-    lib.gbla_decay_backward_workspace_bytes.restype = sz
+    for name in ("gbla_decay_workspace_bytes", "gbla_decay_backward_workspace_bytes",
+                 "gbla_decay_ragged_workspace_bytes", "gbla_decay_backward_ragged_workspace_bytes"):
+        getattr(lib, name).argtypes = [DP]
+        getattr(lib, name).restype = sz
     lib.gbla_decay_forward.argtypes = [DP] + [P] * 7 + [sz] + [P] * 3
     lib.gbla_decay_forward.restype = ctypes.c_int
     lib.gbla_decay_backward.argtypes = [DP] + [P] * 9 + [sz] + [P] * 6
@@ -639,11 +641,17 @@ def qk_norm_rope(q, k, q_w, k_w, positions=None, cu_seqlens=None, rotary_dim=Non
     return q_out, k_out
 
 
-def qk_norm_rope_backward_workspace_bytes(shape: RopeShape) -> int:
-    n = load_library().gbla_qk_norm_rope_backward_workspace_bytes(ctypes.byref(shape))
+def _scratch(name: str, shape, ragged: bool) -> int:
+    name += "_ragged_workspace_bytes" if ragged else "_workspace_bytes"
+    n = getattr(load_library(), name)(ctypes.byref(shape))
     if n == 0:
-        raise GblaError(1, "gbla_qk_norm_rope_backward_workspace_bytes")
+        raise GblaError(1, name)
     return int(n)
+
+
+def qk_norm_rope_backward_workspace_bytes(shape: RopeShape, ragged: bool = False) -> int:
+    """``ragged``: for calls with cu_seqlens only, which take (much) less than both readings."""
+    return _scratch("gbla_qk_norm_rope_backward", shape, ragged)
 
 
 def qk_norm_rope_backward(q, k, q_w, k_w, dq_out, dk_out, positions=None, cu_seqlens=None,
@@ -659,7 +667,7 @@ def qk_norm_rope_backward(q, k, q_w, k_w, dq_out, dk_out, positions=None, cu_seq
     dev = q.device
     _want(dq_out, "dq_out", q.shape, q.dtype, dev)
     _want(dk_out, "dk_out", k.shape, q.dtype, dev)
-    need = qk_norm_rope_backward_workspace_bytes(shape)
+    need = qk_norm_rope_backward_workspace_bytes(shape, cu_seqlens is not None)
     g = dict(grads or {})
     with _on(dev, stream):
         if workspace is None:
@@ -688,18 +696,13 @@ def decay_shape(q, k, scale: Optional[float] = None, cu_seqlens=None, max_seqlen
                       float(d) ** -0.5 if scale is None else float(scale))
 
 
-def decay_workspace_bytes(shape: DecayShape) -> int:
-    n = load_library().gbla_decay_workspace_bytes(ctypes.byref(shape))
-    if n == 0:
-        raise GblaError(1, "gbla_decay_workspace_bytes")
-    return int(n)
+def decay_workspace_bytes(shape: DecayShape, ragged: bool = False) -> int:
+    """``ragged``: for calls with cu_seqlens only, which take (much) less than both readings."""
+    return _scratch("gbla_decay", shape, ragged)
 
 
-def decay_backward_workspace_bytes(shape: DecayShape) -> int:
-    n = load_library().gbla_decay_backward_workspace_bytes(ctypes.byref(shape))
-    if n == 0:
-        raise GblaError(1, "gbla_decay_backward_workspace_bytes")
-    return int(n)
+def decay_backward_workspace_bytes(shape: DecayShape, ragged: bool = False) -> int:
+    return _scratch("gbla_decay_backward", shape, ragged)
 
 
 def _check_decay(q, k, v, log_decay, shape, states):
@@ -726,7 +729,7 @@ def decay_attention(q, k, v, log_decay, scale: Optional[float] = None, initial_s
     given = final_state if isinstance(final_state, torch.Tensor) else None
     _check_decay(q, k, v, log_decay, shape, ((initial_state, "initial_state"), (given, "final_state")))
     dev = q.device
-    need = decay_workspace_bytes(shape)
+    need = decay_workspace_bytes(shape, cu_seqlens is not None)
     with _on(dev, stream):
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
@@ -759,7 +762,7 @@ def decay_attention_backward(q, k, v, log_decay, dout, scale: Optional[float] = 
                   (g.get("dinitial_state"), "dinitial_state")))
     dev = q.device
     _want(dout, "dout", q.shape, q.dtype, dev)
-    need = decay_backward_workspace_bytes(shape)
+    need = decay_backward_workspace_bytes(shape, cu_seqlens is not None)
     with _on(dev, stream):
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
