@@ -33,8 +33,8 @@ using RecordSizes = DC<T, D, D, D == 128 ? 8 : 4, 1, false>;
 // a CU, so that one's matrix products meet the other's vector work.  (One of eight waves,
 // which the barriers keep in step: its time was the sum of the matrix, the vector and the
 // LDS work.)  In the forward two parts of the state and of the scores leave 2^-17 of a
-// term, below the bf16 rounding of the output that they form; a third costs 8 % of one
-// prompt (n = 32768, d = 64) and 26 % of the packed prompts (d = 128, shared heads).  Back,
+// term, below the bf16 rounding of the output that they form; a third costs 10 % of one
+// prompt (n = 32768, d = 64) and 21 % of the packed prompts (d = 128, shared heads).  Back,
 // the sums are gradients' and have fp32's accuracy, by three parts of both: the state's
 // products also form the decay's gradient, an fp32 sum of both signs (its error is 0.1e-6 ..
 // 0.5e-6 where two parts left 1e-6 .. 3e-6).
@@ -85,7 +85,7 @@ __device__ __forceinline__ void record_unit(const DecayPlan& P, const Span& sp, 
 }
 
 // Both sides of a backward (B = 8, n = 2048, H = 16, d = 64) 32 us, 134 MB, 4.2 TB/s: bound
-// by memory.  At d = 128 (16 sequences, T = 57,511, H = 8) 119 us, 4.0 TB/s, with matrix
+// by memory.  At d = 128 (16 sequences, T = 57,511, H = 8) 118 us, 4.0 TB/s, with matrix
 // instructions under way in 37 % of a SIMD's cycles.
 // blockIdx.z = 0: records of the state (k or v by v or k), 1 (backward): of its
 // gradient.
@@ -293,8 +293,8 @@ __device__ __forceinline__ void walk_forgetful(const DecayPlan& P, const Span& s
 // of the decay's gradient of the pairs whose earlier token lies before the tile,
 // with q the forward's queries in `other`.
 // Shared: several query heads to a key head.
-// Measured: bf16, B = 1, n = 32768, H = 8, d = 64 31 us (134 MB, 4.3 TB/s); 64 packed
-// sequences, T = 177,929, H = 8, K = 2, d = 128 363 us, where matrix instructions are
+// Measured: bf16, B = 1, n = 32768, H = 8, d = 64 32 us (134 MB, 4.2 TB/s); 64 packed
+// sequences, T = 177,929, H = 8, K = 2, d = 128 379 us, where matrix instructions are
 // under way in 35 % of a SIMD's cycles and LDS reads in 34 %: two waves a SIMD (the
 // registers allow no more) leave the two, the vector work and the barriers mostly one
 // after the other.  Half of the LDS reads (the state's blocks as operands from the

@@ -162,11 +162,12 @@ __device__ __forceinline__ void keys_forgetful(const DecayPlan& P, const Span& s
 }
 
 // Shared: several query heads to a key head.
-// Measured: bf16, B = 8, n = 2048, H = 16, d = 64 62 us (201 MB, 3.2 TB/s); 16 packed
-// sequences, T = 57,511, H = 8, d = 128 360 us, one workgroup a CU by its LDS, matrix
-// instructions under way in 26 % of a SIMD's cycles and LDS reads in 48 %.  A swizzled
-// layout halves that 48 % and takes as long: the work between two barriers is a chain of
-// products, decays and splits that two waves a SIMD do not cover.
+// Measured: bf16, B = 8, n = 2048, H = 16, d = 64 68 us (201 MB, 3.0 TB/s); 16 packed
+// sequences, T = 57,511, H = 8, d = 128 398 us, one workgroup a CU by its LDS, matrix
+// instructions under way in 27 % of a SIMD's cycles and LDS reads in 47 % (half of that
+// conflicts, which the walk's swizzle would spare for registers that there are none of).
+// The work between two barriers is a chain of products, decays and splits that two waves a
+// SIMD do not cover.
 template <typename T, int D, bool Shared>
 __global__ void __launch_bounds__((KeysSizes<T, D>::NT), 2)
 keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_decay,
@@ -239,8 +240,9 @@ keys_kernel(DecayPlan P, const T* q, const T* k, const T* v, const float* log_de
     pw.fill(lam, P.scale);
 
     // The lane that LDS addresses are made from, anew for each phase of a step: they free
-    // registers, and a backward (B = 8, n = 2048, H = 16, d = 64) takes 134 us for 139.  At
-    // d = 128, where the walk waits for its own products anyway, it takes 719 for 712.
+    // registers, and a backward (B = 8, n = 2048, H = 16, d = 64) takes 141 us for 145.  At
+    // d = 128, where the walk waits for its own products anyway, it changes little (756 us for
+    // 764 of 16 packed sequences).
     auto place = [&] { return D < 128 ? fresh(lane) : lane; };
 
     for (int tile = tiles - 1; tile >= 0; --tile) {

@@ -18,11 +18,12 @@
 // Tiles in LDS: [token][D].  Two kinds of reads meet there: 16 rows of one 16-byte unit
 // (row_at) and columns (col_at; bf16 by transposed reads of four rows and two units a
 // group of 16 lanes).  The walk's bf16 rows store unit u at u ^ swizzle(r), so that the
-// rows that either reads at once fall on different banks (with rows 16 bytes apart, half
-// of its LDS cycles at d = 128 were conflicts: 239 us, 191 with the swizzle).  The other
+// rows that either reads at once fall on different banks (64 packed sequences, T = 177,929,
+// d = 128, shared heads: 407 us a forward, 419 with rows 16 bytes apart).  The other
 // kernels' rows are 16 bytes apart, since the swizzle's addresses cost registers that
-// they do not have (keys at d = 128 348 us, 466 with it; records 117, 141: one workgroup
-// a CU instead of two), and fp32 rows, whose reads of single values that suits.
+// they do not have (16 packed sequences, T = 57,511, d = 128: 764 us a backward, 903 with
+// swizzled keys, 782 with swizzled records), and fp32 rows, whose reads of single values
+// that suits.
 #pragma once
 
 #include <math.h>

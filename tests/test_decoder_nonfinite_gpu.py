@@ -235,3 +235,18 @@ def test_step_with_a_decay_of_zero_forgets(g, d, dtype):
     for slot, n in ((0, 1), (1, 2)):
         final = k[n].double()[:, :, None] * v[n].double()[:, None]
         _same_places(S[slot], final, final, final.abs(), 8 * U, "state")
+
+
+@pytest.mark.parametrize("where", [[("q", 20, 5)], [("dout", 20, 5)], [("dS", 0, 7)]], ids=lambda w: w[0][0])
+@pytest.mark.parametrize("case", DECAY, ids=_IDS)
+def test_decay_backward_without_the_decay_gradient_is_the_same(case, where):
+    """What calls for the second pass does not depend on whether the decay's gradient is wanted."""
+    t, _ = _bad(_case(*case), case[0], case[1], where, NAN)
+    dev = lambda x: None if x is None else x.cuda()
+    args = [dev(t[x]) for x in ("q", "k", "v", "g", "dout")]
+    how = dict(initial_state=dev(t["S0"]), dfinal_state=dev(t["dS"]), cu_seqlens=dev(t["cu"]))
+    a = gbla.decay_attention_backward(*args, **how)
+    b = gbla.decay_attention_backward(*args, decay_grad=False, **how)
+    for n in b:
+        assert torch.equal(torch.isnan(a[n]), torch.isnan(b[n])) and torch.equal(
+            torch.nan_to_num(a[n]), torch.nan_to_num(b[n])), n

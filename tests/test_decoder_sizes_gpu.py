@@ -255,3 +255,24 @@ def test_step_beyond_32_bit_offsets(dtype):
         _check(out[n], want[:, 0], size[:, 0], (d + 8) * 2 * U, "out")
         _check(state[s], final, size_S, 8 * U, "state")
     assert torch.equal(near, state[slots - 3])
+
+
+def test_prompt_into_slots_and_a_step_from_them():
+    """A prompt's final states written into neighbouring slots of a pool, which a step names."""
+    gen = _gen(6)
+    B, H, K, d, n = 3, 4, 2, 64, 150
+    q, k, v = (_randn(gen, B, h, n + 1, d, dtype=BF16) for h in (H, K, K))
+    g = torch.tensor([-0.01, -0.1])
+    pool = torch.full((8, K, d, d), 3.0, device="cuda")
+    cut = lambda x: x[:, :, :n].contiguous().cuda()
+    _, S = gbla.decay_attention(cut(q), cut(k), cut(v), g.cuda(), final_state=pool[2:5])
+    last = lambda x: x[:, :, n].contiguous().cuda()
+    out = gbla.decay_step(last(q), last(k), last(v), g.cuda(), pool,
+                          state_indices=torch.tensor([2, 3, 4], dtype=torch.int32).cuda())
+    assert S.data_ptr() == pool[2:5].data_ptr() and (pool[[0, 1, 5, 6, 7]] == 3.0).all()
+    for b in range(B):
+        want, final = ref.decay(q[b], k[b], v[b], g, d ** -0.5)
+        size, size_S = ref.decay_sizes(q[b], k[b], v[b], g, d ** -0.5)
+        c = (2 * d + 144 + n / 64 + 8) * 2 * U
+        _check(out[b], want[:, n], size[:, n], c, "out")
+        _check(pool[2 + b], final, size_S, c, "state")
