@@ -20,9 +20,9 @@ bool dtype_ok(int32_t t) { return t == GBLA_F32 || t == GBLA_BF16; }
 
 // Tokens of a unit (a power of two): short enough for two workgroups a CU, long enough
 // that the d x d record of a unit stays small beside its tokens.  Whole calls in us,
-// units of 256 / 512 / 1024: forward bf16 B = 1, n = 32768, H = 8, d = 64 63 / 53 / 58;
-// packed, 64 sequences, T = 177,929, d = 128, H = 8, K = 2 410 / 404 / -; backward B = 8, n =
-// 2048, H = 16, d = 64 158 / 141 / 139; 16 sequences, T = 57,511, H = 8, d = 128 793 / 691 / -.
+// units of 256 / 512 / 1024: forward bf16 B = 1, n = 32768, H = 8, d = 64 57 / 49 / 49;
+// packed, 64 sequences, T = 177,929, d = 128, H = 8, K = 2 405 / 406 / 405; backward B = 8, n =
+// 2048, H = 16, d = 64 165 / 141 / 140; 16 sequences, T = 57,511, H = 8, d = 128 880 / 762 / 761.
 int32_t unit_tokens(const DecayPlan& p) {
   int32_t unit = kMaxUnit;
   while (unit > 2 * kTile && p.tokens * p.kv_heads < (int64_t)unit * 512) unit /= 2;
@@ -35,24 +35,28 @@ int32_t unit_tokens(const DecayPlan& p) {
 //   longest (full - tokens of all pairs / longest) <= few,
 // `full` pairs filling the chip at any length and few / full tokens passing for short
 // whatever the pairs.  Single / split in us:
-//   forward bf16 d = 64: B K = 8 n = 257 11 / 13, 384 14 / 13, 1024 32 / 14; 32 n = 384 14 / 14;
-//   128 n = 768 26 / 29, 1024 34 / 33; 256 n = 4096 149 / 201.  d = 32: 8 n = 512 10 / 11, 768
-//   14 / 11; 128 n = 1024 19 / 19.  d = 128: 8 n = 257 17 / 19, 384 20 / 19; 32 n = 512 26 / 26;
-//   128 n = 2048 102 / 128.
-//   forward fp32 d = 32: 8 n = 257 13 / 14; 128 n = 512 20 / 20.  d = 64: 8 n = 192 17 / 20, 257
-//   26 / 20; 128 n = 384 34 / 36, 512 44 / 41.  d = 128: 8 n = 192 26 / 33, 257 43 / 35; 128 n =
-//   2048 275 / 373.
-//   backward bf16 d = 64: 8 n = 192 27 / 26; 128 n = 384 49 / 49; 256 n = 4096 463 / 544.  d = 32:
-//   8 n = 257 22 / 21; 128 n = 512 32 / 31.  d = 128: 32 n = 192 48 / 48; 128 n = 1024 207 / 207.
-//   backward fp32 d = 32: 8 n = 192 27 / 27; 128 n = 257 42 / 42.  d = 64: 8 n = 192 51 / 45; 128
-//   n = 257 84 / 85; 256 n = 2048 515 / 564.  d = 128: 8 n = 192 134 / 105; 128 n = 384 282 / 292.
+//   forward bf16 d = 64: B K = 8 n = 257 12 / 13, 384 14 / 13, 1024 32 / 14; 32 n = 384 14 / 14;
+//   128 n = 768 26 / 29, 1024 34 / 33; 256 n = 4096 152 / 187.  d = 32: 8 n = 512 11 / 11, 768
+//   15 / 11; 128 n = 1024 20 / 20.  d = 128: 8 n = 257 17 / 19, 384 20 / 19; 32 n = 512 27 / 25;
+//   128 n = 2048 102 / 132.
+//   forward fp32 d = 32: 2 n = 257 13 / 13, 320 14 / 13; 8 n = 257 14 / 13; 128 n = 512 22 / 21.
+//   d = 64: 8 n = 192 17 / 20, 257 26 / 20; 128 n = 384 35 / 37, 512 45 / 41.  d = 128: 8 n = 192
+//   26 / 33, 257 43 / 35; 128 n = 2048 293 / 375.
+//   backward bf16 d = 32: 8 n = 192 19 / 21, 257 25 / 22; 64 n = 192 19 / 22, 257 26 / 23; 128 n =
+//   384 30 / 31, 512 37 / 34; 192 n = 768 50 / 52, 1024 64 / 58; 256 n = 4096 234 / 242.  d = 64: 8
+//   n = 128 23 / 27, 192 31 / 29; 64 n = 192 32 / 33, 257 45 / 38; 128 n = 320 49 / 50, 384 56 / 51;
+//   192 n = 768 99 / 108, 1024 126 / 122; 256 n = 4096 499 / 560.  d = 128: 8 n = 128 37 / 41, 160
+//   52 / 47; 64 n = 192 56 / 61, 257 81 / 73; 128 n = 768 191 / 199, 1024 238 / 226; 192 n = 2048
+//   521 / 581.
+//   backward fp32 d = 32: 8 n = 192 29 / 28; 128 n = 257 44 / 44.  d = 64: 8 n = 192 52 / 46; 128
+//   n = 257 85 / 84; 256 n = 2048 495 / 553.  d = 128: 8 n = 192 131 / 105; 128 n = 384 279 / 297.
 bool walk_whole(const DecayPlan& p, int64_t longest, bool backward) {
   struct Rule {
     int32_t full, few;
   };
   static constexpr Rule rules[2][2][3] = {  // forward, backward; bf16, fp32; d = 32, 64, 128
       {{{272, 148000}, {192, 61000}, {72, 20000}}, {{262, 68000}, {233, 47000}, {128, 27000}}},
-      {{{226, 48000}, {245, 45000}, {150, 22500}}, {{256, 47000}, {256, 40000}, {190, 27000}}}};
+      {{{240, 45000}, {245, 43000}, {150, 21500}}, {{256, 47000}, {256, 40000}, {190, 27000}}}};
   const Rule r = rules[backward][p.dtype == GBLA_F32][p.d == 32 ? 0 : p.d == 64 ? 1 : 2];
   return longest * r.full - p.tokens * p.kv_heads <= r.few;
 }
