@@ -450,6 +450,76 @@ gbla_status gbla_decay_step(const gbla_decay_shape* shape, const void* q, const 
                             const void* v, const float* log_decay, const int32_t* state_indices,
                             int32_t slots, float* state, void* out, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The gated delta rule: causal linear attention whose state forgets by a decay of every
+ * token and is corrected towards the token's value where it is read with its key.  It
+ * shares the decoder's conventions above, with these differences:
+ * - q and k have H heads; v, the gates, the output and the states have V value heads,
+ *   a multiple of H: value head h reads query and key head h / (V / H).
+ * - A value that is not finite: in k, v, log_decay (-inf is allowed) or beta it makes the
+ *   outputs of its token and of all later ones of its sequence and value head NaN, and
+ *   their final state; in q, its own token's outputs.  Earlier tokens, other sequences and
+ *   other heads are not reached.  NaN in a state stays, whatever the decay.
+ * ---------------------------------------------------------------------------
+ */
+typedef struct {
+  int32_t batch;       /* B (dense), N_s (ragged) or rows (gbla_delta_step), >= 1  */
+  int32_t seqlen;      /* n (dense) or T (ragged), >= 0; 1 for gbla_delta_step    */
+  int32_t heads;       /* H >= 1: heads of q and k                               */
+  int32_t value_heads; /* V: heads of v, the gates, states and output; H divides V */
+  int32_t head_dim;    /* d in {32, 64, 128}, of keys and values                 */
+  int32_t max_seqlen;  /* ragged: an upper bound of the lengths (>= 0); dense: 0.
+                          It only chooses kernels                                */
+  int32_t dtype;       /* gbla_dtype of q, k, v, the output and their gradients  */
+  float scale;         /* factor of the output (finite), usually d^-1/2          */
+} gbla_delta_shape;
+
+/* Scratch bytes of gbla_delta_forward (the larger of the dense and the ragged reading, for
+ * every max_seqlen; the second: what the ragged reading alone needs); 0 if not accepted. */
+size_t gbla_delta_workspace_bytes(const gbla_delta_shape* shape);
+size_t gbla_delta_ragged_workspace_bytes(const gbla_delta_shape* shape);
+
+/*
+ * The gated delta rule, with g = log_decay and b = beta of token t and value head h:
+ *   u_t = b_t (v_t - exp(g_t) S_{t-1}^T k_t)
+ *   S_t = exp(g_t) S_{t-1} + k_t u_t^T,     o_t = scale * S_t^T q_t
+ * computed in chunks.  S starts from initial_state (zeros if NULL).
+ *   q, k [B,H,n,d] or [H,T,d]; v [B,V,n,d] or [V,T,d]
+ *   log_decay, beta  fp32 [B,V,n] or [V,T]; log_decay <= 0 (-inf: the past is forgotten).
+ *                    Keys of length one and beta within [0, 2] keep the state bounded;
+ *                    nothing is normalised here (gbla_qk_norm_rope with weights d^-1/2 and
+ *                    no rotation does).
+ *   initial_state    fp32 [N,V,d,d] ([c][e]: key channel, value channel) or NULL
+ *   out              like v
+ *   final_state      fp32 [N,V,d,d] or NULL (not wanted); may be initial_state.
+ *                    An empty sequence's is its initial state.
+ * States are sums in fp32.  In bf16 what is computed in fp32 enters the products in two
+ * bf16 parts, 2^-17 of a term; fp32 products are fp32 throughout.
+ */
+gbla_status gbla_delta_forward(const gbla_delta_shape* shape, const void* q, const void* k,
+                               const void* v, const float* log_decay, const float* beta,
+                               const float* initial_state, const int32_t* cu_seqlens,
+                               void* workspace, size_t workspace_bytes, void* out,
+                               float* final_state, void* stream);
+
+/*
+ * The same recurrence for one new token of each of shape->batch rows:
+ *   state[s] = exp(g) state[s];  u = b (v - state[s]^T k);  state[s] += k u^T;
+ *   out = scale * state[s]^T q
+ *   q, k [N,H,d]; v, out [N,V,d]; log_decay, beta fp32 [N,V]
+ *   state          fp32 [slots,V,d,d], updated in place
+ *   state_indices  int32 [N], the slot s of each row, or NULL: row n has slot n
+ *                  (slots >= N)
+ * Rows that name the same slot are applied in row order.  A row whose index is
+ * outside [0, slots) is skipped: no state changes and its output row is left.
+ * Values that are not finite go where these formulas take them.
+ */
+gbla_status gbla_delta_step(const gbla_delta_shape* shape, const void* q, const void* k,
+                            const void* v, const float* log_decay, const float* beta,
+                            const int32_t* state_indices, int32_t slots, float* state, void* out,
+                            void* stream);
+
 /* A static, human-readable name of a status code (never NULL). */
 const char* gbla_status_string(gbla_status status);
 

@@ -2,39 +2,11 @@
 // (include/gbla.h).  Every check runs on the host before anything is enqueued.
 #include <stdint.h>
 
-#include <initializer_list>
-
 #include "gbla.h"
+#include "gbla_checks.h"
 #include "gbla_decay.h"
 
 namespace {
-
-// Arrays in use: present, and aligned to `a` bytes.
-gbla_status present(std::initializer_list<const void*> ptrs, size_t a = 16) {
-  for (const void* p : ptrs) {
-    if (!p) return GBLA_ERR_INVALID_ARGUMENT;
-    if (!gbla::aligned(p, a)) return GBLA_ERR_MISALIGNED;
-  }
-  return GBLA_OK;
-}
-
-// Arrays over the tokens: of no elements, and so possibly NULL, where there are none.
-gbla_status rows_present(int64_t tokens, std::initializer_list<const void*> ptrs) {
-  return tokens > 0 ? present(ptrs) : GBLA_OK;
-}
-
-// Arrays that may be NULL.
-gbla_status optional(std::initializer_list<const void*> ptrs, size_t a = 16) {
-  for (const void* p : ptrs)
-    if (p && !gbla::aligned(p, a)) return GBLA_ERR_MISALIGNED;
-  return GBLA_OK;
-}
-
-gbla_status scratch(const void* ws, size_t have, size_t need) {
-  if (!ws) return GBLA_ERR_WORKSPACE;
-  if (!gbla::aligned(ws, 256)) return GBLA_ERR_MISALIGNED;
-  return have < need ? GBLA_ERR_WORKSPACE : GBLA_OK;
-}
 
 size_t decay_bytes(const gbla_decay_shape* shape, bool ragged, bool backward) {
   gbla::DecayPlan p;
@@ -48,15 +20,9 @@ size_t rope_bytes(const gbla_rope_shape* shape, bool ragged) {
   return bytes < 256 ? 256 : bytes;
 }
 
-size_t larger(size_t a, size_t b) { return a > b ? a : b; }
-
-#define GBLA_TRY(expr)                  \
-  do {                                  \
-    gbla_status _st = (expr);           \
-    if (_st != GBLA_OK) return _st;     \
-  } while (0)
-
 }  // namespace
+
+using namespace gbla::checks;
 
 extern "C" {
 

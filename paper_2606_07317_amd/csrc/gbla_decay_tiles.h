@@ -601,7 +601,8 @@ __device__ __forceinline__ bool wanted4(const T* p, const f32x4_t& z) {
 // The record slot of the first unit of a packed sequence that starts at row c: slots
 // of different sequences never meet (the next starts at least ceil(len / unit) later),
 // and no prefix sum over the lengths is needed.  The last slot is below T / unit + N.
-__device__ __forceinline__ int first_slot(const DecayPlan& P, int c, int s) { return c / P.unit + s; }
+template <typename Plan>
+__device__ __forceinline__ int first_slot(const Plan& P, int c, int s) { return c / P.unit + s; }
 
 // The unit (split) or sequence (single) of a workgroup: tokens [begin, end) of
 // sequence s, whose first row is `row0` of a head's rows.
@@ -615,8 +616,9 @@ struct Span {
 
 // Every thread of the workgroup must call it; false for the whole workgroup where
 // there is none (a slot that no unit has).
-template <int NT>
-__device__ __forceinline__ bool find_span(const DecayPlan& P, const int32_t* cu, int u, Span* o) {
+// Plan: any with DecayPlan's members of the split (single .. units_per_seq, rows, nseq, ragged).
+template <int NT, typename Plan>
+__device__ __forceinline__ bool find_span(const Plan& P, const int32_t* cu, int u, Span* o) {
   if (P.single) {
     o->s = u;
   } else if (P.ragged) {
@@ -662,7 +664,8 @@ __device__ __forceinline__ bool find_span(const DecayPlan& P, const int32_t* cu,
 
 // Row of the first token of span s in head h (of `heads`) of a [.., D] tensor; the rows
 // of head h + 1 are P.rows further.
-__device__ __forceinline__ int64_t first_row(const DecayPlan& P, const Span& s, int heads, int h) {
+template <typename Plan>
+__device__ __forceinline__ int64_t first_row(const Plan& P, const Span& s, int heads, int h) {
   return P.ragged ? (int64_t)h * P.rows + s.row0 : ((int64_t)s.s * heads + h) * P.rows;
 }
 

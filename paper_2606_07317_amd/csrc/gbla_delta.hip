@@ -1,0 +1,515 @@
+// gbla_delta.hip -- the gated delta rule in chunks (gfx950): the forward.
+//
+//   u_t = beta_t (v_t - e^g_t S_{t-1}^T k_t),  S_t = e^g_t S_{t-1} + k_t u_t^T,  o_t = scale S_t^T q_t
+// over a tile of L <= 64 tokens with the state S before it, c the sum of g from the tile's
+// start, L_ts = e^(c_t - c_s) k_t k_s (s < t) and (I + L beta) M = L:
+//   y_t = v_t - e^c_t S^T k_t,   e = y - M (beta y),   u = beta e
+//   o_t = scale (e^c_t S^T q_t + sum_{s <= t} e^(c_t - c_s) (q_t k_s) u_s)
+//   S_out = e^c_L S + sum_s e^(c_L - c_s) k_s u_s^T
+// (e_t is what the token's value differs from the state's prediction.)  Every exponent is
+// <= 0, so strong decays underflow to 0 and nothing overflows, and nothing is divided by
+// beta.
+//
+// M depends on keys and gates alone: a first launch (prep_kernel) forms it for all tiles at
+// once, and the walks read it as operands.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gbla_delta_tiles.h"
+
+namespace gbla {
+namespace {
+
+// Three parts of what the state is made of, so that it keeps fp32's accuracy (with two its
+// error was 3e-6 of its norm); two of what only the output takes, 2^-16 of a term, below its
+// own bf16 rounding.
+constexpr int kParts = 3, kOutParts = 2;
+
+// log2 of a token's decay in 64 bits; -inf (and so low that exp is 0 many times over) stays
+// finite, so that differences of sums do.
+__device__ __forceinline__ double log2_decay(float g) {
+  return (double)(g < -1e5f ? -1e5f : g) * 1.4426950408889634074;
+}
+
+// A tile's gates and its M.  Wave w takes the columns 16 w .. of the tile.  M is formed by
+// blocks of 16 rows, from the first on: with X = (I + L_ii beta)^-1, by substitution,
+//   M_ij = X (L_ij - sum_{j <= m < i} (L_im beta) M_mj)
+// in fp32 products, whose results are the next one's operands as they lie.  (Powers of L
+// beta would need fewer steps, but cancel: binomial coefficients, where keys are alike.)
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, const float* beta,
+            const int32_t* cu, Gates* gates, unsigned char* packs) {
+  using C = DS<T, D, 4, 1>;
+  constexpr int kL = 68;  // floats of a row of L
+  __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes];
+  __shared__ __attribute__((aligned(16))) float ldsL[kDeltaTile][kL], ldsX[4][16][20];
+  __shared__ __attribute__((aligned(16))) Gates G;
+  __shared__ int bad;
+  Span sp;
+  if (!find_span<C::NT>(tiles, cu, blockIdx.x, &sp)) return;
+  const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int live = sp.end - sp.begin;
+  RowsLoad<T, C> lk;
+  lk.load(k + (first_row(P, sp, P.heads, h / P.group) + sp.begin) * D, live);
+  const int64_t at = gate_row(P, sp, h) + sp.begin;
+  float gt = 0.0f, bt = 0.0f;
+  if (w == 0 && lane < live) gt = log_decay[at + lane], bt = beta[at + lane];
+  if (threadIdx.x == 0) bad = live;
+  __syncthreads();
+  if (w == 0 && lane < live && (!(gt <= 3.0e38f) || !isfinite(bt))) atomicMin(&bad, lane);
+  lk.find_bad(&bad);
+  lk.store(ldsK);
+  __syncthreads();
+  const int good = bad;
+  if (good < live) {
+    clear_rows<C>(ldsK, good);
+    __syncthreads();
+  }
+  if (w == 0) {
+    double c = lane < good ? log2_decay(gt) : 0.0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double x = __shfl_up(c, o);
+      if (lane >= o) c += x;
+    }
+    const double end = __shfl(c, 63);
+    const float hi = (float)c;
+    G.hi[lane] = hi;
+    G.lo[lane] = (float)(c - (double)hi);
+    G.beta[lane] = lane < good ? bt : 0.0f;
+    G.into[lane] = __builtin_amdgcn_exp2f(hi) * fmaf((float)(c - (double)hi), 0.69314718f, 1.0f);
+    G.rest[lane] = __builtin_amdgcn_exp2f((float)(end - c));
+    if (lane == 63) G.whole = G.into[63], G.good = good;
+    if (lane < 62) G.pad[lane] = 0.0f;
+  }
+  f32x4_t x[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) x[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int ks = 0; ks < C::KS; ++ks) {
+    const auto own = row_units<T, C>(ldsK, 16 * w + n, ks, g);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) Num<T>::mma(x[b], row_units<T, C>(ldsK, 16 * b + n, ks, g), own);
+  }
+  __syncthreads();
+  {
+    const int s = 16 * w + n;
+    const float hi = G.hi[s], lo = G.lo[s];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * b + 4 * g + r;
+        const float f = decay_between(G, t, hi, lo);
+        ldsL[t][s] = t > s ? x[b][r] * f : 0.0f;
+      }
+  }
+  __syncthreads();
+  // X of the wave's diagonal block: lane n its column n, row after row.
+  {
+    float y[16], bb[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&G.beta[16 * w + 4 * i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bb[4 * i + j] = z[j];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float sum = n == i ? 1.0f : 0.0f;
+#pragma unroll
+      for (int s4 = 0; s4 < i; s4 += 4) {
+        const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&ldsL[16 * w + i][16 * w + s4]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (s4 + j < i) sum = fmaf(-z[j] * bb[s4 + j], y[s4 + j], sum);
+      }
+      y[i] = sum;
+    }
+    if (g == 0) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ldsX[w][i][n] = y[i];
+    }
+  }
+  __syncthreads();
+  f32x4_t m[4];  // M's rows 16 i + 4 g + r of the wave's column n
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x4_t acc;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r] = ldsL[16 * i + 4 * g + r][16 * w + n];
+#pragma unroll
+    for (int j = 0; j < i; ++j) {
+      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(&ldsL[16 * i + n][16 * j + 4 * g]);
+      const f32x4_t b = *reinterpret_cast<const f32x4_t*>(&G.beta[16 * j + 4 * g]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(-a[r] * b[r], m[j][r], acc, 0, 0, 0);
+    }
+    const f32x4_t inv = *reinterpret_cast<const f32x4_t*>(&ldsX[i][n][4 * g]);
+    m[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) m[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(inv[r], acc[r], m[i], 0, 0, 0);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) ldsL[16 * i + 4 * g + r][16 * w + n] = -m[i][r];
+  __syncthreads();
+  const size_t slot = (size_t)h * P.tiles + sp.slot;
+  unsigned char* pack = packs + slot * (Packed<T, kParts>::kBytes);
+  for (int pair = w; pair < 6; pair += 4) {
+    const int b = pair < 2 ? pair : 2 + (pair >> 2), ks = pair < 2 ? 0 : pair & 1;
+    const f32x4_t* p = reinterpret_cast<const f32x4_t*>(&ldsL[row_of(b, n)][32 * ks + 8 * g]);
+    const f32x4_t a = p[0], c = p[1];
+    const float z[8] = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+    Parts<T, kParts> parts;
+    parts.set(z);
+    Packed<T, kParts>::put(pack, pair, lane, parts);
+  }
+  const u32x4_t* src = reinterpret_cast<const u32x4_t*>(&G);
+  u32x4_t* dst = reinterpret_cast<u32x4_t*>(gates + slot);
+  if (threadIdx.x < kGateBytes / 16) dst[threadIdx.x] = src[threadIdx.x];
+}
+
+template <typename T, int D>
+using WalkSizes = DS<T, D, D / 16, 1>;
+// What walk_kernel makes: outputs; or a unit's records: what the unit adds to the state
+// (from zeros), and what it does to the state before it (from the identity, without values).
+enum WalkMode { kOutputs, kRecords };
+
+template <typename T, int D, WalkMode Mode>
+__global__ void __launch_bounds__((WalkSizes<T, D>::NT), 2)
+walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, const int32_t* cu,
+            const Gates* gates, const unsigned char* packs, float* recB, float* recM, T* out,
+            float* final_state) {
+  using C = WalkSizes<T, D>;
+  using M = Packed<T, kParts>;
+  using Pk = Packed<T, kOutParts>;
+  constexpr bool Out = Mode == kOutputs;
+  __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes], ldsV[C::kTileBytes],
+      ldsQ[Out ? C::kTileBytes : 16];
+  __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBytes], ldsP[Out ? Pk::kBytes : 16];
+  __shared__ __attribute__((aligned(16))) Gates G;
+  __shared__ int bad[2];  // of this tile and the next
+  const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Span sp;
+  if (!find_span<C::NT>(P, cu, blockIdx.x, &sp)) return;
+  const int64_t pair = (int64_t)sp.s * P.value_heads + h;
+  const int e0 = 16 * C::CB * w;  // the wave's first column
+  Columns16<T, C> S;
+  const size_t record = ((size_t)h * P.units + sp.slot) * (D * D);
+  const bool map = !Out && blockIdx.z == 1;
+  if (!Out) {
+    // the last unit's record is not needed; nor what the first does to a state of zeros
+    if (sp.last || (map && sp.idx == 0 && !S0)) return;
+    if (map) S.identity(e0, lane);
+    else S.fill(0.0f);
+  } else {
+    const float* init = !P.single && (S0 || sp.idx > 0) ? recB + record : S0 ? S0 + pair * (D * D) : nullptr;
+    if (init) S.load(init, e0, lane);
+    else S.fill(0.0f);
+  }
+
+  const int64_t krow = first_row(P, sp, P.heads, h / P.group), vrow = first_row(P, sp, P.value_heads, h);
+  const size_t slot0 = (size_t)h * P.tiles + tile_slot(P, sp.row0, sp.s);
+  RowsLoad<T, C> lk, lq, lv;
+  BlockLoad<C, M::kBytes> lm;
+  BlockLoad<C, kGateBytes> lg;
+  auto fetch = [&](int t) {
+    const int left = sp.end - t;
+    lk.load(k + (krow + t) * D, left);
+    if (Out) lq.load(q + (krow + t) * D, left);
+    lv.load(v + (vrow + t) * D, map ? 0 : left);
+    const size_t slot = slot0 + t / kDeltaTile;
+    lm.load(packs + slot * M::kBytes, left > 0);
+    lg.load(gates + slot, left > 0);
+  };
+  if (sp.begin < sp.end) fetch(sp.begin);
+  if (threadIdx.x == 0) bad[0] = kDeltaTile;
+  __syncthreads();
+  for (int t0 = sp.begin, flip = 0; t0 < sp.end; t0 += kDeltaTile, flip ^= 1) {
+    const int live = min(kDeltaTile, sp.end - t0);
+    lk.store(ldsK);
+    if (Out) lq.store(ldsQ);
+    lv.store(ldsV);
+    lv.find_bad(&bad[flip]);
+    lm.store(ldsM);
+    lg.store(&G);
+    lds_barrier();
+    fetch(t0 + kDeltaTile);
+    const int good = min(min(bad[flip], G.good), live);
+    if (threadIdx.x == 0) bad[flip ^ 1] = kDeltaTile;
+    if (good < live) {
+      clear_rows<C>(ldsK, good);
+      clear_rows<C>(ldsV, good);
+      lds_barrier();
+    }
+    // Products over key channels: scores of the wave's own tokens, what the state
+    // predicts for the tile's keys, and what it answers to its queries (transposed).
+    constexpr int NP = C::NW < 4 ? 4 / C::NW : 1;  // blocks of 16 tokens whose scores a wave forms,
+    constexpr int PG = C::NW == 8 ? 1 : 2;         // with so many groups of 32 earlier tokens
+    const int pg0 = C::NW == 8 ? w >> 2 : 0;
+    f32x4_t y[C::CB][4], o[C::CB][4], p[NP][2 * PG];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c) y[c][b] = o[c][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int b = 0; b < 2 * PG; ++b) p[i][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) {
+      typename Num<T>::V8 kk[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) kk[b] = row_units<T, C>(ldsK, row_of(b, n), ks, g);
+      if constexpr (Out) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const auto own = row_units<T, C>(ldsQ, row_of((w + C::NW * i) & 3, n), ks, g);
+#pragma unroll
+          for (int b = 0; b < 2 * PG; ++b)
+            Num<T>::mma(p[i][b], PG == 2 ? kk[b] : row_units<T, C>(ldsK, row_of(2 * pg0 + b, n), ks, g), own);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c) {
+        const Parts<T, kParts> s = S.template operand<kParts>(c, ks);
+#pragma unroll
+        for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) Num<T>::mma(y[c][b], kk[b], s.v[i]);
+        if constexpr (Out) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const auto qq = row_units<T, C>(ldsQ, row_of(b, n), ks, g);
+#pragma unroll
+            for (int i = Parts<T, kOutParts>::kN - 1; i >= 0; --i) Num<T>::mma(o[c][b], s.v[i], qq);
+          }
+        }
+      }
+    }
+    // The scores as operands [token][earlier tokens] for all waves.
+    if constexpr (Out) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int b = (w + C::NW * i) & 3, t = row_of(b, n);
+        const float hi = G.hi[t], lo = G.lo[t];
+#pragma unroll
+        for (int z = 0; z < PG; ++z) {
+          const int ks = pg0 + z;
+          float x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int s = 32 * ks + 8 * g + j;
+            const float f = __builtin_amdgcn_exp2f((hi - G.hi[s]) + (lo - G.lo[s]));
+            x[j] = s <= t ? p[i][2 * z + (j >> 2)][j & 3] * (P.scale * f) : 0.0f;
+          }
+          Parts<T, kOutParts> parts;
+          parts.set(x);
+          if (ks == 0 || b >= 2) Pk::put(ldsP, lower_pair(b, ks), lane, parts);
+        }
+      }
+    }
+    // The tile's values less the prediction, and what of that stays as the tile is read
+    // token by token.
+    float beta[2][8], rest[2][8];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        beta[ks][j] = G.beta[32 * ks + 8 * g + j];
+        rest[ks][j] = G.rest[32 * ks + 8 * g + j];
+      }
+#pragma unroll
+    for (int c = 0; c < C::CB; ++c) {
+      Parts<T, kParts> by[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        float x[8];
+        Num<T>::widen(value_column<T, C>(ldsV, C::CB * w + c, ks, lane), x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float z = fmaf(-G.into[32 * ks + 8 * g + j], y[c][2 * ks + (j >> 2)][j & 3], x[j]);
+          y[c][2 * ks + (j >> 2)][j & 3] = z;
+          x[j] = beta[ks][j] * z;
+        }
+        by[ks].set(x);
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int ks = 0; ks <= (b >> 1); ++ks)
+          mma_parts<T>(y[c][b], M::get(ldsM, lower_pair(b, ks), lane), by[ks]);
+    }
+    if (Out) lds_barrier();  // the scores
+    const float whole = G.whole;
+#pragma unroll
+    for (int c = 0; c < C::CB; ++c) {
+      if constexpr (Out) {
+        Parts<T, kOutParts> u[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          float x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = beta[ks][j] * y[c][2 * ks + (j >> 2)][j & 3];
+          u[ks].set(x);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const float f = P.scale * G.into[row_of(b, n)];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[c][b][r] *= f;
+#pragma unroll
+          for (int ks = 0; ks <= (b >> 1); ++ks)
+            mma_parts<T>(o[c][b], u[ks], Pk::get(ldsP, lower_pair(b, ks), lane));
+        }
+      }
+      Parts<T, kParts> u[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = rest[ks][j] * (beta[ks][j] * y[c][2 * ks + (j >> 2)][j & 3]);
+        u[ks].set(x);
+      }
+#pragma unroll
+      for (int i = 0; i < C::NB; ++i) {
+        f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          const auto a = key_column<T, C>(ldsK, i, kt, lane);
+#pragma unroll
+          for (int z = Parts<T, kParts>::kN - 1; z >= 0; --z) Num<T>::mma(x, a, u[kt].v[z]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S.s[c][i][r] = fmaf(whole, S.s[c][i][r], x[r]);
+      }
+    }
+    if constexpr (Out) {
+      const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + (vrow + t0) * D, (uint32_t)(live * C::kRow));
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int t = row_of(b, n);
+          f32x4_t z = o[c][b];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z[r] = t >= good ? __builtin_nanf("") : z[r];
+          const uint32_t to = (uint32_t)(t * C::kRow + (e0 + 16 * c + 4 * g) * C::ES);
+          if constexpr (sizeof(T) == 2) {
+            __builtin_amdgcn_raw_buffer_store_b64((u32x2_t){pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])}, ro,
+                                                  to, 0, 0);
+          } else {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, z), ro, to, 0, 0);
+          }
+        }
+    }
+    if (good < live) S.fill(__builtin_nanf(""));
+    lds_barrier();
+  }
+  if (!Out) S.store((map ? recM : recB) + record, e0, lane);
+  else if (final_state && sp.last) S.store(final_state + pair * (D * D), e0, lane);
+}
+
+// The records become the state before each unit, in place: S -> M S + B from unit to unit.
+// A workgroup takes 16 value channels, wave w the key channels 16 w ..; the state passes from
+// wave to wave through LDS, in fp32, with fp32 products.
+template <int D>
+__global__ void __launch_bounds__(4 * D)
+scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const float* recM) {
+  constexpr int KS = D / 16, kPitch = D + 4;
+  __shared__ __attribute__((aligned(16))) float lds[2][16 * kPitch];
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int s = blockIdx.x / KS, e0 = 16 * (blockIdx.x % KS), h = blockIdx.y;
+  const int64_t len = P.ragged ? (int64_t)cu[s + 1] - cu[s] : P.rows;
+  const int first = P.ragged ? first_slot(P, cu[s], s) : s * P.units_per_seq;
+  const int units = units_of(len, P.unit);
+  const size_t record = ((size_t)h * P.units + first) * (D * D);
+  float* B = recB + record + (16 * w + 4 * g) * D + e0 + n;
+  const float* M = recM + record + (16 * w + n) * D + 4 * g;
+  f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f}, b, m[KS];
+  if (S0) {
+    const float* p = S0 + ((int64_t)s * P.value_heads + h) * (D * D) + (16 * w + 4 * g) * D + e0 + n;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = p[r * D];
+  }
+  // The last unit has no record, and the first no map if the state before it is zeros.
+  auto fetch = [&](int u) {
+    const bool any = u < units - 1, map = any && (u > 0 || S0);
+    const size_t at = (size_t)u * (D * D);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) b[r] = any ? B[at + r * D] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      m[i] = map ? *reinterpret_cast<const f32x4_t*>(M + at + 16 * i) : (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  };
+  fetch(0);
+  for (int u = 0; u < units; ++u) {
+    float* sx = lds[u & 1];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) B[(size_t)u * (D * D) + r * D] = x[r];
+    if (u + 1 == units) break;
+    *reinterpret_cast<f32x4_t*>(&sx[n * kPitch + 16 * w + 4 * g]) = x;
+    lds_barrier();
+    f32x4_t z[2] = {b, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&sx[n * kPitch + 16 * i + 4 * g]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i][r], y[r], z[r & 1], 0, 0, 0);
+    }
+    fetch(u + 1);
+    x = z[0] + z[1];
+  }
+}
+
+template <typename F>
+gbla_status by_type(const DeltaPlan& p, F f) {
+  auto dims = [&](auto t) {
+    if (p.d == 32) f(t, std::integral_constant<int, 32>{});
+    else if (p.d == 64) f(t, std::integral_constant<int, 64>{});
+    else f(t, std::integral_constant<int, 128>{});
+  };
+  if (p.dtype == GBLA_BF16) dims(uint16_t{});
+  else dims(float{});
+  return hipGetLastError() == hipSuccess ? GBLA_OK : GBLA_ERR_HIP;
+}
+
+}  // namespace
+
+gbla_status launch_delta_forward(const DeltaPlan& p, const void* q, const void* k, const void* v,
+                                 const float* log_decay, const float* beta, const float* S0,
+                                 const int32_t* cu, void* ws, void* out, float* final_state,
+                                 hipStream_t st) {
+  unsigned char* base = static_cast<unsigned char*>(ws);
+  Gates* gates = reinterpret_cast<Gates*>(base + p.off_gates);
+  unsigned char* packs = base + p.off_pack;
+  float* recB = reinterpret_cast<float*>(base + p.off_B);
+  float* recM = reinterpret_cast<float*>(base + p.off_M);
+  return by_type(p, [&](auto t, auto dim) {
+    using T = decltype(t);
+    constexpr int D = decltype(dim)::value;
+    const auto walk = [&](auto kernel, int z) {
+      hipLaunchKernelGGL(kernel, dim3(p.grid_units, p.value_heads, z), dim3((WalkSizes<T, D>::NT)), 0, st, p,
+                         (const T*)q, (const T*)k, (const T*)v, S0, cu, gates, packs, recB, recM, (T*)out,
+                         final_state);
+    };
+    if (p.tokens > 0)
+      hipLaunchKernelGGL((prep_kernel<T, D>), dim3(p.tiles, p.value_heads), dim3(kThreads), 0, st, p, tile_spans(p),
+                         (const T*)k, log_decay, beta, cu, gates, packs);
+    if (!p.single) {
+      walk(walk_kernel<T, D, kRecords>, 2);
+      hipLaunchKernelGGL((scan_kernel<D>), dim3(p.nseq * (D / 16), p.value_heads), dim3(4 * D), 0, st, p, cu, S0,
+                         recB, recM);
+    }
+    walk(walk_kernel<T, D, kOutputs>, 1);
+  });
+}
+
+}  // namespace gbla

@@ -1,0 +1,90 @@
+// gbla_delta_plan.cpp -- plans of the gated delta rule: split sizes and workspace
+// layouts, a function of the shape alone.
+#include <math.h>
+#include <stdint.h>
+
+#include "gbla.h"
+#include "gbla_delta.h"
+
+namespace gbla {
+namespace {
+
+// A grid's first dimension has fewer than 2^32 threads; the workgroups here have up to 512.
+constexpr int64_t kMaxGroups = 4294967295LL / 512;
+constexpr int kMaxGridY = 65535;
+
+// Tokens of a unit (a power of two).
+int32_t unit_tokens(const DeltaPlan& p) {
+  int32_t unit = kDeltaMaxUnit;
+  while (unit > 2 * kDeltaTile && p.tokens * p.value_heads < (int64_t)unit * 512) unit /= 2;
+  return unit;
+}
+
+// Whether a workgroup walks a whole sequence.
+bool walk_whole(const DeltaPlan& p, int64_t longest) {
+  return longest <= 2 * kDeltaTile || longest * 256 <= p.tokens * p.value_heads;
+}
+
+}  // namespace
+
+gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backward, DeltaPlan* p) {
+  if (!s || !p) return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->batch < 1 || s->seqlen < 0 || s->heads < 1 || s->value_heads < 1)
+    return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->value_heads % s->heads != 0) return GBLA_ERR_INVALID_ARGUMENT;
+  if (!isfinite(s->scale)) return GBLA_ERR_INVALID_ARGUMENT;
+  if (ragged && s->max_seqlen < 0) return GBLA_ERR_INVALID_ARGUMENT;
+  if (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return GBLA_ERR_UNSUPPORTED;
+  if (s->dtype != GBLA_F32 && s->dtype != GBLA_BF16) return GBLA_ERR_UNSUPPORTED;
+  if (s->value_heads > kMaxGridY) return GBLA_ERR_UNSUPPORTED;
+  DeltaPlan q{};
+  q.nseq = s->batch;
+  q.rows = s->seqlen;
+  q.heads = s->heads;
+  q.value_heads = s->value_heads;
+  q.group = s->value_heads / s->heads;
+  q.d = s->head_dim;
+  q.dtype = s->dtype;
+  q.ragged = ragged ? 1 : 0;
+  q.scale = s->scale;
+  q.tokens = ragged ? (int64_t)s->seqlen : (int64_t)s->batch * s->seqlen;
+  if (q.tokens > kMaxGroups * kDeltaTile) return GBLA_ERR_UNSUPPORTED;  // before products with them
+  // sum over the sequences of max(1, ceil(len / tile)) <= tokens / tile + N
+  const int64_t most = q.tokens / kDeltaTile + q.nseq;
+  if (most > kMaxGroups) return GBLA_ERR_UNSUPPORTED;
+  q.unit = unit_tokens(q);
+  const int64_t cap = q.tokens / q.unit + q.nseq;
+  if (ragged) {
+    q.tiles = (int32_t)most;
+    q.units = (int32_t)cap;
+  } else {
+    const auto pieces = [&](int64_t size) {
+      const int64_t each = ((int64_t)q.rows + size - 1) / size;
+      return (int32_t)(each < 1 ? 1 : each);
+    };
+    q.tiles_per_seq = pieces(kDeltaTile);
+    q.tiles = q.tiles_per_seq * q.nseq;
+    q.units_per_seq = pieces(q.unit);
+    q.units = q.units_per_seq * q.nseq;
+  }
+  q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows) ? 1 : 0;
+  // the split's scan has a workgroup for every 16 value channels of a sequence's states
+  if ((int64_t)q.nseq * (q.d / 16) > kMaxGroups) q.single = 1;
+  q.grid_units = q.single ? q.nseq : q.units;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes, 256);
+    return at;
+  };
+  q.off_gates = take((size_t)most * q.value_heads * kGateBytes);
+  q.off_pack = take((size_t)most * q.value_heads * kPackBytes);
+  const size_t states = (size_t)cap * q.value_heads * q.d * q.d * sizeof(float);
+  q.off_B = take(states);
+  q.off_M = take(states);
+  q.total_bytes = off;
+  *p = q;
+  return GBLA_OK;
+}
+
+}  // namespace gbla

@@ -1,0 +1,146 @@
+// gbla_delta_step.hip -- the gated delta rule for one new token of each row (gfx950):
+//   z = e^g state,  u = beta (v - z^T k),  state = z + k u^T,  out = scale state^T q
+//                                                      = scale (z^T q + (k q) u).
+//
+// Nothing but the states moves: each is read and written once, 8 d^2 bytes a value head,
+// with about seven operations an element.  A workgroup takes one row, one value head and a
+// slice of W value channels; a thread holds four value channels of every R-th key channel in
+// registers, all its loads in flight at once.  The second form of the output needs nothing
+// of the new state, so one round of sums over the key channels (over lanes, then over the
+// waves in LDS, in a fixed order) serves both products.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gbla_decay_tiles.h"
+#include "gbla_delta.h"
+
+namespace gbla {
+namespace {
+
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(kThreads)
+step_kernel(int rows, int heads, int value_heads, float scale, const T* q, const T* k, const T* v,
+            const float* log_decay, const float* beta, const int32_t* indices, int slots, float* state,
+            T* out) {
+  constexpr int L = W / 4;             // lanes of a row of the slice
+  constexpr int R = kThreads / L;      // key channels of a pass
+  constexpr int N = D / R;             // of a thread
+  constexpr int kWaves = kThreads / 64;
+  static_assert(R * N == D && L <= 64, "threads of a slice");
+  __shared__ f32x4_t red[2][kWaves][L];
+  __shared__ float dots[kWaves];
+  __shared__ int same[2];
+  const int n0 = blockIdx.x, h = blockIdx.y, e0 = blockIdx.z * W;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l = threadIdx.x % L, e = 4 * l, c0 = threadIdx.x / L;
+  const int hk = h / (value_heads / heads);
+  const int slot = indices ? indices[n0] : n0;
+  if (slot < 0 || slot >= slots) return;
+  float* S = state + ((int64_t)slot * value_heads + h) * (D * D) + e0 + e;
+  f32x4_t s[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = *reinterpret_cast<const f32x4_t*>(S + (c0 + i * R) * D);
+  bool more = false;
+  if (indices && rows > 1) {  // rows of one slot: the first row's workgroup does them all
+    if (threadIdx.x < 2) same[threadIdx.x] = 0;
+    __syncthreads();
+    for (int m = threadIdx.x; m < rows; m += kThreads)
+      if (m != n0 && indices[m] == slot) same[m > n0] = 1;
+    __syncthreads();
+    if (same[0]) return;
+    more = same[1] != 0;
+  }
+  for (int n = n0; n < rows; ++n) {
+    if (n != n0 && indices[n] != slot) continue;
+    const int64_t vr = (int64_t)n * value_heads + h;
+    const T* kk = k + ((int64_t)n * heads + hk) * D;
+    const T* qq = q + ((int64_t)n * heads + hk) * D;
+    const T* vv = v + vr * D + e0 + e;
+    const float lam = expf(log_decay[vr]), b = beta[vr];
+    float kx[N], vx[4];
+    f32x4_t zk = {0.0f, 0.0f, 0.0f, 0.0f}, zq = {0.0f, 0.0f, 0.0f, 0.0f};
+    float dot = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) vx[r] = widen1(vv[r]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      kx[i] = widen1(kk[c0 + i * R]);
+      const float qx = widen1(qq[c0 + i * R]);
+      dot = fmaf(kx[i], qx, dot);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[i][r] *= lam;
+        zk[r] = fmaf(kx[i], s[i][r], zk[r]);
+        zq[r] = fmaf(qx, s[i][r], zq[r]);
+      }
+    }
+#pragma unroll
+    for (int o = L; o < 64; o <<= 1) {
+      dot += __shfl_xor(dot, o);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        zk[r] += __shfl_xor(zk[r], o);
+        zq[r] += __shfl_xor(zq[r], o);
+      }
+    }
+    if (lane < L) red[0][wave][l] = zk, red[1][wave][l] = zq;
+    if (lane == 0) dots[wave] = dot;
+    __syncthreads();
+    zk = red[0][0][l];
+    zq = red[1][0][l];
+    dot = dots[0];
+#pragma unroll
+    for (int u = 1; u < kWaves; ++u) {
+      zk += red[0][u][l];
+      zq += red[1][u][l];
+      dot += dots[u];
+    }
+    float u[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) u[r] = b * (vx[r] - zk[r]);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[i][r] = fmaf(kx[i], u[r], s[i][r]);
+    if (c0 == 0) {
+      float y[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = scale * fmaf(dot, u[r], zq[r]);
+      T* to = out + vr * D + e0 + e;
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<u32x2_t*>(to) = (u32x2_t){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+      else
+        *reinterpret_cast<f32x4_t*>(to) = (f32x4_t){y[0], y[1], y[2], y[3]};
+    }
+    if (!more) break;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<f32x4_t*>(S + (c0 + i * R) * D) = s[i];
+}
+
+}  // namespace
+
+gbla_status launch_delta_step(const gbla_delta_shape& s, const void* q, const void* k, const void* v,
+                              const float* log_decay, const float* beta, const int32_t* indices,
+                              int32_t slots, float* state, void* out, hipStream_t st) {
+#define GBLA_STEP(T, D, W)                                                                         \
+  hipLaunchKernelGGL((step_kernel<T, D, W>), dim3(s.batch, s.value_heads, D / W), dim3(kThreads),  \
+                     0, st, s.batch, s.heads, s.value_heads, s.scale, (const T*)q, (const T*)k,    \
+                     (const T*)v, log_decay, beta, indices, slots, state, (T*)out)
+  const bool half = s.dtype == GBLA_BF16;
+  if (s.head_dim == 32) {
+    if (half) GBLA_STEP(uint16_t, 32, 32);
+    else GBLA_STEP(float, 32, 32);
+  } else if (s.head_dim == 64) {
+    if (half) GBLA_STEP(uint16_t, 64, 64);
+    else GBLA_STEP(float, 64, 64);
+  } else {
+    if (half) GBLA_STEP(uint16_t, 128, 64);
+    else GBLA_STEP(float, 128, 64);
+  }
+#undef GBLA_STEP
+  return hipGetLastError() == hipSuccess ? GBLA_OK : GBLA_ERR_HIP;
+}
+
+}  // namespace gbla

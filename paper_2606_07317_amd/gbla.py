@@ -65,6 +65,12 @@ class DecayShape(ctypes.Structure):
                 ("max_seqlen", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class DeltaShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("value_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_seqlen", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -127,6 +133,14 @@ def load_library(path: str = LIB_PATH):
     lib.gbla_decay_backward.restype = ctypes.c_int
     lib.gbla_decay_step.argtypes = [DP] + [P] * 5 + [ctypes.c_int32] + [P] * 3
     lib.gbla_decay_step.restype = ctypes.c_int
+    EP = ctypes.POINTER(DeltaShape)
+    for name in ("gbla_delta_workspace_bytes", "gbla_delta_ragged_workspace_bytes"):
+        getattr(lib, name).argtypes = [EP]
+        getattr(lib, name).restype = sz
+    lib.gbla_delta_forward.argtypes = [EP] + [P] * 8 + [sz] + [P] * 3
+    lib.gbla_delta_forward.restype = ctypes.c_int
+    lib.gbla_delta_step.argtypes = [EP] + [P] * 6 + [ctypes.c_int32] + [P] * 3
+    lib.gbla_delta_step.restype = ctypes.c_int
     lib.gbla_status_string.argtypes = [ctypes.c_int]
     lib.gbla_status_string.restype = ctypes.c_char_p
     if path == LIB_PATH:
@@ -810,4 +824,97 @@ def decay_step(q, k, v, log_decay, state, state_indices=None, scale: Optional[fl
             ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state_indices),
             slots, _ptr(state), _ptr(out), _current(dev))
     _raise(st, "gbla_decay_step")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# The gated delta rule.
+# ---------------------------------------------------------------------------
+def delta_shape(q, k, v, scale: Optional[float] = None, cu_seqlens=None, max_seqlen=None) -> DeltaShape:
+    B, n, H, K, d = _query_key(q, k, cu_seqlens)
+    if K != H:
+        raise ValueError("k must have as many heads as q")
+    V = _size_of(v, 4, 1) if cu_seqlens is None else _size_of(v, 3, 0)
+    _want(v, "v", (B, V, n, d) if cu_seqlens is None else (V, n, d), q.dtype, q.device)
+    msl = 0
+    if cu_seqlens is not None:
+        msl = int(max_seqlen) if max_seqlen is not None else n
+    return DeltaShape(B, n, H, V, d, msl, _dtype_code(q),
+                      float(d) ** -0.5 if scale is None else float(scale))
+
+
+def delta_workspace_bytes(shape: DeltaShape, ragged: bool = False) -> int:
+    """``ragged``: for calls with cu_seqlens only, which take less than both readings."""
+    return _scratch("gbla_delta", shape, ragged)
+
+
+def _check_delta(v, log_decay, beta, shape, states):
+    dev = v.device
+    _want(log_decay, "log_decay", v.shape[:-1], torch.float32, dev)
+    _want(beta, "beta", v.shape[:-1], torch.float32, dev)
+    for t, name in states:
+        if t is not None:
+            _want(t, name, (shape.batch, shape.value_heads, shape.head_dim, shape.head_dim),
+                  torch.float32, dev)
+
+
+def delta_attention(q, k, v, log_decay, beta, scale: Optional[float] = None, initial_state=None,
+                    final_state=None, cu_seqlens=None, max_seqlen=None, workspace=None, out=None,
+                    stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """The gated delta rule, u_t = beta_t (v_t - exp(g_t) S_{t-1}^T k_t), S_t = exp(g_t) S_{t-1}
+    + k_t u_t^T, o_t = scale S_t^T q_t (scale d^-1/2 by default); see include/gbla.h.
+    q, k [B, H, n, d] or [H, T, d]; v with V heads, H dividing V; log_decay (<= 0) and beta
+    fp32 [B, V, n] or [V, T]; ``initial_state`` fp32 [N, V, d, d] or None (zeros).  Returns the
+    output, like v, and the final state: None, or ``final_state`` if that is a tensor (it may be
+    initial_state, updated in place), or a new tensor if it is True.
+    ``max_seqlen`` (ragged) is an upper bound of the lengths; it only chooses kernels."""
+    shape = delta_shape(q, k, v, scale, cu_seqlens, max_seqlen)
+    given = final_state if isinstance(final_state, torch.Tensor) else None
+    _check_delta(v, log_decay, beta, shape, ((initial_state, "initial_state"), (given, "final_state")))
+    dev = q.device
+    need = delta_workspace_bytes(shape, cu_seqlens is not None)
+    with _on(dev, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check_ws(workspace, dev, need)
+        out = _like(out, "out", v)
+        if given is None and final_state:
+            d = shape.head_dim
+            given = torch.empty((shape.batch, shape.value_heads, d, d), dtype=torch.float32, device=dev)
+        st = load_library().gbla_delta_forward(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(beta),
+            _ptr(initial_state), _ptr(cu_seqlens), _ptr(workspace), workspace.numel(), _ptr(out),
+            _ptr(given), _current(dev))
+    _raise(st, "gbla_delta_forward")
+    return out, given
+
+
+def delta_step(q, k, v, log_decay, beta, state, state_indices=None, scale: Optional[float] = None,
+               out=None, stream=None) -> torch.Tensor:
+    """delta_attention for one new token of each row: q, k [N, H, d], v [N, V, d], log_decay and
+    beta fp32 [N, V], ``state`` fp32 [slots, V, d, d], updated in place.  Row n uses slot
+    state_indices[n] (int32 [N]; without indices slot n).  Rows of one slot are applied in row
+    order; a row whose index is outside the slots is skipped and its output row left as it is.
+    Returns the output, like v."""
+    _check(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q must be [N, H, d]")
+    N, H, d = q.shape
+    dev, dtype = q.device, q.dtype
+    V = _size_of(v, 3, 1)
+    _want(k, "k", q.shape, dtype, dev)
+    _want(v, "v", (N, V, d), dtype, dev)
+    _want(log_decay, "log_decay", (N, V), torch.float32, dev)
+    _want(beta, "beta", (N, V), torch.float32, dev)
+    slots = _size_of(state, 4, 0)
+    _want(state, "state", (slots, V, d, d), torch.float32, dev)
+    if state_indices is not None:
+        _want(state_indices, "state_indices", (N,), torch.int32, dev)
+    shape = DeltaShape(N, 1, H, V, d, 0, _dtype_code(q), float(d) ** -0.5 if scale is None else float(scale))
+    with _on(dev, stream):
+        out = _like(out, "out", v)
+        st = load_library().gbla_delta_step(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(beta),
+            _ptr(state_indices), slots, _ptr(state), _ptr(out), _current(dev))
+    _raise(st, "gbla_delta_step")
     return out
