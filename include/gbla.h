@@ -475,10 +475,13 @@ typedef struct {
   float scale;         /* factor of the output (finite), usually d^-1/2          */
 } gbla_delta_shape;
 
-/* Scratch bytes of gbla_delta_forward (the larger of the dense and the ragged reading, for
- * every max_seqlen; the second: what the ragged reading alone needs); 0 if not accepted. */
+/* Scratch bytes of gbla_delta_forward / gbla_delta_backward (the larger of the dense and the
+ * ragged reading, for every max_seqlen); 0 if neither is accepted. */
 size_t gbla_delta_workspace_bytes(const gbla_delta_shape* shape);
+size_t gbla_delta_backward_workspace_bytes(const gbla_delta_shape* shape);
+/* What the ragged reading alone needs; 0 if it is not accepted. */
 size_t gbla_delta_ragged_workspace_bytes(const gbla_delta_shape* shape);
+size_t gbla_delta_backward_ragged_workspace_bytes(const gbla_delta_shape* shape);
 
 /*
  * The gated delta rule, with g = log_decay and b = beta of token t and value head h:
@@ -502,6 +505,27 @@ gbla_status gbla_delta_forward(const gbla_delta_shape* shape, const void* q, con
                                const float* initial_state, const int32_t* cu_seqlens,
                                void* workspace, size_t workspace_bytes, void* out,
                                float* final_state, void* stream);
+
+/*
+ * Gradients of L = sum(out * dout) + sum(final_state * dfinal_state):
+ *   dout            like v            dfinal_state  fp32 [N,V,d,d] or NULL (zeros)
+ *   dq, dk          like q, k (summed over the value heads that share them)
+ *   dv              like v            dlog_decay, dbeta  fp32, like the gates
+ *   dinitial_state  fp32 [N,V,d,d] or NULL (not wanted); may be dfinal_state
+ * The states are formed again from the inputs.  Gradients are sums in fp32, of products with
+ * fp32's accuracy for the gates' and the states' in both types; in bf16 those of q, k and v
+ * enter fp32 values in two or three bf16 parts before they are rounded once.  Reductions run
+ * in an order fixed by the shape: repeated calls give the same bits.  A value that is not
+ * finite may reach every gradient of its sequence and of the heads that read it, but none of
+ * another sequence or another query and key head.
+ */
+gbla_status gbla_delta_backward(const gbla_delta_shape* shape, const void* q, const void* k,
+                                const void* v, const float* log_decay, const float* beta,
+                                const float* initial_state, const int32_t* cu_seqlens,
+                                const void* dout, const float* dfinal_state, void* workspace,
+                                size_t workspace_bytes, void* dq, void* dk, void* dv,
+                                float* dlog_decay, float* dbeta, float* dinitial_state,
+                                void* stream);
 
 /*
  * The same recurrence for one new token of each of shape->batch rows:

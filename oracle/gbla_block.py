@@ -96,6 +96,69 @@ def delta_sizes(q, k, v, g, beta, scale, S0=None, tile=64):
     return out, Z[:, None, :]
 
 
+def delta_backward_sizes(q, k, v, g, beta, do, scale, S0=None, dS=None, tile=64):
+    """The like of ``delta_sizes`` for (dq, dk, dv, dg, dbeta, dS0).  A token's map of the state's
+    gradient is the transpose of the forward's and makes no column longer either.  Per token and
+    value channel: A bounds an error in reading the state, Bu one in u, G one in reading the
+    state's gradient, Bf one in f = D^T k (from the tile's do, the gradient after the tile and
+    the tile's later f).  dk = D u - Z dv takes both factors' errors of both products, dbeta = f
+    miss likewise; dg adds up those of do o and dv v over the sequence and of one <D, S>."""
+    V, n, d = v.shape
+    H = q.shape[0]
+    q, k, v, beta, do = _shared(q, V), _shared(k, V), v.double(), beta.double(), do.double()
+    lam = torch.exp(g.double())[..., None]
+    norm = lambda X: X.norm(dim=1)
+    S = torch.zeros(V, d, d, dtype=torch.float64) if S0 is None else S0.double().clone()
+    Z = norm(S)
+    past = []
+    for t in range(n):
+        if t % tile == 0:
+            head, inner, added = norm(S), torch.zeros(V, d), torch.zeros(V, d)
+            Z = Z + head
+        P = lam[:, t, :, None] * S
+        miss = v[:, t] - torch.matmul(k[:, t, None, :], P)[:, 0]
+        u = beta[:, t, None] * miss
+        S = P + k[:, t, :, None] * u[:, None, :]
+        y = v[:, t].abs() + head
+        inner, added = inner + beta[:, t, None] * y, added + u.abs()
+        wrong = Z + y + inner + added  # of miss
+        Z = lam[:, t] * Z + beta[:, t, None] * (y + inner + added) + u.abs()
+        past.append((P, miss, u, S, Z + head + added, wrong))
+    D = torch.zeros_like(S) if dS is None else dS.double().clone()
+    W = norm(D)
+    out = {x: torch.zeros(V, n, d, dtype=torch.float64) for x in ("dq", "dk", "dv")}
+    db = torch.zeros(V, n, dtype=torch.float64)
+    flow = torch.zeros(V, dtype=torch.float64)
+    for t in reversed(range(n)):
+        if t == n - 1 or t % tile == tile - 1:
+            tail, given, later = norm(D), torch.zeros(V, d), torch.zeros(V, d)
+            W = W + tail
+        P, miss, u, S, A, wrong = past[t]
+        o = abs(scale) * do[:, t].abs()
+        D = D + scale * q[:, t, :, None] * do[:, t, None, :]
+        f = torch.matmul(k[:, t, None, :], D)[:, 0]
+        dv = beta[:, t, None] * f
+        given = given + o
+        W = W + q[:, t].norm(dim=-1, keepdim=True) * o
+        G = W + tail + given + later
+        Bf = G + beta[:, t, None] * (tail + given)
+        later = later + dv.abs() + beta[:, t, None] * (tail + given)
+        out["dq"][:, t] = (A * o).sum(-1, keepdim=True)
+        out["dv"][:, t] = beta[:, t, None] * Bf
+        Bu = beta[:, t, None] * wrong
+        out["dk"][:, t] = (G * u.abs() + (norm(D) + tail + given + later) * Bu + A * dv.abs()
+                           + (norm(P) + A) * out["dv"][:, t]).sum(-1, keepdim=True)
+        db[:, t] = (Bf * miss.abs() + f.abs() * wrong).sum(-1)
+        flow = flow + (A * o + out["dv"][:, t] * v[:, t].abs()).sum(-1)
+        D = D - k[:, t, :, None] * dv[:, None, :]
+        W = lam[:, t] * (W + out["dv"][:, t] + dv.abs())
+        D = lam[:, t, :, None] * D
+    start = torch.zeros(V, d, d, dtype=torch.float64) if S0 is None else S0.double()
+    dg = flow[:, None] + ((W * norm(start)) + norm(D) * Z).sum(-1)[:, None]
+    fold = lambda x: x.view(H, V // H, n, d).sum(1)
+    return fold(out["dq"]), fold(out["dk"]), out["dv"], dg.expand(V, n), db, W[:, None, :].expand(V, d, d)
+
+
 def add_norm(x, residual, w, eps):
     """(normalised, sum): the sum rounded to x's type, and the norm of that sum."""
     s = x.double() if residual is None else (x.double() + residual.double()).to(x.dtype).double()

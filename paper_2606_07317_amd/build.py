@@ -24,6 +24,7 @@ SOURCES = [os.path.join(CSRC, "gbla_kernels.hip"), os.path.join(CSRC, "gbla_stre
            os.path.join(CSRC, "gbla_decay_back.hip"), os.path.join(CSRC, "gbla_decay_step.hip"),
            os.path.join(CSRC, "gbla_decay_plan.cpp"), os.path.join(CSRC, "gbla_decay_api.cpp"),
            os.path.join(CSRC, "gbla_delta.hip"), os.path.join(CSRC, "gbla_delta_step.hip"),
+           os.path.join(CSRC, "gbla_delta_back.hip"), os.path.join(CSRC, "gbla_delta_grads.hip"),
            os.path.join(CSRC, "gbla_delta_plan.cpp"), os.path.join(CSRC, "gbla_delta_api.cpp")]
 
 # Packed fp32 VALU ops are switched off for all device code; hipcc's host

@@ -38,6 +38,16 @@ struct DeltaPlan {
   size_t off_pack;   // [V, tiles] packed triangles
   size_t off_B;      // [V, units, d, d] fp32: what a unit adds; then the state before each unit
   size_t off_M;      // [V, units, d, d] fp32: what a unit does to the state before it
+  // Backward:
+  size_t off_packT;  // [V, tiles] packed triangles, transposed
+  size_t off_D;      // [V, units, d, d] fp32: the gradient of the state after each unit
+  size_t off_S;      // [V, tiles, d, d] fp32: the state before each tile, [value][key channel]
+  size_t off_N;      // ... the gradient of the state after each tile
+  size_t off_E;      // [V, tiles, d, 64] fp32: the tiles' e, [value channel][token]
+  size_t off_F;      // ... the gradient of u
+  size_t off_do_o;   // fp32, like the gates: do o of each token
+  size_t off_dv_v;   // ... dv v
+  size_t off_dS0;    // [N, V, d, d] fp32: dinitial_state where the caller wants none
   size_t total_bytes;
 };
 
@@ -47,6 +57,21 @@ gbla_status launch_delta_forward(const DeltaPlan& p, const void* q, const void* 
                                  const float* log_decay, const float* beta, const float* S0,
                                  const int32_t* cu, void* ws, void* out, float* final_state,
                                  hipStream_t st);
+gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void* k, const void* v,
+                                  const float* log_decay, const float* beta, const float* S0,
+                                  const int32_t* cu, const void* dout, const float* dfinal, void* ws,
+                                  void* dq, void* dk, void* dv, float* dlog_decay, float* dbeta,
+                                  float* dS0, hipStream_t st);
+// Its pass from the last tile to the first (gbla_delta_back.hip): the units' records, and the
+// walk; and its last launches (gbla_delta_grads.hip): the gradients of q, k, v and log_decay.
+gbla_status launch_delta_back_records(const DeltaPlan& p, const void* q, const void* k, const int32_t* cu,
+                                      const void* dout, void* ws, hipStream_t st);
+gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void* k, const void* v,
+                                   const int32_t* cu, const void* dout, const float* dfinal, void* ws,
+                                   float* dS0, hipStream_t st);
+gbla_status launch_delta_grads(const DeltaPlan& p, const void* q, const void* k, const float* S0,
+                               const int32_t* cu, const void* dout, void* ws, void* dq, void* dk,
+                               void* dv, float* dlog_decay, const float* dS0, hipStream_t st);
 gbla_status launch_delta_step(const gbla_delta_shape& s, const void* q, const void* k,
                               const void* v, const float* log_decay, const float* beta,
                               const int32_t* indices, int32_t slots, float* state, void* out,

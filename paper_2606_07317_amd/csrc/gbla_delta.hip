@@ -36,10 +36,11 @@ __device__ __forceinline__ double log2_decay(float g) {
 //   M_ij = X (L_ij - sum_{j <= m < i} (L_im beta) M_mj)
 // in fp32 products, whose results are the next one's operands as they lie.  (Powers of L
 // beta would need fewer steps, but cancel: binomial coefficients, where keys are alike.)
+// packsT (backward): M's transpose too.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads)
 prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, const float* beta,
-            const int32_t* cu, Gates* gates, unsigned char* packs) {
+            const int32_t* cu, Gates* gates, unsigned char* packs, unsigned char* packsT) {
   using C = DS<T, D, 4, 1>;
   constexpr int kL = 68;  // floats of a row of L
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes];
@@ -169,6 +170,18 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
     parts.set(z);
     Packed<T, kParts>::put(pack, pair, lane, parts);
   }
+  if (packsT) {
+    pack = packsT + slot * (Packed<T, kParts>::kBytes);
+    for (int pair = w; pair < 6; pair += 4) {
+      const int b = pair < 4 ? pair >> 1 : pair - 2, ks = pair < 4 ? pair & 1 : 1;
+      float z[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = ldsL[32 * ks + 8 * g + j][row_of(b, n)];
+      Parts<T, kParts> parts;
+      parts.set(z);
+      Packed<T, kParts>::put(pack, pair, lane, parts);
+    }
+  }
   const u32x4_t* src = reinterpret_cast<const u32x4_t*>(&G);
   u32x4_t* dst = reinterpret_cast<u32x4_t*>(gates + slot);
   if (threadIdx.x < kGateBytes / 16) dst[threadIdx.x] = src[threadIdx.x];
@@ -176,24 +189,34 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
 
 template <typename T, int D>
 using WalkSizes = DS<T, D, D / 16, 1>;
-// What walk_kernel makes: outputs; or a unit's records: what the unit adds to the state
-// (from zeros), and what it does to the state before it (from the identity, without values).
-enum WalkMode { kOutputs, kRecords };
+// What walk_kernel makes: outputs; a unit's records, which are what the unit adds to the state
+// (from zeros) and what it does to the state before it (from the identity, without values);
+// or what the backward needs of the forward, and the strengths' gradient.
+enum WalkMode { kOutputs, kRecords, kBack };
+struct BackOut {
+  const void* dout;
+  const float* F;     // the gradient of u
+  float *S, *E, *do_o, *dbeta;
+  bool final_gradient;  // the final state has one
+};
 
 template <typename T, int D, WalkMode Mode>
 __global__ void __launch_bounds__((WalkSizes<T, D>::NT), 2)
 walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, const int32_t* cu,
             const Gates* gates, const unsigned char* packs, float* recB, float* recM, T* out,
-            float* final_state) {
+            float* final_state, BackOut back) {
   using C = WalkSizes<T, D>;
+  // Back, what is formed from the outputs are sums of both signs in fp32.
+  constexpr int kOut = Mode == kBack ? 3 : kOutParts;
   using M = Packed<T, kParts>;
-  using Pk = Packed<T, kOutParts>;
-  constexpr bool Out = Mode == kOutputs;
+  using Pk = Packed<T, kOut>;
+  constexpr bool Out = Mode != kRecords, Back = Mode == kBack;
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes], ldsV[C::kTileBytes],
       ldsQ[Out ? C::kTileBytes : 16];
   __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBytes], ldsP[Out ? Pk::kBytes : 16];
   __shared__ __attribute__((aligned(16))) Gates G;
   __shared__ int bad[2];  // of this tile and the next
+  __shared__ float sums[2][Back ? C::NW : 1][kDeltaTile];
   const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Span sp;
@@ -204,8 +227,11 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   const size_t record = ((size_t)h * P.units + sp.slot) * (D * D);
   const bool map = !Out && blockIdx.z == 1;
   if (!Out) {
-    // the last unit's record is not needed; nor what the first does to a state of zeros
-    if (sp.last || (map && sp.idx == 0 && !S0)) return;
+    // The scan passes over all units but the last; its first has no map where it starts from
+    // zeros.  The backward's scan, which takes the maps too, begins with the last unit.
+    const bool there = !sp.last && (!map || sp.idx > 0 || S0);
+    const bool back_too = map && back.dout && sp.idx > 0 && (!sp.last || back.final_gradient);
+    if (!there && !back_too) return;
     if (map) S.identity(e0, lane);
     else S.fill(0.0f);
   } else {
@@ -248,6 +274,25 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
       clear_rows<C>(ldsV, good);
       lds_barrier();
     }
+    const size_t slot = slot0 + t0 / kDeltaTile;
+    u32x2_t dob[C::CB][4];  // (fp32: the first two of four)
+    u32x2_t dob2[C::CB][4];
+    f32x4_t f[C::CB][4];
+    if constexpr (Back) {
+      const __amdgpu_buffer_rsrc_t rd =
+          make_rsrc(static_cast<const T*>(back.dout) + (vrow + t0) * D, (uint32_t)(live * C::kRow));
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const uint32_t from = (uint32_t)(row_of(b, n) * C::kRow + (e0 + 16 * c + 4 * g) * C::ES);
+          dob[c][b] = __builtin_amdgcn_raw_buffer_load_b64(rd, from, 0, 0);
+          if constexpr (sizeof(T) == 4) dob2[c][b] = __builtin_amdgcn_raw_buffer_load_b64(rd, from + 8, 0, 0);
+          f[c][b] = *reinterpret_cast<const f32x4_t*>(back.F + (slot * D + e0 + 16 * c + n) * kDeltaTile +
+                                                      row_of(b, 4 * g));
+        }
+      S.store_columns(back.S + slot * (D * D), e0, lane);
+    }
     // Products over key channels: scores of the wave's own tokens, what the state
     // predicts for the tile's keys, and what it answers to its queries (transposed).
     constexpr int NP = C::NW < 4 ? 4 / C::NW : 1;  // blocks of 16 tokens whose scores a wave forms,
@@ -288,7 +333,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
           for (int b = 0; b < 4; ++b) {
             const auto qq = row_units<T, C>(ldsQ, row_of(b, n), ks, g);
 #pragma unroll
-            for (int i = Parts<T, kOutParts>::kN - 1; i >= 0; --i) Num<T>::mma(o[c][b], s.v[i], qq);
+            for (int i = Parts<T, kOut>::kN - 1; i >= 0; --i) Num<T>::mma(o[c][b], s.v[i], qq);
           }
         }
       }
@@ -309,7 +354,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
             const float f = __builtin_amdgcn_exp2f((hi - G.hi[s]) + (lo - G.lo[s]));
             x[j] = s <= t ? p[i][2 * z + (j >> 2)][j & 3] * (P.scale * f) : 0.0f;
           }
-          Parts<T, kOutParts> parts;
+          Parts<T, kOut> parts;
           parts.set(x);
           if (ks == 0 || b >= 2) Pk::put(ldsP, lower_pair(b, ks), lane, parts);
         }
@@ -346,12 +391,31 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
         for (int ks = 0; ks <= (b >> 1); ++ks)
           mma_parts<T>(y[c][b], M::get(ldsM, lower_pair(b, ks), lane), by[ks]);
     }
+    if constexpr (Back) {
+      float x[2][8];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[ks][j] = 0.0f;
+#pragma unroll
+          for (int c = 0; c < C::CB; ++c)
+            x[ks][j] = fmaf(y[c][2 * ks + (j >> 2)][j & 3], f[c][2 * ks + (j >> 2)][j & 3], x[ks][j]);
+        }
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<f32x4_t*>(back.E + (slot * D + e0 + 16 * c + n) * kDeltaTile + row_of(b, 4 * g)) = y[c][b];
+      const float sum = token_sums(x, lane);
+      sums[0][w][token_of(lane)] = sum;
+    }
     if (Out) lds_barrier();  // the scores
     const float whole = G.whole;
 #pragma unroll
     for (int c = 0; c < C::CB; ++c) {
       if constexpr (Out) {
-        Parts<T, kOutParts> u[2];
+        Parts<T, kOut> u[2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           float x[8];
@@ -390,7 +454,23 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
         for (int r = 0; r < 4; ++r) S.s[c][i][r] = fmaf(whole, S.s[c][i][r], x[r]);
       }
     }
-    if constexpr (Out) {
+    if constexpr (Back) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        float x = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C::CB; ++c)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t z = sizeof(T) == 2 ? dob[c][b][r >> 1] : r < 2 ? dob[c][b][r & 1] : dob2[c][b][r & 1];
+            x = fmaf(o[c][b][r], sizeof(T) == 4 ? __uint_as_float(z) : r & 1 ? bf16_hi(z) : bf16_lo(z), x);
+          }
+        x += __shfl_xor(x, 16);
+        x += __shfl_xor(x, 32);
+        sums[1][w][row_of(b, n)] = x;
+      }
+    }
+    if constexpr (Mode == kOutputs) {
       const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + (vrow + t0) * D, (uint32_t)(live * C::kRow));
 #pragma unroll
       for (int c = 0; c < C::CB; ++c)
@@ -411,15 +491,27 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     }
     if (good < live) S.fill(__builtin_nanf(""));
     lds_barrier();
+    if constexpr (Back) {
+      // (the next tile's are written behind two more barriers)
+      if ((int)threadIdx.x < live) {
+        const int64_t at = gate_row(P, sp, h) + t0 + threadIdx.x;
+        float a = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C::NW; ++i) a += sums[0][i][threadIdx.x], b += sums[1][i][threadIdx.x];
+        back.dbeta[at] = a;
+        back.do_o[at] = b;
+      }
+    }
   }
   if (!Out) S.store((map ? recM : recB) + record, e0, lane);
-  else if (final_state && sp.last) S.store(final_state + pair * (D * D), e0, lane);
+  else if (!Back && final_state && sp.last) S.store(final_state + pair * (D * D), e0, lane);
 }
 
 // The records become the state before each unit, in place: S -> M S + B from unit to unit.
 // A workgroup takes 16 value channels, wave w the key channels 16 w ..; the state passes from
-// wave to wave through LDS, in fp32, with fp32 products.
-template <int D>
+// wave to wave through LDS, in fp32, with fp32 products.  Back: from the last unit to the
+// first, with M's transpose, the gradient of the state after each unit.
+template <int D, bool Back>
 __global__ void __launch_bounds__(4 * D)
 scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const float* recM) {
   constexpr int KS = D / 16, kPitch = D + 4;
@@ -432,53 +524,81 @@ scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const 
   const int units = units_of(len, P.unit);
   const size_t record = ((size_t)h * P.units + first) * (D * D);
   float* B = recB + record + (16 * w + 4 * g) * D + e0 + n;
-  const float* M = recM + record + (16 * w + n) * D + 4 * g;
+  const float* M = recM + record + (Back ? 4 * g * D + 16 * w + n : (16 * w + n) * D + 4 * g);
   f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f}, b, m[KS];
   if (S0) {
     const float* p = S0 + ((int64_t)s * P.value_heads + h) * (D * D) + (16 * w + 4 * g) * D + e0 + n;
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[r] = p[r * D];
   }
-  // The last unit has no record, and the first no map if the state before it is zeros.
-  auto fetch = [&](int u) {
-    const bool any = u < units - 1, map = any && (u > 0 || S0);
-    const size_t at = (size_t)u * (D * D);
+  // The i-th unit of the walk.  The last has no record, and the first no map where it starts
+  // from zeros.
+  auto unit = [&](int i) { return Back ? units - 1 - i : i; };
+  auto fetch = [&](int i) {
+    const bool any = i < units - 1, map = any && (i > 0 || S0);
+    const size_t at = (size_t)unit(min(i, units - 1)) * (D * D);
 #pragma unroll
     for (int r = 0; r < 4; ++r) b[r] = any ? B[at + r * D] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < KS; ++i)
-      m[i] = map ? *reinterpret_cast<const f32x4_t*>(M + at + 16 * i) : (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < KS; ++j) {
+      m[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+      if (map) {
+        if constexpr (Back) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) m[j][r] = M[at + (16 * j + r) * D];
+        } else {
+          m[j] = *reinterpret_cast<const f32x4_t*>(M + at + 16 * j);
+        }
+      }
+    }
   };
   fetch(0);
-  for (int u = 0; u < units; ++u) {
-    float* sx = lds[u & 1];
+  for (int i = 0; i < units; ++i) {
+    float* sx = lds[i & 1];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) B[(size_t)u * (D * D) + r * D] = x[r];
-    if (u + 1 == units) break;
+    for (int r = 0; r < 4; ++r) B[(size_t)unit(i) * (D * D) + r * D] = x[r];
+    if (i + 1 == units) break;
     *reinterpret_cast<f32x4_t*>(&sx[n * kPitch + 16 * w + 4 * g]) = x;
     lds_barrier();
     f32x4_t z[2] = {b, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&sx[n * kPitch + 16 * i + 4 * g]);
+    for (int j = 0; j < KS; ++j) {
+      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&sx[n * kPitch + 16 * j + 4 * g]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i][r], y[r], z[r & 1], 0, 0, 0);
+      for (int r = 0; r < 4; ++r) z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[j][r], y[r], z[r & 1], 0, 0, 0);
     }
-    fetch(u + 1);
+    fetch(i + 1);
     x = z[0] + z[1];
   }
 }
 
-template <typename F>
-gbla_status by_type(const DeltaPlan& p, F f) {
-  auto dims = [&](auto t) {
-    if (p.d == 32) f(t, std::integral_constant<int, 32>{});
-    else if (p.d == 64) f(t, std::integral_constant<int, 64>{});
-    else f(t, std::integral_constant<int, 128>{});
-  };
-  if (p.dtype == GBLA_BF16) dims(uint16_t{});
-  else dims(float{});
-  return hipGetLastError() == hipSuccess ? GBLA_OK : GBLA_ERR_HIP;
+}  // namespace
+
+namespace {
+
+// The launches before the outputs: gates and triangles; records and the states between units.
+template <typename T, int D>
+void launch_prep(const DeltaPlan& p, const void* k, const float* log_decay, const float* beta, const int32_t* cu,
+                 unsigned char* base, bool backward, hipStream_t st) {
+  if (p.tokens > 0)
+    hipLaunchKernelGGL((prep_kernel<T, D>), dim3(p.tiles, p.value_heads), dim3(kThreads), 0, st, p, tile_spans(p),
+                       (const T*)k, log_decay, beta, cu, reinterpret_cast<Gates*>(base + p.off_gates),
+                       base + p.off_pack, backward ? base + p.off_packT : nullptr);
+}
+template <typename T, int D, WalkMode Mode>
+void launch_walk(const DeltaPlan& p, const void* q, const void* k, const void* v, const float* S0, const int32_t* cu,
+                 unsigned char* base, void* out, float* final_state, const BackOut& back, hipStream_t st) {
+  hipLaunchKernelGGL((walk_kernel<T, D, Mode>), dim3(p.grid_units, p.value_heads, Mode == kRecords ? 2 : 1),
+                     dim3((WalkSizes<T, D>::NT)), 0, st, p, (const T*)q, (const T*)k, (const T*)v, S0, cu,
+                     reinterpret_cast<const Gates*>(base + p.off_gates), base + p.off_pack,
+                     reinterpret_cast<float*>(base + p.off_B), reinterpret_cast<float*>(base + p.off_M), (T*)out,
+                     final_state, back);
+}
+template <int D, bool Back>
+void launch_scan(const DeltaPlan& p, const int32_t* cu, const float* S0, unsigned char* base, hipStream_t st) {
+  hipLaunchKernelGGL((scan_kernel<D, Back>), dim3(p.nseq * (D / 16), p.value_heads), dim3(4 * D), 0, st, p, cu, S0,
+                     reinterpret_cast<float*>(base + (Back ? p.off_D : p.off_B)),
+                     reinterpret_cast<const float*>(base + p.off_M));
 }
 
 }  // namespace
@@ -488,28 +608,55 @@ gbla_status launch_delta_forward(const DeltaPlan& p, const void* q, const void* 
                                  const int32_t* cu, void* ws, void* out, float* final_state,
                                  hipStream_t st) {
   unsigned char* base = static_cast<unsigned char*>(ws);
-  Gates* gates = reinterpret_cast<Gates*>(base + p.off_gates);
-  unsigned char* packs = base + p.off_pack;
-  float* recB = reinterpret_cast<float*>(base + p.off_B);
-  float* recM = reinterpret_cast<float*>(base + p.off_M);
   return by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    const auto walk = [&](auto kernel, int z) {
-      hipLaunchKernelGGL(kernel, dim3(p.grid_units, p.value_heads, z), dim3((WalkSizes<T, D>::NT)), 0, st, p,
-                         (const T*)q, (const T*)k, (const T*)v, S0, cu, gates, packs, recB, recM, (T*)out,
-                         final_state);
-    };
-    if (p.tokens > 0)
-      hipLaunchKernelGGL((prep_kernel<T, D>), dim3(p.tiles, p.value_heads), dim3(kThreads), 0, st, p, tile_spans(p),
-                         (const T*)k, log_decay, beta, cu, gates, packs);
+    launch_prep<T, D>(p, k, log_decay, beta, cu, base, false, st);
     if (!p.single) {
-      walk(walk_kernel<T, D, kRecords>, 2);
-      hipLaunchKernelGGL((scan_kernel<D>), dim3(p.nseq * (D / 16), p.value_heads), dim3(4 * D), 0, st, p, cu, S0,
-                         recB, recM);
+      launch_walk<T, D, kRecords>(p, q, k, v, S0, cu, base, nullptr, nullptr, {}, st);
+      launch_scan<D, false>(p, cu, S0, base, st);
     }
-    walk(walk_kernel<T, D, kOutputs>, 1);
+    launch_walk<T, D, kOutputs>(p, q, k, v, S0, cu, base, out, final_state, {}, st);
   });
+}
+
+gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void* k, const void* v,
+                                  const float* log_decay, const float* beta, const float* S0,
+                                  const int32_t* cu, const void* dout, const float* dfinal, void* ws,
+                                  void* dq, void* dk, void* dv, float* dlog_decay, float* dbeta,
+                                  float* dS0, hipStream_t st) {
+  unsigned char* base = static_cast<unsigned char*>(ws);
+  auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+  // (the decays' gradient takes it too)
+  if (!dS0 && S0) dS0 = floats(p.off_dS0);
+  gbla_status done = by_type(p, [&](auto t, auto dim) {
+    using T = decltype(t);
+    constexpr int D = decltype(dim)::value;
+    const BackOut back = {dout,         floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_do_o),
+                          dbeta, dfinal != nullptr};
+    launch_prep<T, D>(p, k, log_decay, beta, cu, base, true, st);
+    if (!p.single) {
+      launch_walk<T, D, kRecords>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
+      launch_scan<D, false>(p, cu, S0, base, st);
+    }
+  });
+  if (done == GBLA_OK) done = launch_delta_back_records(p, q, k, cu, dout, ws, st);
+  if (done != GBLA_OK) return done;
+  done = by_type(p, [&](auto, auto dim) {
+    constexpr int D = decltype(dim)::value;
+    if (!p.single) launch_scan<D, true>(p, cu, dfinal, base, st);
+  });
+  if (done == GBLA_OK) done = launch_delta_back_walk(p, q, k, v, cu, dout, dfinal, ws, dS0, st);
+  if (done != GBLA_OK) return done;
+  done = by_type(p, [&](auto t, auto dim) {
+    using T = decltype(t);
+    constexpr int D = decltype(dim)::value;
+    const BackOut back = {dout,         floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_do_o),
+                          dbeta, dfinal != nullptr};
+    launch_walk<T, D, kBack>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
+  });
+  if (done != GBLA_OK) return done;
+  return launch_delta_grads(p, q, k, S0, cu, dout, ws, dq, dk, dv, dlog_decay, dS0, st);
 }
 
 }  // namespace gbla

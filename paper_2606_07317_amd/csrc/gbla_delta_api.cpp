@@ -43,6 +43,33 @@ gbla_status gbla_delta_forward(const gbla_delta_shape* shape, const void* q, con
                                     workspace, out, final_state, static_cast<hipStream_t>(stream));
 }
 
+size_t gbla_delta_backward_workspace_bytes(const gbla_delta_shape* shape) {
+  return larger(delta_bytes(shape, false, true), delta_bytes(shape, true, true));
+}
+
+size_t gbla_delta_backward_ragged_workspace_bytes(const gbla_delta_shape* shape) {
+  return delta_bytes(shape, true, true);
+}
+
+gbla_status gbla_delta_backward(const gbla_delta_shape* shape, const void* q, const void* k,
+                                const void* v, const float* log_decay, const float* beta,
+                                const float* initial_state, const int32_t* cu_seqlens,
+                                const void* dout, const float* dfinal_state, void* workspace,
+                                size_t workspace_bytes, void* dq, void* dk, void* dv,
+                                float* dlog_decay, float* dbeta, float* dinitial_state,
+                                void* stream) {
+  gbla::DeltaPlan p;
+  GBLA_TRY(gbla::make_delta_plan(shape, cu_seqlens != nullptr, true, &p));
+  GBLA_TRY(rows_present(p.tokens, {q, k, v, dout, dq, dk, dv}));
+  GBLA_TRY(rows_present(p.tokens, {log_decay, beta, dlog_decay, dbeta}, 4));
+  GBLA_TRY(optional({initial_state, dfinal_state, dinitial_state}));
+  GBLA_TRY(optional({cu_seqlens}, 4));
+  GBLA_TRY(scratch(workspace, workspace_bytes, p.total_bytes));
+  return gbla::launch_delta_backward(p, q, k, v, log_decay, beta, initial_state, cu_seqlens, dout,
+                                     dfinal_state, workspace, dq, dk, dv, dlog_decay, dbeta,
+                                     dinitial_state, static_cast<hipStream_t>(stream));
+}
+
 gbla_status gbla_delta_step(const gbla_delta_shape* shape, const void* q, const void* k,
                             const void* v, const float* log_decay, const float* beta,
                             const int32_t* state_indices, int32_t slots, float* state, void* out,

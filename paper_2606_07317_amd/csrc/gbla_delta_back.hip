@@ -1,0 +1,278 @@
+// gbla_delta_back.hip -- the gated delta rule's backward, from the last tile to the first
+// (gfx950): the gradients of u, and of the states.
+//
+// With N the gradient of the state after a tile, and P, M, c as in the forward
+// (gbla_delta.hip; P the tile's scaled and decayed scores):
+//   du = P^T do + e^(c_L - c) K N
+//   f  = du - M^T (beta du),    dv = beta f,    dbeta = f e   (e from the forward's tiles)
+//   N_in = e^c_L N + scale (e^c Q)^T do - (e^c K)^T dv
+// which needs nothing of the forward's states.  As there, a wave owns 16 value channels and
+// all that one product hands to the next stays in its registers; units run at the same time,
+// joined by the transposes of the forward's maps.
+//
+// All sums here form fp32 results of both signs (the gradients of the gates): everything that
+// is computed in fp32 enters its products in three parts.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gbla_delta_tiles.h"
+
+namespace gbla {
+namespace {
+
+constexpr int kParts = 3;
+template <typename T, int D>
+using BackSizes = DS<T, D, D / 16, 1>;
+
+struct BackArrays {
+  const Gates* gates;
+  const unsigned char* packs;  // M's transposes
+  float* recD;                 // the gradient of the state after each unit; what it adds (Records)
+  float *N, *F, *dv_v;
+};
+
+// Records: what the unit's own tokens add to the gradient of the state before it, into recD.
+template <typename T, int D, bool Records>
+__global__ void __launch_bounds__((BackSizes<T, D>::NT), 2)
+back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, const int32_t* cu, const float* dfinal,
+            BackArrays a, float* dS0) {
+  using C = BackSizes<T, D>;
+  using M = Packed<T, kParts>;
+  constexpr bool All = !Records;
+  __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes], ldsQ[C::kTileBytes],
+      ldsO[C::kTileBytes], ldsV[All ? C::kTileBytes : 16];
+  __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBytes], ldsP[M::kBytes];
+  __shared__ __attribute__((aligned(16))) Gates G;
+  __shared__ float sums[All ? C::NW : 1][kDeltaTile];
+  const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Span sp;
+  if (!find_span<C::NT>(P, cu, blockIdx.x, &sp)) return;
+  if (Records && sp.idx == 0) return;  // nothing comes before it
+  const int64_t pair = (int64_t)sp.s * P.value_heads + h;
+  const int e0 = 16 * C::CB * w;
+  const size_t record = ((size_t)h * P.units + sp.slot) * (D * D);
+  Columns16<T, C> N;
+  const float* init = Records                                ? nullptr
+                      : !P.single && (dfinal || !sp.last) ? a.recD + record
+                      : dfinal                               ? dfinal + pair * (D * D)
+                                                             : nullptr;
+  if (init) N.load(init, e0, lane);
+  else N.fill(0.0f);
+
+  const int64_t krow = first_row(P, sp, P.heads, h / P.group), vrow = first_row(P, sp, P.value_heads, h);
+  const size_t slot0 = (size_t)h * P.tiles + tile_slot(P, sp.row0, sp.s);
+  RowsLoad<T, C> lk, lq, lo, lv;
+  BlockLoad<C, M::kBytes> lm;
+  BlockLoad<C, kGateBytes> lg;
+  auto fetch = [&](int t) {  // (none before the unit's first tile)
+    const int left = t < sp.begin ? 0 : sp.end - t;
+    const int64_t row = max(t, 0);
+    lk.load(k + (krow + row) * D, left);
+    lq.load(q + (krow + row) * D, left);
+    lo.load(dout + (vrow + row) * D, left);
+    if (All) lv.load(v + (vrow + row) * D, left);
+    const size_t slot = slot0 + row / kDeltaTile;
+    lm.load(a.packs + slot * M::kBytes, left > 0);
+    lg.load(a.gates + slot, left > 0);
+  };
+  const int last = sp.begin < sp.end ? sp.begin + (sp.end - 1 - sp.begin) / kDeltaTile * kDeltaTile : sp.begin - 1;
+  if (sp.begin < sp.end) fetch(last);
+  for (int t0 = last; t0 >= sp.begin; t0 -= kDeltaTile) {
+    const int live = min(kDeltaTile, sp.end - t0);
+    const size_t slot = slot0 + t0 / kDeltaTile;
+    lk.store(ldsK);
+    lq.store(ldsQ);
+    lo.store(ldsO);
+    if (All) lv.store(ldsV);
+    lm.store(ldsM);
+    lg.store(&G);
+    lds_barrier();
+    fetch(t0 - kDeltaTile);
+    if (All) N.store_columns(a.N + slot * (D * D), e0, lane);
+    // Scores [later tokens][own earlier tokens] and, with the gradient of the state, of u.
+    constexpr int NP = C::NW < 4 ? 4 / C::NW : 1;
+    constexpr int PG = C::NW == 8 ? 1 : 2;
+    const int pg0 = C::NW == 8 ? w >> 2 : 0;
+    f32x4_t x[C::CB][4], p[NP][2 * PG];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c) x[c][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int b = 0; b < 2 * PG; ++b) p[i][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) {
+      typename Num<T>::V8 kk[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) kk[b] = row_units<T, C>(ldsK, row_of(b, n), ks, g);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const auto own = row_units<T, C>(ldsK, row_of((w + C::NW * i) & 3, n), ks, g);
+#pragma unroll
+        for (int b = 0; b < 2 * PG; ++b)
+          Num<T>::mma(p[i][b], row_units<T, C>(ldsQ, row_of(2 * pg0 + b, n), ks, g), own);
+      }
+#pragma unroll
+      for (int c = 0; c < C::CB; ++c) {
+        const Parts<T, kParts> s = N.template operand<kParts>(c, ks);
+#pragma unroll
+        for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) Num<T>::mma(x[c][b], kk[b], s.v[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int b = (w + C::NW * i) & 3, s = row_of(b, n);
+      const float hi = G.hi[s], lo = G.lo[s];
+#pragma unroll
+      for (int z = 0; z < PG; ++z) {
+        const int ks = pg0 + z;
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = 32 * ks + 8 * g + j;
+          const float f = decay_between(G, t, hi, lo);
+          y[j] = s <= t ? p[i][2 * z + (j >> 2)][j & 3] * (P.scale * f) : 0.0f;
+        }
+        Parts<T, kParts> parts;
+        parts.set(y);
+        if (ks == 1 || b < 2) M::put(ldsP, upper_pair(b, ks), lane, parts);
+      }
+    }
+    lds_barrier();  // the scores
+    float beta[2][8], into[2][8], part[2][8];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        beta[ks][j] = G.beta[32 * ks + 8 * g + j];
+        into[ks][j] = G.into[32 * ks + 8 * g + j];
+        part[ks][j] = 0.0f;
+      }
+    const float whole = G.whole;
+#pragma unroll
+    for (int c = 0; c < C::CB; ++c) {
+      typename Num<T>::V8 o[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) o[ks] = value_column<T, C>(ldsO, C::CB * w + c, ks, lane);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[c][b][r] *= G.rest[row_of(b, 4 * g + r)];
+#pragma unroll
+        for (int ks = b >> 1; ks < 2; ++ks) {
+          const Parts<T, kParts> y = M::get(ldsP, upper_pair(b, ks), lane);
+#pragma unroll
+          for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i) Num<T>::mma(x[c][b], y.v[i], o[ks]);
+        }
+      }
+      Parts<T, kParts> y[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        float z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = beta[ks][j] * x[c][2 * ks + (j >> 2)][j & 3];
+        y[ks].set(z);
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int ks = b >> 1; ks < 2; ++ks) mma_parts<T>(x[c][b], M::get(ldsM, upper_pair(b, ks), lane), y[ks]);
+      // x: the gradient of u without the tile's later ones, f
+      Parts<T, kParts> up[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        float z[8], dv[8];
+        Num<T>::widen(o[ks], z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          dv[j] = beta[ks][j] * x[c][2 * ks + (j >> 2)][j & 3];
+          z[j] *= P.scale * into[ks][j];
+        }
+        up[ks].set(z);
+        if constexpr (All) {
+          Num<T>::widen(value_column<T, C>(ldsV, C::CB * w + c, ks, lane), z);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) part[ks][j] = fmaf(dv[j], z[j], part[ks][j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dv[j] *= -into[ks][j];
+        y[ks].set(dv);
+      }
+      if constexpr (All) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<f32x4_t*>(a.F + (slot * D + e0 + 16 * c + n) * kDeltaTile + row_of(b, 4 * g)) = x[c][b];
+      }
+#pragma unroll
+      for (int i = 0; i < C::NB; ++i) {
+        f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          const auto kc = key_column<T, C>(ldsK, i, kt, lane), qc = key_column<T, C>(ldsQ, i, kt, lane);
+#pragma unroll
+          for (int j = Parts<T, kParts>::kN - 1; j >= 0; --j) {
+            Num<T>::mma(z, kc, y[kt].v[j]);
+            Num<T>::mma(z, qc, up[kt].v[j]);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) N.s[c][i][r] = fmaf(whole, N.s[c][i][r], z[r]);
+      }
+    }
+    if constexpr (All) {
+      const float sum = token_sums(part, lane);
+      sums[w][token_of(lane)] = sum;
+    }
+    lds_barrier();
+    if constexpr (All) {
+      // (the next tile's are written behind two more barriers)
+      if ((int)threadIdx.x < live) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C::NW; ++i) sum += sums[i][threadIdx.x];
+        a.dv_v[gate_row(P, sp, h) + t0 + threadIdx.x] = sum;
+      }
+    }
+  }
+  if (Records) N.store(a.recD + record, e0, lane);
+  else if (dS0 && sp.idx == 0) N.store(dS0 + pair * (D * D), e0, lane);
+}
+
+BackArrays arrays(const DeltaPlan& p, void* ws) {
+  unsigned char* base = static_cast<unsigned char*>(ws);
+  auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+  return {reinterpret_cast<const Gates*>(base + p.off_gates), base + p.off_packT, floats(p.off_D), floats(p.off_N),
+          floats(p.off_F), floats(p.off_dv_v)};
+}
+
+}  // namespace
+
+gbla_status launch_delta_back_records(const DeltaPlan& p, const void* q, const void* k, const int32_t* cu,
+                                      const void* dout, void* ws, hipStream_t st) {
+  if (p.single) return GBLA_OK;
+  return by_type(p, [&](auto t, auto dim) {
+    using T = decltype(t);
+    constexpr int D = decltype(dim)::value;
+    hipLaunchKernelGGL((back_kernel<T, D, true>), dim3(p.grid_units, p.value_heads), dim3((BackSizes<T, D>::NT)), 0,
+                       st, p, (const T*)q, (const T*)k, (const T*)nullptr, (const T*)dout, cu, (const float*)nullptr,
+                       arrays(p, ws), (float*)nullptr);
+  });
+}
+
+gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void* k, const void* v,
+                                   const int32_t* cu, const void* dout, const float* dfinal, void* ws,
+                                   float* dS0, hipStream_t st) {
+  return by_type(p, [&](auto t, auto dim) {
+    using T = decltype(t);
+    constexpr int D = decltype(dim)::value;
+    hipLaunchKernelGGL((back_kernel<T, D, false>), dim3(p.grid_units, p.value_heads), dim3((BackSizes<T, D>::NT)), 0,
+                       st, p, (const T*)q, (const T*)k, (const T*)v, (const T*)dout, cu, dfinal, arrays(p, ws), dS0);
+  });
+}
+
+}  // namespace gbla

@@ -82,6 +82,20 @@ gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backwar
   const size_t states = (size_t)cap * q.value_heads * q.d * q.d * sizeof(float);
   q.off_B = take(states);
   q.off_M = take(states);
+  if (backward) {
+    const size_t each = (size_t)most * q.value_heads, state = (size_t)q.d * q.d * sizeof(float);
+    const size_t vectors = (size_t)q.d * kDeltaTile * sizeof(float);
+    const size_t gate = (size_t)q.tokens * q.value_heads * sizeof(float);
+    q.off_packT = take(each * kPackBytes);
+    q.off_D = take(states);
+    q.off_S = take(each * state);
+    q.off_N = take(each * state);
+    q.off_E = take(each * vectors);
+    q.off_F = take(each * vectors);
+    q.off_do_o = take(gate);
+    q.off_dv_v = take(gate);
+    q.off_dS0 = take((size_t)q.nseq * q.value_heads * state);
+  }
   q.total_bytes = off;
   *p = q;
   return GBLA_OK;

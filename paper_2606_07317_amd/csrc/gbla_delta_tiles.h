@@ -176,6 +176,7 @@ __device__ __forceinline__ void clear_rows(unsigned char* lds, int from) {
 // A 64 x 64 lower (upper) triangle as operands: the six (row block b, K step ks) that are
 // not all zero, each [pieces of 16 bytes][lane]: N bf16 parts, or eight fp32 values.
 __device__ __forceinline__ int lower_pair(int b, int ks) { return b < 2 ? b : 2 * b - 2 + ks; }
+__device__ __forceinline__ int upper_pair(int b, int ks) { return b < 2 ? 2 * b + ks : b + 2; }
 template <typename T, int N>
 struct Packed {
   static constexpr int kPieces = sizeof(T) == 2 ? N : 2;
@@ -262,6 +263,16 @@ struct Columns16 {
         for (int r = 0; r < 4; ++r)
           m[row_of(i, 4 * (lane >> 4) + r) * C::D + col0 + 16 * c + (lane & 15)] = s[c][i][r];
   }
+  // m: [column][row]
+  __device__ __forceinline__ void store_columns(float* m, int col0, int lane) const {
+#pragma unroll
+    for (int c = 0; c < C::CB; ++c) {
+      float* to = m + (col0 + 16 * c + (lane & 15)) * C::D + 8 * (lane >> 4);
+#pragma unroll
+      for (int i = 0; i < C::NB; ++i)
+        *reinterpret_cast<f32x4_t*>(to + 32 * (i >> 1) + 4 * (i & 1)) = s[c][i];
+    }
+  }
   // K step ks of column block c as an operand.
   template <int N>
   __device__ __forceinline__ Parts<T, N> operand(int c, int ks) const {
@@ -272,6 +283,28 @@ struct Columns16 {
     return p;
   }
 };
+
+// Sums over a wave's 16 value channels (lanes n) of a lane's values of its 16 tokens, x[ks][j]
+// of token 32 ks + 8 g + j: halving exchanges, after which lane n has token
+// 32 (n / 8) + 8 g + n % 8's.
+template <int W, int O>
+__device__ __forceinline__ void halve(float* v, int lane) {
+  const bool high = lane & O;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const float keep = high ? v[i + W] : v[i], give = high ? v[i] : v[i + W];
+    v[i] = keep + __shfl_xor(give, O);
+  }
+}
+__device__ __forceinline__ float token_sums(float (&x)[2][8], int lane) {
+  float* v = &x[0][0];
+  halve<8, 8>(v, lane);
+  halve<4, 4>(v, lane);
+  halve<2, 2>(v, lane);
+  halve<1, 1>(v, lane);
+  return v[0];
+}
+__device__ __forceinline__ int token_of(int lane) { return 32 * ((lane >> 3) & 1) + 8 * (lane >> 4) + (lane & 7); }
 
 // The tiles of a plan as spans of their own.
 struct TileSpans {
@@ -285,6 +318,18 @@ __device__ __forceinline__ int tile_slot(const DeltaPlan& P, int64_t c, int s) {
 // A tile's gates [rows][tile] start: row of its first token in a [B,V,n] or [V,T] array.
 __device__ __forceinline__ int64_t gate_row(const DeltaPlan& P, const Span& s, int h) {
   return P.ragged ? (int64_t)h * P.rows + s.row0 : ((int64_t)s.s * P.value_heads + h) * P.rows;
+}
+
+template <typename F>
+inline gbla_status by_type(const DeltaPlan& p, F f) {
+  auto dims = [&](auto t) {
+    if (p.d == 32) f(t, std::integral_constant<int, 32>{});
+    else if (p.d == 64) f(t, std::integral_constant<int, 64>{});
+    else f(t, std::integral_constant<int, 128>{});
+  };
+  if (p.dtype == GBLA_BF16) dims(uint16_t{});
+  else dims(float{});
+  return hipGetLastError() == hipSuccess ? GBLA_OK : GBLA_ERR_HIP;
 }
 
 }  // namespace gbla

@@ -134,11 +134,14 @@ def load_library(path: str = LIB_PATH):
     lib.gbla_decay_step.argtypes = [DP] + [P] * 5 + [ctypes.c_int32] + [P] * 3
     lib.gbla_decay_step.restype = ctypes.c_int
     EP = ctypes.POINTER(DeltaShape)
-    for name in ("gbla_delta_workspace_bytes", "gbla_delta_ragged_workspace_bytes"):
+    for name in ("gbla_delta_workspace_bytes", "gbla_delta_backward_workspace_bytes",
+                 "gbla_delta_ragged_workspace_bytes", "gbla_delta_backward_ragged_workspace_bytes"):
         getattr(lib, name).argtypes = [EP]
         getattr(lib, name).restype = sz
     lib.gbla_delta_forward.argtypes = [EP] + [P] * 8 + [sz] + [P] * 3
     lib.gbla_delta_forward.restype = ctypes.c_int
+    lib.gbla_delta_backward.argtypes = [EP] + [P] * 10 + [sz] + [P] * 7
+    lib.gbla_delta_backward.restype = ctypes.c_int
     lib.gbla_delta_step.argtypes = [EP] + [P] * 6 + [ctypes.c_int32] + [P] * 3
     lib.gbla_delta_step.restype = ctypes.c_int
     lib.gbla_status_string.argtypes = [ctypes.c_int]
@@ -848,6 +851,10 @@ def delta_workspace_bytes(shape: DeltaShape, ragged: bool = False) -> int:
     return _scratch("gbla_delta", shape, ragged)
 
 
+def delta_backward_workspace_bytes(shape: DeltaShape, ragged: bool = False) -> int:
+    return _scratch("gbla_delta_backward", shape, ragged)
+
+
 def _check_delta(v, log_decay, beta, shape, states):
     dev = v.device
     _want(log_decay, "log_decay", v.shape[:-1], torch.float32, dev)
@@ -887,6 +894,38 @@ def delta_attention(q, k, v, log_decay, beta, scale: Optional[float] = None, ini
             _ptr(given), _current(dev))
     _raise(st, "gbla_delta_forward")
     return out, given
+
+
+def delta_attention_backward(q, k, v, log_decay, beta, dout, scale: Optional[float] = None,
+                             initial_state=None, dfinal_state=None, cu_seqlens=None, max_seqlen=None,
+                             workspace=None, grads: Optional[dict] = None, stream=None) -> dict:
+    """Gradients of sum(out * dout) + sum(final_state * dfinal_state) for the inputs of
+    delta_attention: a dict with dq, dk, dv (in q's type), dlog_decay, dbeta (fp32) and, if
+    initial_state is given, dinitial_state (fp32).  ``grads`` may hold outputs under those
+    names; dinitial_state may be dfinal_state itself."""
+    shape = delta_shape(q, k, v, scale, cu_seqlens, max_seqlen)
+    g = dict(grads or {})
+    _check_delta(v, log_decay, beta, shape,
+                 ((initial_state, "initial_state"), (dfinal_state, "dfinal_state"),
+                  (g.get("dinitial_state"), "dinitial_state")))
+    dev = q.device
+    _want(dout, "dout", v.shape, q.dtype, dev)
+    need = delta_backward_workspace_bytes(shape, cu_seqlens is not None)
+    with _on(dev, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check_ws(workspace, dev, need)
+        for name, like in (("dq", q), ("dk", k), ("dv", v), ("dlog_decay", log_decay), ("dbeta", beta)):
+            g[name] = _like(g.get(name), name, like)
+        if initial_state is not None and g.get("dinitial_state") is None:
+            g["dinitial_state"] = torch.empty_like(initial_state)
+        st = load_library().gbla_delta_backward(
+            ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(beta),
+            _ptr(initial_state), _ptr(cu_seqlens), _ptr(dout), _ptr(dfinal_state), _ptr(workspace),
+            workspace.numel(), _ptr(g["dq"]), _ptr(g["dk"]), _ptr(g["dv"]), _ptr(g["dlog_decay"]),
+            _ptr(g["dbeta"]), _ptr(g.get("dinitial_state")), _current(dev))
+    _raise(st, "gbla_delta_backward")
+    return g
 
 
 def delta_step(q, k, v, log_decay, beta, state, state_indices=None, scale: Optional[float] = None,
