@@ -58,7 +58,9 @@ typedef enum {
   GBLA_ERR_HIP = 5               /* the HIP runtime reported an error         */
 } gbla_status;
 
-typedef enum { GBLA_F32 = 0, GBLA_BF16 = 1 } gbla_dtype;
+/* GBLA_E4M3 (four bits of exponent, three of fraction, at most 448): outputs of
+ * gbla_add_norm alone. */
+typedef enum { GBLA_F32 = 0, GBLA_BF16 = 1, GBLA_E4M3 = 2 } gbla_dtype;
 
 /*
  * Ablation switches, the rows of the paper's ablation table (Section 3,
@@ -543,6 +545,53 @@ gbla_status gbla_delta_step(const gbla_delta_shape* shape, const void* q, const 
                             const void* v, const float* log_decay, const float* beta,
                             const int32_t* state_indices, int32_t slots, float* state, void* out,
                             void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * The residual stream's norm: what stands before every layer of a decoder block.
+ * ---------------------------------------------------------------------------
+ */
+typedef struct {
+  int64_t rows;      /* >= 0: tokens                                              */
+  int32_t width;     /* channels: a multiple of 8, at most 16384                  */
+  int32_t dtype;     /* gbla_dtype of x, residual, sum and the gradients          */
+  int32_t out_dtype; /* of out: dtype, or GBLA_E4M3 (not looked at by the backward) */
+  int32_t group;     /* GBLA_E4M3: channels of a scale, 128 (dividing the width) or 0, one
+                        scale a row; else 0 (not looked at by the backward)       */
+  float eps;         /* finite and >= 0                                           */
+} gbla_norm_shape;
+
+/*
+ * The residual's addition and the RMS norm over the width, row by row:
+ *   s = x + residual, rounded to dtype (x if residual is NULL)
+ *   y = s / sqrt(mean_c s_c^2 + eps) * weight        (of the rounded s; squares summed in fp32)
+ *   x, residual    [rows, width]; residual or NULL
+ *   weight         fp32 [width]
+ *   sum            [rows, width] takes s, or NULL (not wanted)
+ *   out            [rows, width] takes y: rounded to dtype, or as GBLA_E4M3 with
+ *   scales         fp32 [rows] or [rows, width / 128]: the largest |y| of the row or the 128
+ *                  channels over 448, at least 2^-126; out = y / scale, rounded to nearest even
+ * sum, and out of x's type, may be the buffer of x or of residual (not both the same one).  A
+ * value that is not finite reaches its own row alone; in 8 bits every value of a row (or of 128
+ * channels) with such a y stands for NaN.
+ */
+gbla_status gbla_add_norm(const gbla_norm_shape* shape, const void* x, const void* residual,
+                          const float* weight, void* sum, void* out, float* scales, void* stream);
+
+/* Scratch bytes of gbla_add_norm_backward; 0 if the shape is not accepted. */
+size_t gbla_add_norm_backward_workspace_bytes(const gbla_norm_shape* shape);
+
+/*
+ * Gradients of L = sum(y * dout) + sum(s * dsum), from the s that the forward left:
+ *   dout     [rows, width]           dsum    [rows, width] or NULL (zeros)
+ *   dx       [rows, width], of x and of residual alike; may be the buffer of dout or dsum
+ *   dweight  fp32 [width], summed over all rows in an order fixed by the shape
+ * Roundings (of s, and of y to 8 bits) count as the identity.
+ */
+gbla_status gbla_add_norm_backward(const gbla_norm_shape* shape, const void* sum,
+                                   const float* weight, const void* dout, const void* dsum,
+                                   void* workspace, size_t workspace_bytes, void* dx,
+                                   float* dweight, void* stream);
 
 /* A static, human-readable name of a status code (never NULL). */
 const char* gbla_status_string(gbla_status status);

@@ -25,7 +25,8 @@ SOURCES = [os.path.join(CSRC, "gbla_kernels.hip"), os.path.join(CSRC, "gbla_stre
            os.path.join(CSRC, "gbla_decay_plan.cpp"), os.path.join(CSRC, "gbla_decay_api.cpp"),
            os.path.join(CSRC, "gbla_delta.hip"), os.path.join(CSRC, "gbla_delta_step.hip"),
            os.path.join(CSRC, "gbla_delta_back.hip"), os.path.join(CSRC, "gbla_delta_grads.hip"),
-           os.path.join(CSRC, "gbla_delta_plan.cpp"), os.path.join(CSRC, "gbla_delta_api.cpp")]
+           os.path.join(CSRC, "gbla_delta_plan.cpp"), os.path.join(CSRC, "gbla_delta_api.cpp"),
+           os.path.join(CSRC, "gbla_norm.hip"), os.path.join(CSRC, "gbla_norm_api.cpp")]
 
 # Packed fp32 VALU ops are switched off for all device code; hipcc's host
 # pass warns that it does not know the feature, which is harmless.

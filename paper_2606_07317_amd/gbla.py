@@ -22,6 +22,7 @@ HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "gbla.h")
 
 GBLA_F32 = 0
 GBLA_BF16 = 1
+GBLA_E4M3 = 2  # outputs of add_rms_norm_e4m3
 # Ablation switches (shape.flags); all three together is plain BLA, Eq. (1).
 NO_GATE = 1   # uniform key gates; gate_logits may be None
 NO_CONV = 2   # identity Conv1D; conv_w may be None
@@ -69,6 +70,11 @@ class DeltaShape(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("seqlen", ctypes.c_int32), ("heads", ctypes.c_int32),
                 ("value_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("max_seqlen", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("group", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -144,6 +150,13 @@ def load_library(path: str = LIB_PATH):
     lib.gbla_delta_backward.restype = ctypes.c_int
     lib.gbla_delta_step.argtypes = [EP] + [P] * 6 + [ctypes.c_int32] + [P] * 3
     lib.gbla_delta_step.restype = ctypes.c_int
+    NP = ctypes.POINTER(NormShape)
+    lib.gbla_add_norm.argtypes = [NP] + [P] * 7
+    lib.gbla_add_norm.restype = ctypes.c_int
+    lib.gbla_add_norm_backward_workspace_bytes.argtypes = [NP]
+    lib.gbla_add_norm_backward_workspace_bytes.restype = sz
+    lib.gbla_add_norm_backward.argtypes = [NP] + [P] * 5 + [sz] + [P] * 3
+    lib.gbla_add_norm_backward.restype = ctypes.c_int
     lib.gbla_status_string.argtypes = [ctypes.c_int]
     lib.gbla_status_string.restype = ctypes.c_char_p
     if path == LIB_PATH:
@@ -957,3 +970,96 @@ def delta_step(q, k, v, log_decay, beta, state, state_indices=None, scale: Optio
             _ptr(state_indices), slots, _ptr(state), _ptr(out), _current(dev))
     _raise(st, "gbla_delta_step")
     return out
+
+
+# ---------------------------------------------------------------------------
+# The residual stream's norm.
+# ---------------------------------------------------------------------------
+def norm_shape(x, eps: float = 1e-6, out_dtype: Optional[int] = None, group: int = 0) -> NormShape:
+    _check(x, "x")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must be [..., width]")
+    width = x.shape[-1]
+    code = _dtype_code(x)
+    return NormShape(x.numel() // width, width, code, code if out_dtype is None else out_dtype, int(group),
+                     float(eps))
+
+
+def _add_norm(shape, x, weight, residual, total, out, scales, stream):
+    dev = x.device
+    _want(weight, "weight", (shape.width,), torch.float32, dev)
+    if residual is not None:
+        _want(residual, "residual", x.shape, x.dtype, dev)
+    if total is not None:
+        _want(total, "sum_out", x.shape, x.dtype, dev)
+    with _on(dev, stream):
+        if total is None:
+            total = x if residual is None else torch.empty_like(x)
+        if shape.out_dtype == GBLA_E4M3:
+            each = shape.group or shape.width
+            if out is None:
+                out = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev)
+            if scales is None:
+                scales = torch.empty(x.shape[:-1] + (shape.width // each,), dtype=torch.float32, device=dev)
+            _want(out, "out", x.shape, torch.float8_e4m3fn, dev)
+            _want(scales, "scales", x.shape[:-1] + (shape.width // each,), torch.float32, dev)
+        else:
+            out = _like(out, "out", x)
+        st = load_library().gbla_add_norm(
+            ctypes.byref(shape), _ptr(x), _ptr(residual), _ptr(weight),
+            None if total is x and residual is None else _ptr(total), _ptr(out), _ptr(scales), _current(dev))
+    _raise(st, "gbla_add_norm")
+    return out, scales, total
+
+
+def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, sum_out=None, out=None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """s = x + residual in x's type (x if residual is None) and y = s / sqrt(mean s^2 + eps) *
+    weight over the last dimension, in x's type; see include/gbla.h.  x [..., width], weight fp32
+    [width].  Returns (y, s); s is x itself without a residual.  ``sum_out`` and ``out`` may be x
+    or residual themselves, not both the same one."""
+    shape = norm_shape(x, eps)
+    out, _, total = _add_norm(shape, x, weight, residual, sum_out, out, None, stream)
+    return out, total
+
+
+def add_rms_norm_e4m3(x, weight, residual=None, eps: float = 1e-6, group: int = 0, sum_out=None, out=None,
+                      scales=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """add_rms_norm with y in eight bits: returns (y as float8_e4m3fn, scales, s), where y stands
+    for out * scale.  ``group`` 128: a scale for every 128 channels (fp32 [..., width / 128]),
+    0: one a row ([..., 1])."""
+    shape = norm_shape(x, eps, GBLA_E4M3, group)
+    return _add_norm(shape, x, weight, residual, sum_out, out, scales, stream)
+
+
+def add_rms_norm_backward_workspace_bytes(shape: NormShape) -> int:
+    n = load_library().gbla_add_norm_backward_workspace_bytes(ctypes.byref(shape))
+    if n == 0:
+        raise GblaError(1, "gbla_add_norm_backward_workspace_bytes")
+    return int(n)
+
+
+def add_rms_norm_backward(total, weight, dout, dsum=None, eps: float = 1e-6, workspace=None,
+                          grads: Optional[dict] = None, stream=None) -> dict:
+    """Gradients of sum(y * dout) + sum(s * dsum), from the s that add_rms_norm returned: a dict
+    with dx (of x and of residual alike, in x's type) and dweight (fp32).  ``dsum`` None: zeros.
+    ``grads`` may hold outputs under those names; dx may be dout or dsum itself."""
+    shape = norm_shape(total, eps)
+    dev = total.device
+    _want(weight, "weight", (shape.width,), torch.float32, dev)
+    _want(dout, "dout", total.shape, total.dtype, dev)
+    if dsum is not None:
+        _want(dsum, "dsum", total.shape, total.dtype, dev)
+    need = add_rms_norm_backward_workspace_bytes(shape)
+    g = dict(grads or {})
+    with _on(dev, stream):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check_ws(workspace, dev, need)
+        g["dx"] = _like(g.get("dx"), "dx", total)
+        g["dweight"] = _like(g.get("dweight"), "dweight", weight)
+        st = load_library().gbla_add_norm_backward(
+            ctypes.byref(shape), _ptr(total), _ptr(weight), _ptr(dout), _ptr(dsum), _ptr(workspace),
+            workspace.numel(), _ptr(g["dx"]), _ptr(g["dweight"]), _current(dev))
+    _raise(st, "gbla_add_norm_backward")
+    return g
