@@ -13,8 +13,8 @@ namespace gbla {
 
 constexpr int kDeltaTile = 64;      // tokens of a tile
 constexpr int kDeltaMaxUnit = 512;  // tokens of a unit, at most
-constexpr int kPackBytes = 6 * 64 * 48;  // a tile's 64 x 64 triangle as operands (Packed), at most
-constexpr int kGateBytes = 1536;         // a tile's gates (struct Gates)
+constexpr int kGateBytes = 1792;         // a tile's gates (struct Gates)
+constexpr int kPackBytes = 6 * 64 * 48 + kGateBytes;  // a tile's triangle as operands (Packed), at most, and gates
 
 // The launches of gbla_delta_forward / gbla_delta_backward; a function of the shape
 // alone (and of max_seqlen, which only sets `single`).
@@ -34,12 +34,11 @@ struct DeltaPlan {
   int32_t tiles_per_seq;  // dense: ceil(n / kDeltaTile), at least 1
   int32_t tiles;          // tile slots of a value head (dense exact, ragged bound)
   // Workspace (bytes from its base)
-  size_t off_gates;  // [V, tiles] Gates
-  size_t off_pack;   // [V, tiles] packed triangles
+  size_t off_pack;   // [V, tiles] packed triangles and gates
   size_t off_B;      // [V, units, d, d] fp32: what a unit adds; then the state before each unit
   size_t off_M;      // [V, units, d, d] fp32: what a unit does to the state before it
   // Backward:
-  size_t off_packT;  // [V, tiles] packed triangles, transposed
+  size_t off_packT;  // ... with the triangles transposed
   size_t off_D;      // [V, units, d, d] fp32: the gradient of the state after each unit
   size_t off_S;      // [V, tiles, d, d] fp32: the state before each tile, [value][key channel]
   size_t off_N;      // ... the gradient of the state after each tile

@@ -40,8 +40,8 @@ __device__ __forceinline__ double log2_decay(float g) {
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads)
 prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, const float* beta,
-            const int32_t* cu, Gates* gates, unsigned char* packs, unsigned char* packsT) {
-  using C = DS<T, D, 4, 1>;
+            const int32_t* cu, unsigned char* packs, unsigned char* packsT) {
+  using C = DS<T, D, 4>;
   constexpr int kL = 68;  // floats of a row of L
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes];
   __shared__ __attribute__((aligned(16))) float ldsL[kDeltaTile][kL], ldsX[4][16][20];
@@ -81,7 +81,9 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
     G.lo[lane] = (float)(c - (double)hi);
     G.beta[lane] = lane < good ? bt : 0.0f;
     G.into[lane] = __builtin_amdgcn_exp2f(hi) * fmaf((float)(c - (double)hi), 0.69314718f, 1.0f);
-    G.rest[lane] = __builtin_amdgcn_exp2f((float)(end - c));
+    const float rest = __builtin_amdgcn_exp2f((float)(end - c));
+    G.rest[lane] = rest;
+    G.late[lane] = lane < good ? rest * bt : 0.0f;
     if (lane == 63) G.whole = G.into[63], G.good = good;
     if (lane < 62) G.pad[lane] = 0.0f;
   }
@@ -99,13 +101,15 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
     const int s = 16 * w + n;
     const float hi = G.hi[s], lo = G.lo[s];
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 4; ++b) {
+      const int t0 = 16 * b + 4 * g;
+      const f32x4_t h4 = *reinterpret_cast<const f32x4_t*>(&G.hi[t0]), l4 = *reinterpret_cast<const f32x4_t*>(&G.lo[t0]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int t = 16 * b + 4 * g + r;
-        const float f = decay_between(G, t, hi, lo);
-        ldsL[t][s] = t > s ? x[b][r] * f : 0.0f;
+        const float y = x[b][r] * __builtin_amdgcn_exp2f((h4[r] - hi) + (l4[r] - lo));
+        ldsL[t0 + r][s] = t0 + r > s ? y : 0.0f;
       }
+    }
   }
   __syncthreads();
   // X of the wave's diagonal block: lane n its column n, row after row.
@@ -160,39 +164,46 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
     for (int r = 0; r < 4; ++r) ldsL[16 * i + 4 * g + r][16 * w + n] = -m[i][r];
   __syncthreads();
   const size_t slot = (size_t)h * P.tiles + sp.slot;
-  unsigned char* pack = packs + slot * (Packed<T, kParts>::kBytes);
+  using Pack = Packed<T, kParts>;
+  unsigned char* pack = packs + slot * Pack::kBlock;
   for (int pair = w; pair < 6; pair += 4) {
     const int b = pair < 2 ? pair : 2 + (pair >> 2), ks = pair < 2 ? 0 : pair & 1;
     const f32x4_t* p = reinterpret_cast<const f32x4_t*>(&ldsL[row_of(b, n)][32 * ks + 8 * g]);
     const f32x4_t a = p[0], c = p[1];
     const float z[8] = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
     Parts<T, kParts> parts;
-    parts.set(z);
-    Packed<T, kParts>::put(pack, pair, lane, parts);
+    split(parts, z);
+    Pack::put(pack, pair, lane, parts);
   }
+  auto put_gates = [&] {
+    if (threadIdx.x < kGateBytes / 16)
+      reinterpret_cast<u32x4_t*>(pack + Pack::kBytes)[threadIdx.x] = reinterpret_cast<const u32x4_t*>(&G)[threadIdx.x];
+  };
+  put_gates();
   if (packsT) {
-    pack = packsT + slot * (Packed<T, kParts>::kBytes);
+    pack = packsT + slot * Pack::kBlock;
+    put_gates();
     for (int pair = w; pair < 6; pair += 4) {
       const int b = pair < 4 ? pair >> 1 : pair - 2, ks = pair < 4 ? pair & 1 : 1;
       float z[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) z[j] = ldsL[32 * ks + 8 * g + j][row_of(b, n)];
       Parts<T, kParts> parts;
-      parts.set(z);
-      Packed<T, kParts>::put(pack, pair, lane, parts);
+      split(parts, z);
+      Pack::put(pack, pair, lane, parts);
     }
   }
-  const u32x4_t* src = reinterpret_cast<const u32x4_t*>(&G);
-  u32x4_t* dst = reinterpret_cast<u32x4_t*>(gates + slot);
-  if (threadIdx.x < kGateBytes / 16) dst[threadIdx.x] = src[threadIdx.x];
 }
 
-template <typename T, int D>
-using WalkSizes = DS<T, D, D / 16, 1>;
 // What walk_kernel makes: outputs; a unit's records, which are what the unit adds to the state
 // (from zeros) and what it does to the state before it (from the identity, without values);
 // or what the backward needs of the forward, and the strengths' gradient.
 enum WalkMode { kOutputs, kRecords, kBack };
+template <typename T, int D>
+using WalkSizes = DS<T, D, D / 16>;
+// Waves a SIMD that the registers are kept to.
+template <typename T, int D, WalkMode Mode>
+constexpr int kWalkWaves = sizeof(T) == 4 || D == 32 || Mode == kBack ? 2 : 4;
 struct BackOut {
   const void* dout;
   const float* F;     // the gradient of u
@@ -201,9 +212,9 @@ struct BackOut {
 };
 
 template <typename T, int D, WalkMode Mode>
-__global__ void __launch_bounds__((WalkSizes<T, D>::NT), 2)
+__global__ void __launch_bounds__((WalkSizes<T, D>::NT), (kWalkWaves<T, D, Mode>))
 walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, const int32_t* cu,
-            const Gates* gates, const unsigned char* packs, float* recB, float* recM, T* out,
+            const unsigned char* packs, float* recB, float* recM, T* out,
             float* final_state, BackOut back) {
   using C = WalkSizes<T, D>;
   // Back, what is formed from the outputs are sums of both signs in fp32.
@@ -217,12 +228,13 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   __shared__ __attribute__((aligned(16))) Gates G;
   __shared__ int bad[2];  // of this tile and the next
   __shared__ float sums[2][Back ? C::NW : 1][kDeltaTile];
-  const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int h = blockIdx.y;
+  int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Span sp;
   if (!find_span<C::NT>(P, cu, blockIdx.x, &sp)) return;
   const int64_t pair = (int64_t)sp.s * P.value_heads + h;
-  const int e0 = 16 * C::CB * w;  // the wave's first column
+  const int e0 = 16 * w;  // the wave's first column
   Columns16<T, C> S;
   const size_t record = ((size_t)h * P.units + sp.slot) * (D * D);
   const bool map = !Out && blockIdx.z == 1;
@@ -242,245 +254,207 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
 
   const int64_t krow = first_row(P, sp, P.heads, h / P.group), vrow = first_row(P, sp, P.value_heads, h);
   const size_t slot0 = (size_t)h * P.tiles + tile_slot(P, sp.row0, sp.s);
+  // The next tile on its way: keys, queries and gates, whose places in LDS are read to a tile's
+  // end, through registers; values and the triangle, which are done with before the outputs,
+  // straight into theirs (fp32, whose rows there are padded: through registers too).
+  constexpr bool kDirect = sizeof(T) == 2;
   RowsLoad<T, C> lk, lq, lv;
   BlockLoad<C, M::kBytes> lm;
   BlockLoad<C, kGateBytes> lg;
+  const uint32_t atV = lds_address(ldsV), atM = lds_address(ldsM);
   auto fetch = [&](int t) {
     const int left = sp.end - t;
     lk.load(k + (krow + t) * D, left);
     if (Out) lq.load(q + (krow + t) * D, left);
-    lv.load(v + (vrow + t) * D, map ? 0 : left);
-    const size_t slot = slot0 + t / kDeltaTile;
-    lm.load(packs + slot * M::kBytes, left > 0);
-    lg.load(gates + slot, left > 0);
+    lg.load(packs + (slot0 + t / kDeltaTile) * M::kBlock + M::kBytes, left > 0);
   };
-  if (sp.begin < sp.end) fetch(sp.begin);
+  auto fetch_direct = [&](int t) {
+    const int left = sp.end - t;
+    const T* vt = v + (vrow + t) * D;
+    const unsigned char* mt = packs + (slot0 + t / kDeltaTile) * M::kBlock;
+    if constexpr (kDirect) {
+      rows_to_lds<T, C>(atV, vt, map ? 0 : left, w, fresh(lane));
+      block_to_lds<C, M::kBytes>(atM, mt, left > 0, w, fresh(lane));
+    } else {
+      lv.load(vt, map ? 0 : left);
+      lm.load(mt, left > 0);
+    }
+  };
+  if (sp.begin < sp.end) {
+    fetch(sp.begin);
+    fetch_direct(sp.begin);
+  }
   if (threadIdx.x == 0) bad[0] = kDeltaTile;
   __syncthreads();
+  // (addresses in LDS are worked out phase by phase: held over the loop they cost registers)
+  auto again = [&] { lane = fresh(lane), n = lane & 15, g = lane >> 4; };
   for (int t0 = sp.begin, flip = 0; t0 < sp.end; t0 += kDeltaTile, flip ^= 1) {
     const int live = min(kDeltaTile, sp.end - t0);
     lk.store(ldsK);
     if (Out) lq.store(ldsQ);
-    lv.store(ldsV);
-    lv.find_bad(&bad[flip]);
-    lm.store(ldsM);
     lg.store(&G);
+    if constexpr (kDirect) {
+      wait_vm<0>();
+    } else {
+      lv.store(ldsV);
+      lm.store(ldsM);
+    }
     lds_barrier();
     fetch(t0 + kDeltaTile);
-    const int good = min(min(bad[flip], G.good), live);
     if (threadIdx.x == 0) bad[flip ^ 1] = kDeltaTile;
-    if (good < live) {
-      clear_rows<C>(ldsK, good);
-      clear_rows<C>(ldsV, good);
+    if (G.good < live) {
+      clear_rows<C>(ldsK, G.good);
       lds_barrier();
     }
     const size_t slot = slot0 + t0 / kDeltaTile;
-    u32x2_t dob[C::CB][4];  // (fp32: the first two of four)
-    u32x2_t dob2[C::CB][4];
-    f32x4_t f[C::CB][4];
-    if constexpr (Back) {
-      const __amdgpu_buffer_rsrc_t rd =
-          make_rsrc(static_cast<const T*>(back.dout) + (vrow + t0) * D, (uint32_t)(live * C::kRow));
-#pragma unroll
-      for (int c = 0; c < C::CB; ++c)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const uint32_t from = (uint32_t)(row_of(b, n) * C::kRow + (e0 + 16 * c + 4 * g) * C::ES);
-          dob[c][b] = __builtin_amdgcn_raw_buffer_load_b64(rd, from, 0, 0);
-          if constexpr (sizeof(T) == 4) dob2[c][b] = __builtin_amdgcn_raw_buffer_load_b64(rd, from + 8, 0, 0);
-          f[c][b] = *reinterpret_cast<const f32x4_t*>(back.F + (slot * D + e0 + 16 * c + n) * kDeltaTile +
-                                                      row_of(b, 4 * g));
-        }
-      S.store_columns(back.S + slot * (D * D), e0, lane);
-    }
-    // Products over key channels: scores of the wave's own tokens, what the state
-    // predicts for the tile's keys, and what it answers to its queries (transposed).
-    constexpr int NP = C::NW < 4 ? 4 / C::NW : 1;  // blocks of 16 tokens whose scores a wave forms,
-    constexpr int PG = C::NW == 8 ? 1 : 2;         // with so many groups of 32 earlier tokens
-    const int pg0 = C::NW == 8 ? w >> 2 : 0;
-    f32x4_t y[C::CB][4], o[C::CB][4], p[NP][2 * PG];
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int c = 0; c < C::CB; ++c) y[c][b] = o[c][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-      for (int b = 0; b < 2 * PG; ++b) p[i][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int ks = 0; ks < C::KS; ++ks) {
-      typename Num<T>::V8 kk[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) kk[b] = row_units<T, C>(ldsK, row_of(b, n), ks, g);
-      if constexpr (Out) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const auto own = row_units<T, C>(ldsQ, row_of((w + C::NW * i) & 3, n), ks, g);
-#pragma unroll
-          for (int b = 0; b < 2 * PG; ++b)
-            Num<T>::mma(p[i][b], PG == 2 ? kk[b] : row_units<T, C>(ldsK, row_of(2 * pg0 + b, n), ks, g), own);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < C::CB; ++c) {
-        const Parts<T, kParts> s = S.template operand<kParts>(c, ks);
-#pragma unroll
-        for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i)
-#pragma unroll
-          for (int b = 0; b < 4; ++b) Num<T>::mma(y[c][b], kk[b], s.v[i]);
-        if constexpr (Out) {
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const auto qq = row_units<T, C>(ldsQ, row_of(b, n), ks, g);
-#pragma unroll
-            for (int i = Parts<T, kOut>::kN - 1; i >= 0; --i) Num<T>::mma(o[c][b], s.v[i], qq);
-          }
-        }
-      }
-    }
-    // The scores as operands [token][earlier tokens] for all waves.
+    again();
+    // Scores [own token][earlier tokens] as operands for all waves: a wave forms NP blocks of 16
+    // own tokens with PG groups of 32 earlier ones.
     if constexpr (Out) {
+      constexpr int NP = C::NW < 4 ? 4 / C::NW : 1, PG = C::NW == 8 ? 1 : 2;
+      const int pg0 = C::NW == 8 ? w >> 2 : 0;
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int b = (w + C::NW * i) & 3, t = row_of(b, n);
-        const float hi = G.hi[t], lo = G.lo[t];
+        f32x4_t p[2 * PG];
+#pragma unroll
+        for (int j = 0; j < 2 * PG; ++j) p[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks) {
+          const auto own = row_units<T, C>(ldsQ, t, ks, g);
+#pragma unroll
+          for (int j = 0; j < 2 * PG; ++j) Num<T>::mma(p[j], row_units<T, C>(ldsK, row_of(2 * pg0 + j, n), ks, g), own);
+        }
 #pragma unroll
         for (int z = 0; z < PG; ++z) {
           const int ks = pg0 + z;
           float x[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int s = 32 * ks + 8 * g + j;
-            const float f = __builtin_amdgcn_exp2f((hi - G.hi[s]) + (lo - G.lo[s]));
-            x[j] = s <= t ? p[i][2 * z + (j >> 2)][j & 3] * (P.scale * f) : 0.0f;
-          }
+          for (int j = 0; j < 8; ++j) x[j] = p[2 * z + (j >> 2)][j & 3];
+          decayed<true>(G, t, 32 * ks + 8 * g, P.scale, x);
           Parts<T, kOut> parts;
-          parts.set(x);
+          split(parts, x);
           if (ks == 0 || b >= 2) Pk::put(ldsP, lower_pair(b, ks), lane, parts);
         }
       }
     }
-    // The tile's values less the prediction, and what of that stays as the tile is read
-    // token by token.
-    float beta[2][8], rest[2][8];
+    __builtin_amdgcn_sched_barrier(0);
+    again();
+    // What the state predicts for the tile's keys; the values less that, y; and what of that
+    // stays as the tile is read token by token, e.
+    f32x4_t y[4];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int b = 0; b < 4; ++b) y[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        beta[ks][j] = G.beta[32 * ks + 8 * g + j];
-        rest[ks][j] = G.rest[32 * ks + 8 * g + j];
-      }
+    for (int ks = 0; ks < C::KS; ++ks) {
+      typename Num<T>::V8 kk[4];
 #pragma unroll
-    for (int c = 0; c < C::CB; ++c) {
+      for (int b = 0; b < 4; ++b) kk[b] = row_units<T, C>(ldsK, row_of(b, n), ks, g);
+      const Parts<T, kParts> s = S.template operand<kParts>(ks);
+      if constexpr (Back) store_columns<T, C>(back.S + slot * (D * D), ks, e0, lane, s);
+#pragma unroll
+      for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) Num<T>::mma(y[b], kk[b], s.v[i]);
+    }
+    {
       Parts<T, kParts> by[2];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
+        float into[8], beta[8];
+        eight(&G.into[32 * ks + 8 * g], into);
+        eight(&G.beta[32 * ks + 8 * g], beta);
         float x[8];
-        Num<T>::widen(value_column<T, C>(ldsV, C::CB * w + c, ks, lane), x);
+        auto v8 = value_column<T, C>(ldsV, w, ks, lane);
+        drop_bad<T>(v8, 32 * ks + 8 * g, &bad[flip]);
+        Num<T>::widen(v8, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float z = fmaf(-G.into[32 * ks + 8 * g + j], y[c][2 * ks + (j >> 2)][j & 3], x[j]);
-          y[c][2 * ks + (j >> 2)][j & 3] = z;
-          x[j] = beta[ks][j] * z;
-        }
-        by[ks].set(x);
+        for (int j = 0; j < 8; ++j) y[2 * ks + (j >> 2)][j & 3] = fmaf(-into[j], y[2 * ks + (j >> 2)][j & 3], x[j]);
+        weighted<T>(by[ks], beta, y[2 * ks], y[2 * ks + 1]);
       }
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int ks = 0; ks <= (b >> 1); ++ks)
-          mma_parts<T>(y[c][b], M::get(ldsM, lower_pair(b, ks), lane), by[ks]);
+      triangle<T, kParts, false>(y, ldsM, by, lane);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    again();
     if constexpr (Back) {
       float x[2][8];
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int b = 0; b < 4; ++b) {
+        float* at = back.E + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g);
+        *reinterpret_cast<f32x4_t*>(at) = y[b];
+        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(back.F + (at - back.E));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[ks][j] = 0.0f;
-#pragma unroll
-          for (int c = 0; c < C::CB; ++c)
-            x[ks][j] = fmaf(y[c][2 * ks + (j >> 2)][j & 3], f[c][2 * ks + (j >> 2)][j & 3], x[ks][j]);
+        for (int r = 0; r < 4; ++r) {
+          x[b >> 1][4 * (b & 1) + r] = y[b][r] * f[r];
         }
-#pragma unroll
-      for (int c = 0; c < C::CB; ++c)
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-          *reinterpret_cast<f32x4_t*>(back.E + (slot * D + e0 + 16 * c + n) * kDeltaTile + row_of(b, 4 * g)) = y[c][b];
+      }
       const float sum = token_sums(x, lane);
       sums[0][w][token_of(lane)] = sum;
     }
-    if (Out) lds_barrier();  // the scores
-    const float whole = G.whole;
+    lds_barrier();  // the scores are there; nobody reads the values and the triangle any more
+    const int good = min(min(bad[flip], G.good), live);
+    if (t0 + kDeltaTile < sp.end) fetch_direct(t0 + kDeltaTile);
+    if constexpr (Out) {
+      again();
+      f32x4_t o[4];
 #pragma unroll
-    for (int c = 0; c < C::CB; ++c) {
-      if constexpr (Out) {
+      for (int b = 0; b < 4; ++b) o[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int ks = 0; ks < C::KS; ++ks) {
+        typename Num<T>::V8 qq[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) qq[b] = row_units<T, C>(ldsQ, row_of(b, n), ks, g);
+        const Parts<T, kOut> s = S.template operand<kOut>(ks);
+#pragma unroll
+        for (int i = Parts<T, kOut>::kN - 1; i >= 0; --i)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) Num<T>::mma(o[b], s.v[i], qq[b]);
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const float f = P.scale * G.into[row_of(b, n)];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[b][r] *= f;
+      }
+      {
         Parts<T, kOut> u[2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          float x[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = beta[ks][j] * y[c][2 * ks + (j >> 2)][j & 3];
-          u[ks].set(x);
+          float beta[8];
+          eight(&G.beta[32 * ks + 8 * g], beta);
+          weighted<T>(u[ks], beta, y[2 * ks], y[2 * ks + 1]);
         }
+        triangle<T, kOut, true>(o, ldsP, u, lane);
+      }
+      if constexpr (Back) {
+        const __amdgpu_buffer_rsrc_t rd =
+            make_rsrc(static_cast<const T*>(back.dout) + (vrow + t0) * D, (uint32_t)(live * C::kRow));
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          const float f = P.scale * G.into[row_of(b, n)];
+          float x = 0.0f;
+          const uint32_t from = (uint32_t)(row_of(b, n) * C::kRow + (e0 + 4 * g) * C::ES);
+          if constexpr (sizeof(T) == 2) {
+            const u32x2_t z = __builtin_amdgcn_raw_buffer_load_b64(rd, from, 0, 0);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[c][b][r] *= f;
+            for (int r = 0; r < 4; ++r) x = fmaf(o[b][r], r & 1 ? bf16_hi(z[r >> 1]) : bf16_lo(z[r >> 1]), x);
+          } else {
+            const u32x4_t z = __builtin_amdgcn_raw_buffer_load_b128(rd, from, 0, 0);
 #pragma unroll
-          for (int ks = 0; ks <= (b >> 1); ++ks)
-            mma_parts<T>(o[c][b], u[ks], Pk::get(ldsP, lower_pair(b, ks), lane));
-        }
-      }
-      Parts<T, kParts> u[2];
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = rest[ks][j] * (beta[ks][j] * y[c][2 * ks + (j >> 2)][j & 3]);
-        u[ks].set(x);
-      }
-#pragma unroll
-      for (int i = 0; i < C::NB; ++i) {
-        f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const auto a = key_column<T, C>(ldsK, i, kt, lane);
-#pragma unroll
-          for (int z = Parts<T, kParts>::kN - 1; z >= 0; --z) Num<T>::mma(x, a, u[kt].v[z]);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S.s[c][i][r] = fmaf(whole, S.s[c][i][r], x[r]);
-      }
-    }
-    if constexpr (Back) {
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        float x = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C::CB; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const uint32_t z = sizeof(T) == 2 ? dob[c][b][r >> 1] : r < 2 ? dob[c][b][r & 1] : dob2[c][b][r & 1];
-            x = fmaf(o[c][b][r], sizeof(T) == 4 ? __uint_as_float(z) : r & 1 ? bf16_hi(z) : bf16_lo(z), x);
+            for (int r = 0; r < 4; ++r) x = fmaf(o[b][r], __uint_as_float(z[r]), x);
           }
-        x += __shfl_xor(x, 16);
-        x += __shfl_xor(x, 32);
-        sums[1][w][row_of(b, n)] = x;
-      }
-    }
-    if constexpr (Mode == kOutputs) {
-      const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + (vrow + t0) * D, (uint32_t)(live * C::kRow));
-#pragma unroll
-      for (int c = 0; c < C::CB; ++c)
+          x += __shfl_xor(x, 16);
+          x += __shfl_xor(x, 32);
+          sums[1][w][row_of(b, n)] = x;
+        }
+      } else {
+        const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + (vrow + t0) * D, (uint32_t)(live * C::kRow));
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           const int t = row_of(b, n);
-          f32x4_t z = o[c][b];
+          f32x4_t z = o[b];
 #pragma unroll
           for (int r = 0; r < 4; ++r) z[r] = t >= good ? __builtin_nanf("") : z[r];
-          const uint32_t to = (uint32_t)(t * C::kRow + (e0 + 16 * c + 4 * g) * C::ES);
+          const uint32_t to = (uint32_t)(t * C::kRow + (e0 + 4 * g) * C::ES);
           if constexpr (sizeof(T) == 2) {
             __builtin_amdgcn_raw_buffer_store_b64((u32x2_t){pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])}, ro,
                                                   to, 0, 0);
@@ -488,6 +462,29 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, z), ro, to, 0, 0);
           }
         }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    again();
+    Parts<T, kParts> u[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      float late[8];
+      eight(&G.late[32 * ks + 8 * g], late);
+      weighted<T>(u[ks], late, y[2 * ks], y[2 * ks + 1]);
+    }
+    const float whole = G.whole;
+#pragma unroll
+    for (int i = 0; i < C::NB; ++i) {
+      f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const auto a = key_column<T, C>(ldsK, i, kt, lane);
+#pragma unroll
+        for (int z = Parts<T, kParts>::kN - 1; z >= 0; --z) Num<T>::mma(x, a, u[kt].v[z]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) S.s[i][r] = fmaf(whole, S.s[i][r], x[r]);
     }
     if (good < live) S.fill(__builtin_nanf(""));
     lds_barrier();
@@ -503,8 +500,9 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
       }
     }
   }
-  if (!Out) S.store((map ? recM : recB) + record, e0, lane);
-  else if (!Back && final_state && sp.last) S.store(final_state + pair * (D * D), e0, lane);
+  float* to = !Out ? (map ? recM : recB) + record
+              : !Back && final_state && sp.last ? final_state + pair * (D * D) : nullptr;
+  if (to) S.store(to, e0, lane);
 }
 
 // The records become the state before each unit, in place: S -> M S + B from unit to unit.
@@ -525,7 +523,10 @@ scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const 
   const size_t record = ((size_t)h * P.units + first) * (D * D);
   float* B = recB + record + (16 * w + 4 * g) * D + e0 + n;
   const float* M = recM + record + (Back ? 4 * g * D + 16 * w + n : (16 * w + n) * D + 4 * g);
-  f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f}, b, m[KS];
+  f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+  struct Records {
+    f32x4_t b, m[KS];
+  };
   if (S0) {
     const float* p = S0 + ((int64_t)s * P.value_heads + h) * (D * D) + (16 * w + 4 * g) * D + e0 + n;
 #pragma unroll
@@ -535,39 +536,42 @@ scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const 
   // from zeros.
   auto unit = [&](int i) { return Back ? units - 1 - i : i; };
   auto fetch = [&](int i) {
+    Records rec;
     const bool any = i < units - 1, map = any && (i > 0 || S0);
     const size_t at = (size_t)unit(min(i, units - 1)) * (D * D);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) b[r] = any ? B[at + r * D] : 0.0f;
+    for (int r = 0; r < 4; ++r) rec.b[r] = any ? B[at + r * D] : 0.0f;
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
-      m[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+      rec.m[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
       if (map) {
         if constexpr (Back) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) m[j][r] = M[at + (16 * j + r) * D];
+          for (int r = 0; r < 4; ++r) rec.m[j][r] = M[at + (16 * j + r) * D];
         } else {
-          m[j] = *reinterpret_cast<const f32x4_t*>(M + at + 16 * j);
+          rec.m[j] = *reinterpret_cast<const f32x4_t*>(M + at + 16 * j);
         }
       }
     }
+    return rec;
   };
-  fetch(0);
+  Records rec = fetch(0);
   for (int i = 0; i < units; ++i) {
     float* sx = lds[i & 1];
 #pragma unroll
     for (int r = 0; r < 4; ++r) B[(size_t)unit(i) * (D * D) + r * D] = x[r];
     if (i + 1 == units) break;
     *reinterpret_cast<f32x4_t*>(&sx[n * kPitch + 16 * w + 4 * g]) = x;
+    const Records now = rec;
+    rec = fetch(i + 1);  // under way while this unit's are multiplied
     lds_barrier();
-    f32x4_t z[2] = {b, {0.0f, 0.0f, 0.0f, 0.0f}};
+    f32x4_t z[2] = {now.b, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
       const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&sx[n * kPitch + 16 * j + 4 * g]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[j][r], y[r], z[r & 1], 0, 0, 0);
+      for (int r = 0; r < 4; ++r) z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(now.m[j][r], y[r], z[r & 1], 0, 0, 0);
     }
-    fetch(i + 1);
     x = z[0] + z[1];
   }
 }
@@ -582,15 +586,14 @@ void launch_prep(const DeltaPlan& p, const void* k, const float* log_decay, cons
                  unsigned char* base, bool backward, hipStream_t st) {
   if (p.tokens > 0)
     hipLaunchKernelGGL((prep_kernel<T, D>), dim3(p.tiles, p.value_heads), dim3(kThreads), 0, st, p, tile_spans(p),
-                       (const T*)k, log_decay, beta, cu, reinterpret_cast<Gates*>(base + p.off_gates),
-                       base + p.off_pack, backward ? base + p.off_packT : nullptr);
+                       (const T*)k, log_decay, beta, cu, base + p.off_pack, backward ? base + p.off_packT : nullptr);
 }
 template <typename T, int D, WalkMode Mode>
 void launch_walk(const DeltaPlan& p, const void* q, const void* k, const void* v, const float* S0, const int32_t* cu,
                  unsigned char* base, void* out, float* final_state, const BackOut& back, hipStream_t st) {
   hipLaunchKernelGGL((walk_kernel<T, D, Mode>), dim3(p.grid_units, p.value_heads, Mode == kRecords ? 2 : 1),
                      dim3((WalkSizes<T, D>::NT)), 0, st, p, (const T*)q, (const T*)k, (const T*)v, S0, cu,
-                     reinterpret_cast<const Gates*>(base + p.off_gates), base + p.off_pack,
+                     base + p.off_pack,
                      reinterpret_cast<float*>(base + p.off_B), reinterpret_cast<float*>(base + p.off_M), (T*)out,
                      final_state, back);
 }

@@ -22,18 +22,21 @@ namespace {
 
 constexpr int kParts = 3;
 template <typename T, int D>
-using BackSizes = DS<T, D, D / 16, 1>;
+using BackSizes = DS<T, D, D / 16>;
+
+// Waves a SIMD that the registers are kept to.
+template <typename T, int D, bool Records>
+constexpr int kBackWaves = 2;
 
 struct BackArrays {
-  const Gates* gates;
-  const unsigned char* packs;  // M's transposes
+  const unsigned char* packs;  // M's transposes and the gates
   float* recD;                 // the gradient of the state after each unit; what it adds (Records)
   float *N, *F, *dv_v;
 };
 
 // Records: what the unit's own tokens add to the gradient of the state before it, into recD.
 template <typename T, int D, bool Records>
-__global__ void __launch_bounds__((BackSizes<T, D>::NT), 2)
+__global__ void __launch_bounds__((BackSizes<T, D>::NT), (kBackWaves<T, D, Records>))
 back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, const int32_t* cu, const float* dfinal,
             BackArrays a, float* dS0) {
   using C = BackSizes<T, D>;
@@ -41,16 +44,17 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
   constexpr bool All = !Records;
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes], ldsQ[C::kTileBytes],
       ldsO[C::kTileBytes], ldsV[All ? C::kTileBytes : 16];
-  __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBytes], ldsP[M::kBytes];
-  __shared__ __attribute__((aligned(16))) Gates G;
+  __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBlock], ldsP[M::kBytes];
+  const Gates& G = *reinterpret_cast<const Gates*>(ldsM + M::kBytes);
   __shared__ float sums[All ? C::NW : 1][kDeltaTile];
-  const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int h = blockIdx.y;
+  int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Span sp;
   if (!find_span<C::NT>(P, cu, blockIdx.x, &sp)) return;
   if (Records && sp.idx == 0) return;  // nothing comes before it
   const int64_t pair = (int64_t)sp.s * P.value_heads + h;
-  const int e0 = 16 * C::CB * w;
+  const int e0 = 16 * w;
   const size_t record = ((size_t)h * P.units + sp.slot) * (D * D);
   Columns16<T, C> N;
   const float* init = Records                                ? nullptr
@@ -63,8 +67,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
   const int64_t krow = first_row(P, sp, P.heads, h / P.group), vrow = first_row(P, sp, P.value_heads, h);
   const size_t slot0 = (size_t)h * P.tiles + tile_slot(P, sp.row0, sp.s);
   RowsLoad<T, C> lk, lq, lo, lv;
-  BlockLoad<C, M::kBytes> lm;
-  BlockLoad<C, kGateBytes> lg;
+  BlockLoad<C, M::kBlock> lm;
   auto fetch = [&](int t) {  // (none before the unit's first tile)
     const int left = t < sp.begin ? 0 : sp.end - t;
     const int64_t row = max(t, 0);
@@ -72,12 +75,12 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
     lq.load(q + (krow + row) * D, left);
     lo.load(dout + (vrow + row) * D, left);
     if (All) lv.load(v + (vrow + row) * D, left);
-    const size_t slot = slot0 + row / kDeltaTile;
-    lm.load(a.packs + slot * M::kBytes, left > 0);
-    lg.load(a.gates + slot, left > 0);
+    lm.load(a.packs + (slot0 + row / kDeltaTile) * M::kBlock, left > 0);
   };
   const int last = sp.begin < sp.end ? sp.begin + (sp.end - 1 - sp.begin) / kDeltaTile * kDeltaTile : sp.begin - 1;
   if (sp.begin < sp.end) fetch(last);
+  // (addresses in LDS are worked out phase by phase: held over the loop they cost registers)
+  auto again = [&] { lane = fresh(lane), n = lane & 15, g = lane >> 4; };
   for (int t0 = last; t0 >= sp.begin; t0 -= kDeltaTile) {
     const int live = min(kDeltaTile, sp.end - t0);
     const size_t slot = slot0 + t0 / kDeltaTile;
@@ -86,128 +89,124 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
     lo.store(ldsO);
     if (All) lv.store(ldsV);
     lm.store(ldsM);
-    lg.store(&G);
     lds_barrier();
-    fetch(t0 - kDeltaTile);
-    if (All) N.store_columns(a.N + slot * (D * D), e0, lane);
-    // Scores [later tokens][own earlier tokens] and, with the gradient of the state, of u.
-    constexpr int NP = C::NW < 4 ? 4 / C::NW : 1;
-    constexpr int PG = C::NW == 8 ? 1 : 2;
-    const int pg0 = C::NW == 8 ? w >> 2 : 0;
-    f32x4_t x[C::CB][4], p[NP][2 * PG];
+    again();
+    // Scores [later tokens][own earlier token] as operands for all waves.
+    {
+      constexpr int NP = C::NW < 4 ? 4 / C::NW : 1, PG = C::NW == 8 ? 1 : 2;
+      const int pg0 = C::NW == 8 ? w >> 2 : 0;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+      for (int i = 0; i < NP; ++i) {
+        const int b = (w + C::NW * i) & 3, s = row_of(b, n);
+        f32x4_t p[2 * PG];
 #pragma unroll
-      for (int c = 0; c < C::CB; ++c) x[c][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < 2 * PG; ++j) p[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
+        for (int ks = 0; ks < C::KS; ++ks) {
+          const auto own = row_units<T, C>(ldsK, s, ks, g);
 #pragma unroll
-      for (int b = 0; b < 2 * PG; ++b) p[i][b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+          for (int j = 0; j < 2 * PG; ++j) Num<T>::mma(p[j], row_units<T, C>(ldsQ, row_of(2 * pg0 + j, n), ks, g), own);
+        }
+#pragma unroll
+        for (int z = 0; z < PG; ++z) {
+          const int ks = pg0 + z;
+          float y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = p[2 * z + (j >> 2)][j & 3];
+          decayed<false>(G, s, 32 * ks + 8 * g, P.scale, y);
+          Parts<T, kParts> parts;
+          split(parts, y);
+          if (ks == 1 || b < 2) M::put(ldsP, upper_pair(b, ks), lane, parts);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    again();
+    // The gradient of u: from the states after the tile, from the tile's outputs; f is that
+    // without the tile's later ones.
+    f32x4_t x[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) x[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int ks = 0; ks < C::KS; ++ks) {
+      const Parts<T, kParts> s = N.template operand<kParts>(ks);
+      if constexpr (All) store_columns<T, C>(a.N + slot * (D * D), ks, e0, lane, s);
       typename Num<T>::V8 kk[4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) kk[b] = row_units<T, C>(ldsK, row_of(b, n), ks, g);
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const auto own = row_units<T, C>(ldsK, row_of((w + C::NW * i) & 3, n), ks, g);
+      for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i)
 #pragma unroll
-        for (int b = 0; b < 2 * PG; ++b)
-          Num<T>::mma(p[i][b], row_units<T, C>(ldsQ, row_of(2 * pg0 + b, n), ks, g), own);
-      }
-#pragma unroll
-      for (int c = 0; c < C::CB; ++c) {
-        const Parts<T, kParts> s = N.template operand<kParts>(c, ks);
-#pragma unroll
-        for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i)
-#pragma unroll
-          for (int b = 0; b < 4; ++b) Num<T>::mma(x[c][b], kk[b], s.v[i]);
-      }
+        for (int b = 0; b < 4; ++b) Num<T>::mma(x[b], kk[b], s.v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int b = (w + C::NW * i) & 3, s = row_of(b, n);
-      const float hi = G.hi[s], lo = G.lo[s];
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int z = 0; z < PG; ++z) {
-        const int ks = pg0 + z;
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = 32 * ks + 8 * g + j;
-          const float f = decay_between(G, t, hi, lo);
-          y[j] = s <= t ? p[i][2 * z + (j >> 2)][j & 3] * (P.scale * f) : 0.0f;
-        }
-        Parts<T, kParts> parts;
-        parts.set(y);
-        if (ks == 1 || b < 2) M::put(ldsP, upper_pair(b, ks), lane, parts);
-      }
-    }
+      for (int r = 0; r < 4; ++r) x[b][r] *= G.rest[row_of(b, 4 * g + r)];
     lds_barrier();  // the scores
-    float beta[2][8], into[2][8], part[2][8];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        beta[ks][j] = G.beta[32 * ks + 8 * g + j];
-        into[ks][j] = G.into[32 * ks + 8 * g + j];
-        part[ks][j] = 0.0f;
-      }
-    const float whole = G.whole;
-#pragma unroll
-    for (int c = 0; c < C::CB; ++c) {
+    again();
+    {
       typename Num<T>::V8 o[2];
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) o[ks] = value_column<T, C>(ldsO, C::CB * w + c, ks, lane);
+      for (int ks = 0; ks < 2; ++ks) o[ks] = value_column<T, C>(ldsO, w, ks, lane);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[c][b][r] *= G.rest[row_of(b, 4 * g + r)];
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int ks = b >> 1; ks < 2; ++ks) {
           const Parts<T, kParts> y = M::get(ldsP, upper_pair(b, ks), lane);
 #pragma unroll
-          for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i) Num<T>::mma(x[c][b], y.v[i], o[ks]);
+          for (int i = Parts<T, kParts>::kN - 1; i >= 0; --i) Num<T>::mma(x[b], y.v[i], o[ks]);
         }
-      }
       Parts<T, kParts> y[2];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         float z[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = beta[ks][j] * x[c][2 * ks + (j >> 2)][j & 3];
-        y[ks].set(z);
+        for (int j = 0; j < 8; ++j) z[j] = G.beta[32 * ks + 8 * g + j] * x[2 * ks + (j >> 2)][j & 3];
+        split(y[ks], z);
       }
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int ks = b >> 1; ks < 2; ++ks) mma_parts<T>(x[c][b], M::get(ldsM, upper_pair(b, ks), lane), y[ks]);
-      // x: the gradient of u without the tile's later ones, f
-      Parts<T, kParts> up[2];
+        for (int ks = b >> 1; ks < 2; ++ks) mma_parts<T>(x[b], M::get(ldsM, upper_pair(b, ks), lane), y[ks]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    again();
+    if constexpr (All) {
+      float part[2][8];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        float z[8], dv[8];
-        Num<T>::widen(o[ks], z);
+        float z[8];
+        Num<T>::widen(value_column<T, C>(ldsV, w, ks, lane), z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[ks][j] = G.beta[32 * ks + 8 * g + j] * x[2 * ks + (j >> 2)][j & 3] * z[j];
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<f32x4_t*>(a.F + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g)) = x[b];
+      const float sum = token_sums(part, lane);
+      sums[w][token_of(lane)] = sum;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(t0 - kDeltaTile);
+    again();
+    {
+      Parts<T, kParts> up[2], down[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        float z[8];
+        Num<T>::widen(value_column<T, C>(ldsO, w, ks, lane), z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] *= P.scale * G.into[32 * ks + 8 * g + j];
+        split(up[ks], z);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          dv[j] = beta[ks][j] * x[c][2 * ks + (j >> 2)][j & 3];
-          z[j] *= P.scale * into[ks][j];
+          const int t = 32 * ks + 8 * g + j;
+          z[j] = -G.into[t] * (G.beta[t] * x[2 * ks + (j >> 2)][j & 3]);
         }
-        up[ks].set(z);
-        if constexpr (All) {
-          Num<T>::widen(value_column<T, C>(ldsV, C::CB * w + c, ks, lane), z);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) part[ks][j] = fmaf(dv[j], z[j], part[ks][j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dv[j] *= -into[ks][j];
-        y[ks].set(dv);
+        split(down[ks], z);
       }
-      if constexpr (All) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-          *reinterpret_cast<f32x4_t*>(a.F + (slot * D + e0 + 16 * c + n) * kDeltaTile + row_of(b, 4 * g)) = x[c][b];
-      }
+      const float whole = G.whole;
 #pragma unroll
       for (int i = 0; i < C::NB; ++i) {
         f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -216,17 +215,13 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
           const auto kc = key_column<T, C>(ldsK, i, kt, lane), qc = key_column<T, C>(ldsQ, i, kt, lane);
 #pragma unroll
           for (int j = Parts<T, kParts>::kN - 1; j >= 0; --j) {
-            Num<T>::mma(z, kc, y[kt].v[j]);
+            Num<T>::mma(z, kc, down[kt].v[j]);
             Num<T>::mma(z, qc, up[kt].v[j]);
           }
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) N.s[c][i][r] = fmaf(whole, N.s[c][i][r], z[r]);
+        for (int r = 0; r < 4; ++r) N.s[i][r] = fmaf(whole, N.s[i][r], z[r]);
       }
-    }
-    if constexpr (All) {
-      const float sum = token_sums(part, lane);
-      sums[w][token_of(lane)] = sum;
     }
     lds_barrier();
     if constexpr (All) {
@@ -246,7 +241,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
 BackArrays arrays(const DeltaPlan& p, void* ws) {
   unsigned char* base = static_cast<unsigned char*>(ws);
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
-  return {reinterpret_cast<const Gates*>(base + p.off_gates), base + p.off_packT, floats(p.off_D), floats(p.off_N),
+  return {base + p.off_packT, floats(p.off_D), floats(p.off_N),
           floats(p.off_F), floats(p.off_dv_v)};
 }
 

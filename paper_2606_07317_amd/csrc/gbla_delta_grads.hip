@@ -23,27 +23,271 @@ namespace {
 // gradients that they form.
 constexpr int kParts = 2;
 
-// One value of a row-major tile of `live` rows (zero behind them).
-template <typename T>
-__device__ __forceinline__ float value_at(__amdgpu_buffer_rsrc_t r, int at) {
-  if constexpr (sizeof(T) == 2)
-    return __uint_as_float((uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, (uint32_t)(2 * at), 0, 0) << 16);
-  else
-    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (uint32_t)(4 * at), 0, 0));
+// bf16.  Wave w takes the tokens row_of(w, ..) of a tile as its own.  All that is computed in
+// fp32 enters as two bf16 parts: the states come so from the walks; the vectors u and dv are
+// weighted and split once for all waves, into LDS as [value channel][token], where both the own
+// tokens' operands and the others' are transposed reads.
+//
+// Half of LDS holds them first (u | dv, each in two parts); after the pairs' products the same
+// place holds keys and queries below, and above the first 32 key channels of both states (in two
+// parts, [value channel][key channel]); the others follow by turns above and below, each loaded
+// while the one before is multiplied.
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2)
+grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k, const uint16_t* dout,
+             const int32_t* cu, const unsigned char* packs, const float* S, const float* N, const float* E,
+             const float* F, uint16_t* dq, uint16_t* dk, uint16_t* dv) {
+  using T = uint16_t;
+  using C = DS<T, D, 4>;            // rows of the operands
+  using V = DS<T, kDeltaTile, 4>;   // rows of the vectors
+  using B = DS<T, 32, 4>;           // rows of 32 key channels of a state
+  constexpr int kPlane = D * V::kRow, kHalf = 2 * kPlane;
+  static_assert(kHalf == 2 * C::kTileBytes && kHalf == 4 * D * B::kRow, "the halves' uses");
+  __shared__ __attribute__((aligned(512))) unsigned char lds[2 * kHalf];
+  __shared__ __attribute__((aligned(16))) Gates G;
+  unsigned char *ldsK = lds, *ldsQ = lds + C::kTileBytes;
+  Span sp;
+  if (!find_span<kThreads>(tiles, cu, blockIdx.x, &sp)) return;
+  const int hk = blockIdx.y, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = w >> 1;
+  int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, own = row_of(w, n);
+  // (addresses are worked out phase by phase: held over the kernel they cost registers)
+  auto again = [&] { lane = fresh(lane), n = lane & 15, g = lane >> 4, own = row_of(w, n); };
+  const int live = sp.end - sp.begin;
+  if (live <= 0) return;
+  const int64_t krow = first_row(P, sp, P.heads, hk) + sp.begin;
+  const uint32_t bytes = (uint32_t)(live * C::kRow), at_lds = lds_address(lds);
+  f32x4_t aq[C::NB], ak[C::NB];  // channels row_of(c, 4 g + r) of the own token
+#pragma unroll
+  for (int c = 0; c < C::NB; ++c) aq[c] = ak[c] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int gi = 0; gi < P.group; ++gi) {
+    const int h = hk * P.group + gi;
+    const size_t slot = (size_t)h * P.tiles + sp.slot;
+    const int64_t vrow = first_row(P, sp, P.value_heads, h) + sp.begin;
+    const __amdgpu_buffer_rsrc_t ro = make_rsrc(dout + vrow * D, bytes);
+    if (gi > 0) lds_barrier();
+    if (threadIdx.x < kGateBytes / 16)
+      reinterpret_cast<u32x4_t*>(&G)[threadIdx.x] =
+          reinterpret_cast<const u32x4_t*>(packs + slot * Packed<T, 3>::kBlock + Packed<T, 3>::kBytes)[threadIdx.x];
+    auto gradient = [&](int t, int ks) {  // of the outputs
+      Parts<T, 1> o;
+      o.v[0] = __builtin_amdgcn_raw_buffer_load_b128(ro, (uint32_t)(t * C::kRow + 64 * ks + 16 * g), 0, 0);
+      return o;
+    };
+    {
+      const int id = fresh((int)threadIdx.x), unit = id & 7;
+      f32x4_t x[2][C::KS][2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int i = 0; i < C::KS; ++i) {
+          const f32x4_t* from = reinterpret_cast<const f32x4_t*>((z ? F : E) + slot * (D * kDeltaTile)) +
+                                2 * (i * kThreads + id);
+          x[z][i][0] = from[0];
+          x[z][i][1] = from[1];
+        }
+      lds_barrier();
+      float beta[8];
+      eight(&G.beta[8 * unit], beta);
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int i = 0; i < C::KS; ++i) {
+          Parts<T, kParts> p;
+          weighted<T>(p, beta, x[z][i][0], x[z][i][1]);
+#pragma unroll
+          for (int j = 0; j < kParts; ++j)
+            *reinterpret_cast<u32x4_t*>(lds + (2 * z + j) * kPlane +
+                                        V::unit_at((i * kThreads + id) / 8, unit)) = p.v[j];
+        }
+    }
+    lds_barrier();
+    auto vectors = [&](int z, int b, int ks) {  // u (z = 0) or dv of the tokens row_of(b, ..)
+      Parts<T, kParts> p;
+#pragma unroll
+      for (int j = 0; j < kParts; ++j) p.v[j] = key_column<T, V>(lds + (2 * z + j) * kPlane, b, ks, lane);
+      return p;
+    };
+    // Pairs of an own token and others of the tile, [others][own]; the products of one order
+    // are left out where the others' half has only the other.
+    again();
+    Parts<T, kParts> xp[2], yp[2], zp[2];
+    auto pairs = [&](auto kt_, auto before_, auto after_) {
+      constexpr int kt = decltype(kt_)::value;
+      constexpr bool Before = decltype(before_)::value, After = decltype(after_)::value;
+      float x[8], y[8], z[8], hi[8], lo[8];
+      eight(&G.hi[32 * kt + 8 * g], hi);
+      eight(&G.lo[32 * kt + 8 * g], lo);
+      const float own_hi = G.hi[own], own_lo = G.lo[own];
+      f32x4_t ou[2], uo[2], vu[2], uv[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) ou[i] = uo[i] = vu[i] = uv[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int ks = 0; ks < C::KS; ++ks) {
+        Parts<T, kParts> u, v;
+        Parts<T, 1> o;
+        if constexpr (Before) o = gradient(own, ks), v = vectors(1, w, ks);
+        if constexpr (After) u = vectors(0, w, ks);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int b = 2 * kt + i;
+          if constexpr (Before) {
+            const Parts<T, kParts> a = vectors(0, b, ks);
+            mma_parts<T>(uo[i], a, o);
+            mma_parts<T>(uv[i], a, v);
+          }
+          if constexpr (After) {
+            mma_parts<T>(vu[i], vectors(1, b, ks), u);
+            mma_parts<T>(ou[i], gradient(row_of(b, n), ks), u);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = 4 * i + r, t = 32 * kt + 8 * g + j;
+          const float away = (own_hi - hi[j]) + (own_lo - lo[j]);
+          const bool before = After ? Before && t <= own : true, after = Before ? After && t >= own : true;
+          const float f = __builtin_amdgcn_exp2f(before ? away : -away), sf = P.scale * f;
+          if constexpr (Before) x[j] = before ? sf * uo[i][r] : 0.0f;
+          if constexpr (After) y[j] = after ? sf * ou[i][r] : 0.0f;
+          if constexpr (Before && After) z[j] = t == own ? 0.0f : -f * (before ? uv[i][r] : vu[i][r]);
+          else z[j] = -f * (Before ? uv[i][r] : vu[i][r]);
+        }
+      if constexpr (Before) split(xp[kt], x);
+      if constexpr (After) split(yp[kt], y);
+      split(zp[kt], z);
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    if (half) {
+      pairs(I0{}, std::true_type{}, std::false_type{});
+      pairs(I1{}, std::true_type{}, std::true_type{});
+    } else {
+      pairs(I0{}, std::true_type{}, std::true_type{});
+      pairs(I1{}, std::false_type{}, std::true_type{});
+    }
+    again();
+    Parts<T, kParts> u[C::KS], v[C::KS];
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) {
+      u[ks] = vectors(0, w, ks);
+      v[ks] = vectors(1, w, ks);
+    }
+    if (own < live) {
+#pragma unroll
+      for (int ks = 0; ks < C::KS; ++ks) {
+        u32x4_t y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          y[j] = pack_bf16x2(bf16_lo(v[ks].v[0][j]) + bf16_lo(v[ks].v[1][j]),
+                             bf16_hi(v[ks].v[0][j]) + bf16_hi(v[ks].v[1][j]));
+        *reinterpret_cast<u32x4_t*>(dv + (vrow + own) * D + 32 * ks + 8 * g) = y;
+      }
+    }
+    lds_barrier();
+    again();
+    auto states = [&](int cc, int to) {
+      const T* from = reinterpret_cast<const T*>(S + slot * (D * D)) + cc * (2 * D * 32);
+      rows_to_lds<T, B, 2 * D>(at_lds + to * kHalf, from, 2 * D, w, lane);
+      from = reinterpret_cast<const T*>(N + slot * (D * D)) + cc * (2 * D * 32);
+      rows_to_lds<T, B, 2 * D>(at_lds + to * kHalf + 2 * D * B::kRow, from, 2 * D, w, lane);
+    };
+    rows_to_lds<T, C>(at_lds, k + krow * D, live, w, lane);
+    rows_to_lds<T, C>(at_lds + C::kTileBytes, q + krow * D, live, w, lane);
+    states(0, 1);
+    wait_vm<0>();
+    lds_barrier();
+    auto apply = [&](auto kt_, auto before_, auto after_) {
+      constexpr int kt = decltype(kt_)::value;
+#pragma unroll
+      for (int c = 0; c < C::NB; ++c) {
+        Parts<T, 1> kc, qc;
+        kc.v[0] = key_column<T, C>(ldsK, c, kt, lane);
+        mma_parts<T>(ak[c], kc, zp[kt]);
+        if constexpr (decltype(before_)::value) mma_parts<T>(aq[c], kc, xp[kt]);
+        if constexpr (decltype(after_)::value) {
+          qc.v[0] = key_column<T, C>(ldsQ, c, kt, lane);
+          mma_parts<T>(ak[c], qc, yp[kt]);
+        }
+        if (c & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (half) {
+      apply(I0{}, std::true_type{}, std::false_type{});
+      apply(I1{}, std::true_type{}, std::true_type{});
+    } else {
+      apply(I0{}, std::true_type{}, std::true_type{});
+      apply(I1{}, std::false_type{}, std::true_type{});
+    }
+    again();
+    Parts<T, 1> o[C::KS];
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) o[ks] = gradient(own, ks);
+    const float into = G.into[own], rest = G.rest[own], scaled = P.scale * into;
+#pragma unroll
+    for (int cc = 0; cc < C::KS; ++cc) {
+      if (cc + 1 < C::KS) {
+        lds_barrier();  // nobody reads the half before this one any more
+        states(cc + 1, cc & 1);
+      }
+      const unsigned char* at = lds + ((cc & 1) ^ 1) * kHalf;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        f32x4_t so = {0.0f, 0.0f, 0.0f, 0.0f}, sv = so, nu = so;
+#pragma unroll
+        for (int kt = 0; kt < C::KS; ++kt) {
+          Parts<T, kParts> a;
+#pragma unroll
+          for (int j = 0; j < kParts; ++j) a.v[j] = key_column<T, B>(at + j * D * B::kRow, i, kt, lane);
+          mma_parts<T>(so, a, o[kt]);
+          mma_parts<T>(sv, a, v[kt]);
+#pragma unroll
+          for (int j = 0; j < kParts; ++j) a.v[j] = key_column<T, B>(at + (2 + j) * D * B::kRow, i, kt, lane);
+          mma_parts<T>(nu, a, u[kt]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        f32x4_t &x = aq[2 * cc + i], &y = ak[2 * cc + i];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[r] = fmaf(scaled, so[r], x[r]);
+          y[r] = fmaf(rest, nu[r], fmaf(-into, sv[r], y[r]));
+        }
+      }
+      if (cc + 1 < C::KS) wait_vm<0>();
+    }
+  }
+  if (own >= live) return;
+#pragma unroll
+  for (int ks = 0; ks < C::KS; ++ks) {
+    const int64_t at = (krow + own) * D + 32 * ks + 8 * g;
+    auto rounded = [&](const f32x4_t& a, const f32x4_t& b) {
+      return (u32x4_t){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+    };
+    *reinterpret_cast<u32x4_t*>(dq + at) = rounded(aq[2 * ks], aq[2 * ks + 1]);
+    *reinterpret_cast<u32x4_t*>(dk + at) = rounded(ak[2 * ks], ak[2 * ks + 1]);
+  }
 }
-template <typename T>
-__device__ __forceinline__ Parts<T, 1> exact(const float* x) {
-  Parts<T, 1> p;
+
+__device__ __forceinline__ float value_at(__amdgpu_buffer_rsrc_t r, int at) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (uint32_t)(4 * at), 0, 0));
+}
+__device__ __forceinline__ Parts<float, 1> exact(const float* x) {
+  Parts<float, 1> p;
   p.set(x);
   return p;
 }
 
-// Wave w takes the tokens row_of(w, ..) of a tile as its own.
-template <typename T, int D>
+// fp32: the same in its order, operands gathered from memory.
+template <int D>
 __global__ void __launch_bounds__(kThreads)
-grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout, const int32_t* cu,
-             const Gates* gates, const float* S, const float* N, const float* E, const float* F, T* dq, T* dk, T* dv) {
-  using C = DS<T, D, 4, 1>;
+grads_kernel(DeltaPlan P, TileSpans tiles, const float* q, const float* k, const float* dout, const int32_t* cu,
+             const unsigned char* packs, const float* S, const float* N, const float* E, const float* F, float* dq,
+             float* dk, float* dv) {
+  using T = float;
+  using C = DS<T, D, 4>;
+  using Pack = Packed<T, 3>;
   __shared__ __attribute__((aligned(16))) Gates G;
   Span sp;
   if (!find_span<kThreads>(tiles, cu, blockIdx.x, &sp)) return;
@@ -64,7 +308,8 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
     const __amdgpu_buffer_rsrc_t ro = make_rsrc(dout + vrow * D, bytes);
     __syncthreads();
     if (threadIdx.x < kGateBytes / 16)
-      reinterpret_cast<u32x4_t*>(&G)[threadIdx.x] = reinterpret_cast<const u32x4_t*>(gates + slot)[threadIdx.x];
+      reinterpret_cast<u32x4_t*>(&G)[threadIdx.x] = 
+          reinterpret_cast<const u32x4_t*>(packs + slot * Pack::kBlock + Pack::kBytes)[threadIdx.x];
     __syncthreads();
     const float *St = S + slot * (D * D), *Nt = N + slot * (D * D);
     const float *Et = E + slot * (D * kDeltaTile), *Ft = F + slot * (D * kDeltaTile);
@@ -74,24 +319,24 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
     };
     auto gradient = [&](int t, int ks, float* x) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = value_at<T>(ro, t * D + 32 * ks + 8 * g + j);
+      for (int j = 0; j < 8; ++j) x[j] = value_at(ro, t * D + 32 * ks + 8 * g + j);
     };
-    Parts<T, kParts> u[C::KS], v[C::KS];
+    Parts<T, 1> u[C::KS], v[C::KS];
     Parts<T, 1> o[C::KS];
     const float beta = G.beta[own];
 #pragma unroll
     for (int ks = 0; ks < C::KS; ++ks) {
       float x[8];
       vectors(Et, own, ks, beta, x);
-      u[ks].set(x);
+      split(u[ks], x);
       vectors(Ft, own, ks, beta, x);
-      v[ks].set(x);
+      split(v[ks], x);
       if (own < live) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dv[(vrow + own) * D + 32 * ks + 8 * g + j] = narrow1<T>(x[j]);
+        for (int j = 0; j < 8; ++j) dv[(vrow + own) * D + 32 * ks + 8 * g + j] = x[j];
       }
       gradient(own, ks, x);
-      o[ks] = exact<T>(x);
+      o[ks] = exact(x);
     }
     const float into = G.into[own], rest = G.rest[own];
 #pragma unroll
@@ -100,15 +345,15 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
         float x[8];
-        Parts<T, kParts> a;
+        Parts<T, 1> a;
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = St[(32 * ks + 8 * g + j) * D + 16 * c + n];
-        a.set(x);
+        split(a, x);
         mma_parts<T>(so, a, o[ks]);
         mma_parts<T>(sv, a, v[ks]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = Nt[(32 * ks + 8 * g + j) * D + 16 * c + n];
-        a.set(x);
+        split(a, x);
         mma_parts<T>(nu, a, u[ks]);
       }
 #pragma unroll
@@ -130,16 +375,16 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
 #pragma unroll
         for (int ks = 0; ks < C::KS; ++ks) {
           float f[8];
-          Parts<T, kParts> a;
+          Parts<T, 1> a;
           vectors(Et, other, ks, bo, f);
-          a.set(f);
+          split(a, f);
           mma_parts<T>(uo, a, o[ks]);
           mma_parts<T>(uv, a, v[ks]);
           vectors(Ft, other, ks, bo, f);
-          a.set(f);
+          split(a, f);
           mma_parts<T>(vu, a, u[ks]);
           gradient(other, ks, f);
-          mma_parts<T>(ou, exact<T>(f), u[ks]);
+          mma_parts<T>(ou, exact(f), u[ks]);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -151,19 +396,19 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
           z[j] = t < own ? -f * uv[r] : t > own ? -f * vu[r] : 0.0f;
         }
       }
-      Parts<T, kParts> xp, yp, zp;
-      xp.set(x);
-      yp.set(y);
-      zp.set(z);
+      Parts<T, 1> xp, yp, zp;
+      split(xp, x);
+      split(yp, y);
+      split(zp, z);
 #pragma unroll
       for (int c = 0; c < C::NB; ++c) {
         float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = value_at<T>(rk, (32 * kt + 8 * g + j) * D + 16 * c + n);
-        const Parts<T, 1> kc = exact<T>(f);
+        for (int j = 0; j < 8; ++j) f[j] = value_at(rk, (32 * kt + 8 * g + j) * D + 16 * c + n);
+        const Parts<T, 1> kc = exact(f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = value_at<T>(rq, (32 * kt + 8 * g + j) * D + 16 * c + n);
-        const Parts<T, 1> qc = exact<T>(f);
+        for (int j = 0; j < 8; ++j) f[j] = value_at(rq, (32 * kt + 8 * g + j) * D + 16 * c + n);
+        const Parts<T, 1> qc = exact(f);
         mma_parts<T>(aq[c], kc, xp);
         mma_parts<T>(ak[c], kc, zp);
         mma_parts<T>(ak[c], qc, yp);
@@ -176,8 +421,8 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int64_t at = (krow + own) * D + 16 * c + 4 * g + r;
-      dq[at] = narrow1<T>(aq[c][r]);
-      dk[at] = narrow1<T>(ak[c][r]);
+      dq[at] = aq[c][r];
+      dk[at] = ak[c][r];
     }
 }
 
@@ -239,8 +484,8 @@ gbla_status launch_delta_grads(const DeltaPlan& p, const void* q, const void* k,
   return by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    hipLaunchKernelGGL((grads_kernel<T, D>), dim3(p.tiles, p.heads), dim3(kThreads), 0, st, p, tile_spans(p),
-                       (const T*)q, (const T*)k, (const T*)dout, cu, reinterpret_cast<const Gates*>(base + p.off_gates),
+    hipLaunchKernelGGL((grads_kernel<D>), dim3(p.tiles, p.heads), dim3(kThreads), 0, st, p, tile_spans(p),
+                       (const T*)q, (const T*)k, (const T*)dout, cu, base + p.off_pack,
                        floats(p.off_S), floats(p.off_N), floats(p.off_E), floats(p.off_F), (T*)dq, (T*)dk, (T*)dv);
     hipLaunchKernelGGL(decay_kernel, dim3(p.grid_units, p.value_heads), dim3(kThreads), 0, st, p, cu, S0, dS0,
                        floats(p.off_B), floats(p.off_D), floats(p.off_do_o), floats(p.off_dv_v), dlog_decay);

@@ -77,7 +77,6 @@ gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backwar
     off = align_up(off + bytes, 256);
     return at;
   };
-  q.off_gates = take((size_t)most * q.value_heads * kGateBytes);
   q.off_pack = take((size_t)most * q.value_heads * kPackBytes);
   const size_t states = (size_t)cap * q.value_heads * q.d * q.d * sizeof(float);
   q.off_B = take(states);

@@ -23,11 +23,11 @@ __device__ __forceinline__ int row_of(int b, int n) {
   return 32 * (b >> 1) + 8 * (n >> 2) + 4 * (b & 1) + (n & 3);
 }
 
-// Sizes of a kernel of NWAVES waves that each own COLS column blocks.
-template <typename T, int DIM, int NWAVES, int COLS>
+// Sizes of a kernel of NWAVES waves.
+template <typename T, int DIM, int NWAVES>
 struct DS {
   static constexpr int D = DIM;
-  static constexpr int NW = NWAVES, CB = COLS;
+  static constexpr int NW = NWAVES;
   static constexpr int NT = 64 * NW;
   static constexpr int ES = (int)sizeof(T);
   static constexpr int kRow = D * ES;     // bytes of a row in memory
@@ -57,15 +57,68 @@ struct Gates {
   float beta[kDeltaTile];
   float into[kDeltaTile];  // decay from the tile's start through the token
   float rest[kDeltaTile];  // decay from the token to the tile's end
+  float late[kDeltaTile];  // that times beta
   float whole;             // decay over the tile
   int good;                // tokens before the first whose key or gates are not finite
   float pad[62];
 };
 static_assert(sizeof(Gates) == kGateBytes, "size of Gates");
 
-// decay from token s (of log2 hi, lo) to token t >= s
-__device__ __forceinline__ float decay_between(const Gates& G, int t, float hi, float lo) {
-  return __builtin_amdgcn_exp2f((G.hi[t] - hi) + (G.lo[t] - lo));
+// Eight consecutive values of an array in LDS.
+__device__ __forceinline__ void eight(const float* p, float* x) {
+  const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p), b = *reinterpret_cast<const f32x4_t*>(p + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
+}
+// x[j], a product of the tokens `own` and other + j, times `scale` and the decay between the two;
+// zero where the other is not at or before (Before) / at or after it.  By selects: what is loaded
+// under a condition is waited for one by one.
+template <bool Before>
+__device__ __forceinline__ void decayed(const Gates& G, int own, int other, float scale, float* x) {
+  const float oh = G.hi[own], ol = G.lo[own];
+  float hi[8], lo[8];
+  eight(&G.hi[other], hi);
+  eight(&G.lo[other], lo);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float away = (oh - hi[j]) + (ol - lo[j]);
+    const float f = __builtin_amdgcn_exp2f(Before ? away : -away);
+    const bool in = Before ? other + j <= own : other + j >= own;
+    const float y = x[j] * (scale * f);
+    x[j] = in ? y : 0.0f;
+  }
+}
+
+// x - (the bf16 in the low / high half of h), exactly, for an h that rounds x: one instruction
+// where unpacking and subtracting are two.  The factors (-1, 0) are kept in scalar registers:
+// as an inline constant -1.0 stands for its fp32 bits, whose high half is the factor.
+__device__ __forceinline__ float rest_lo(uint32_t h, float x) {
+  uint32_t f = 0x0000bf80u;
+  asm("" : "+s"(f));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, h), __builtin_bit_cast(bf16x2_t, f), x, false);
+}
+__device__ __forceinline__ float rest_hi(uint32_t h, float x) {
+  uint32_t f = 0xbf800000u;
+  asm("" : "+s"(f));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, h), __builtin_bit_cast(bf16x2_t, f), x, false);
+}
+// Eight fp32 values as an operand in N parts.
+template <typename T, int N>
+__device__ __forceinline__ void split(Parts<T, N>& p, const float* x) {
+  if constexpr (sizeof(T) == 4) {
+    p.set(x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float a = x[2 * j], b = x[2 * j + 1];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint32_t h = pack_bf16x2(a, b);
+        p.v[i][j] = h;
+        if (i + 1 < N) a = rest_lo(h, a), b = rest_hi(h, b);
+      }
+    }
+  }
 }
 
 // c += a b of two operands in parts, the smaller products first; of products with a
@@ -145,26 +198,53 @@ struct RowsLoad {
   }
   // Lowers *first to the row of this thread's first piece with an infinite or NaN value.
   __device__ __forceinline__ void find_bad(int* first) const {
-    bool any = false;
-    bool bad[N];
+    // one added to exponents that are all ones carries out of them
+    constexpr uint32_t kExponents = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u;
+    constexpr uint32_t kOnes = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+    constexpr uint32_t kCarries = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    uint32_t bad[N], any = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      bad[i] = false;
+      bad[i] = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w = x[i][j];
-        if constexpr (sizeof(T) == 2) bad[i] |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-        else bad[i] |= (w & 0x7f800000u) == 0x7f800000u;
-      }
+      for (int j = 0; j < 4; ++j) bad[i] |= (x[i][j] & kExponents) + kOnes;
       any |= bad[i];
     }
-    if (__builtin_expect(__ballot(any) != 0, 0)) {
+    if (__builtin_expect(__ballot((any & kCarries) != 0) != 0, 0)) {
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (bad[i]) atomicMin(first, (i * C::NT + (int)threadIdx.x) / per);
+        if (bad[i] & kCarries) atomicMin(first, (i * C::NT + (int)threadIdx.x) / per);
     }
   }
 };
+
+// A tile's rows, and `bytes` of a block, straight from memory to LDS (bf16: its tiles' rows lie
+// next to each other there): a kilobyte an instruction, the waves in turn.  What they load has
+// arrived once its waves have waited for all of their loads and met at a barrier.
+template <typename T, typename C, int Rows = kDeltaTile>
+__device__ __forceinline__ void rows_to_lds(uint32_t lds, const T* first, int live, int w, int lane) {
+  constexpr int per = C::kRow / 16, step = 64 / per;  // units of a row, rows of an instruction
+  const int rows = live < 0 ? 0 : live > Rows ? Rows : live;
+  const u32x4_t r = rsrc_sgprs(first, (uint32_t)(rows * C::kRow));
+#pragma unroll
+  for (int i = 0; i < Rows / step / C::NW; ++i) {
+    const int at = i * C::NW + w, row = at * step + lane / per;
+    dma16(r, lds + 1024 * at, (uint32_t)(row * C::kRow + ((lane % per) ^ C::swizzle(row)) * 16));
+  }
+}
+template <typename C, int Bytes>
+__device__ __forceinline__ void block_to_lds(uint32_t lds, const void* from, bool any, int w, int lane) {
+  static_assert(Bytes % 1024 == 0, "whole instructions");
+  const u32x4_t r = rsrc_sgprs(from, any ? (uint32_t)Bytes : 0u);
+#pragma unroll
+  for (int i = 0; i < (Bytes / 1024 + C::NW - 1) / C::NW; ++i) {
+    const int at = i * C::NW + w;
+    if (at < Bytes / 1024) dma16(r, lds + 1024 * at, (uint32_t)(1024 * at + 16 * lane));
+  }
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p);
+}
 
 // Rows from `from` on of a tile in LDS become zeros.
 template <typename C>
@@ -181,6 +261,7 @@ template <typename T, int N>
 struct Packed {
   static constexpr int kPieces = sizeof(T) == 2 ? N : 2;
   static constexpr int kBytes = 6 * kPieces * 64 * 16;
+  static constexpr int kBlock = kBytes + kGateBytes;  // with the tile's gates behind it
   static __device__ __forceinline__ Parts<T, N> get(const unsigned char* pack, int pair, int lane) {
     const u32x4_t* p = reinterpret_cast<const u32x4_t*>(pack) + pair * (64 * kPieces) + lane;
     Parts<T, N> x;
@@ -204,7 +285,46 @@ struct Packed {
   }
 };
 
-// Copies of a tile's packed triangle and gates on their way to LDS.
+// Eight values of a column, tokens t .. t + 7: from the first that is not finite on they become
+// zeros, and *first is lowered to its token.
+template <typename T>
+__device__ __forceinline__ void drop_bad(typename Num<T>::V8& v, int t, int* first) {
+  float x[8];
+  Num<T>::widen(v, x);
+  float z = 0.0f;  // stays 0 while all are finite
+#pragma unroll
+  for (int j = 0; j < 8; ++j) z = fmaf(x[j], 0.0f, z);
+  if (__builtin_expect(__ballot(z != 0.0f) != 0, 0)) {
+    int bad = 8;
+#pragma unroll
+    for (int j = 7; j >= 0; --j) bad = isfinite(x[j]) ? bad : j;
+    if (bad < 8) atomicMin(first, t + bad);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < bad ? x[j] : 0.0f;
+    Parts<T, 1> p;
+    p.set(x);
+    v = p.v[0];
+  }
+}
+
+// x[b] += the packed lower triangle's rows of block b times `by` (Swapped: by's transpose times
+// theirs).  One operand ahead: more cost registers, none the wait for LDS.
+template <typename T, int N, bool Swapped>
+__device__ __forceinline__ void triangle(f32x4_t (&x)[4], const unsigned char* pack, const Parts<T, N> (&by)[2],
+                                         int lane) {
+  Parts<T, N> next = Packed<T, N>::get(pack, 0, lane);
+#pragma unroll
+  for (int pair = 0; pair < 6; ++pair) {
+    const int b = pair < 2 ? pair : 2 + (pair >> 2), ks = pair < 2 ? 0 : pair & 1;
+    const Parts<T, N> m = next;
+    if (pair < 5) next = Packed<T, N>::get(pack, pair + 1, lane);
+    if constexpr (Swapped) mma_parts<T>(x[b], by[ks], m);
+    else mma_parts<T>(x[b], m, by[ks]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// A tile's packed triangle and gates on their way to LDS.
 template <typename C, int Bytes>
 struct BlockLoad {
   static constexpr int N = (Bytes / 16 + C::NT - 1) / C::NT;
@@ -224,65 +344,70 @@ struct BlockLoad {
   }
 };
 
-// A wave's blocks of a state X[key channel][value channel] in fp32: s[c][i][r] is row
-// row_of(i, 4 g + r), column 16 (cb0 + c) + n.
+// A wave's column block of a state X[key channel][value channel] in fp32: s[i][r] is row
+// row_of(i, 4 g + r), column col0 + n.
 template <typename T, typename C>
 struct Columns16 {
-  f32x4_t s[C::CB][C::NB];
+  f32x4_t s[C::NB];
   __device__ __forceinline__ void fill(float x) {
 #pragma unroll
-    for (int c = 0; c < C::CB; ++c)
-#pragma unroll
-      for (int i = 0; i < C::NB; ++i) s[c][i] = (f32x4_t){x, x, x, x};
+    for (int i = 0; i < C::NB; ++i) s[i] = (f32x4_t){x, x, x, x};
   }
   __device__ __forceinline__ void identity(int col0, int lane) {
 #pragma unroll
-    for (int c = 0; c < C::CB; ++c)
+    for (int i = 0; i < C::NB; ++i)
 #pragma unroll
-      for (int i = 0; i < C::NB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          s[c][i][r] = row_of(i, 4 * (lane >> 4) + r) == col0 + 16 * c + (lane & 15) ? 1.0f : 0.0f;
+      for (int r = 0; r < 4; ++r) s[i][r] = row_of(i, 4 * (lane >> 4) + r) == col0 + (lane & 15) ? 1.0f : 0.0f;
   }
   // m: [row][column]
   __device__ __forceinline__ void load(const float* m, int col0, int lane) {
 #pragma unroll
-    for (int c = 0; c < C::CB; ++c)
+    for (int i = 0; i < C::NB; ++i)
 #pragma unroll
-      for (int i = 0; i < C::NB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          s[c][i][r] = m[row_of(i, 4 * (lane >> 4) + r) * C::D + col0 + 16 * c + (lane & 15)];
+      for (int r = 0; r < 4; ++r) s[i][r] = m[row_of(i, 4 * (lane >> 4) + r) * C::D + col0 + (lane & 15)];
   }
   __device__ __forceinline__ void store(float* m, int col0, int lane) const {
 #pragma unroll
-    for (int c = 0; c < C::CB; ++c)
+    for (int i = 0; i < C::NB; ++i)
 #pragma unroll
-      for (int i = 0; i < C::NB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          m[row_of(i, 4 * (lane >> 4) + r) * C::D + col0 + 16 * c + (lane & 15)] = s[c][i][r];
+      for (int r = 0; r < 4; ++r) m[row_of(i, 4 * (lane >> 4) + r) * C::D + col0 + (lane & 15)] = s[i][r];
   }
-  // m: [column][row]
-  __device__ __forceinline__ void store_columns(float* m, int col0, int lane) const {
-#pragma unroll
-    for (int c = 0; c < C::CB; ++c) {
-      float* to = m + (col0 + 16 * c + (lane & 15)) * C::D + 8 * (lane >> 4);
-#pragma unroll
-      for (int i = 0; i < C::NB; ++i)
-        *reinterpret_cast<f32x4_t*>(to + 32 * (i >> 1) + 4 * (i & 1)) = s[c][i];
-    }
-  }
-  // K step ks of column block c as an operand.
+  // K step ks as an operand.
   template <int N>
-  __device__ __forceinline__ Parts<T, N> operand(int c, int ks) const {
-    const f32x4_t &a = s[c][2 * ks], &b = s[c][2 * ks + 1];
+  __device__ __forceinline__ Parts<T, N> operand(int ks) const {
+    const f32x4_t &a = s[2 * ks], &b = s[2 * ks + 1];
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     Parts<T, N> p;
-    p.set(x);
+    split(p, x);
     return p;
   }
 };
+
+// K step ks of a state's column block for the gradients' kernel, into m of D * D words.  bf16: the
+// first two parts, [ks][part][column][32 rows], so that a wave writes a kilobyte on end and 32
+// rows are read as one block; fp32: [column][row].
+template <typename T, typename C, int N>
+__device__ __forceinline__ void store_columns(float* m, int ks, int col0, int lane, const Parts<T, N>& p) {
+  const int col = col0 + (lane & 15), g = lane >> 4;
+  if constexpr (sizeof(T) == 2) {
+    u32x4_t* to = reinterpret_cast<u32x4_t*>(m) + (2 * ks * C::D + col) * 4 + g;
+    to[0] = p.v[0];
+    to[4 * C::D] = p.v[1];
+  } else {
+    f32x4_t* to = reinterpret_cast<f32x4_t*>(m + col * C::D + 32 * ks + 8 * g);
+    to[0] = p.v[0].a;
+    to[1] = p.v[0].b;
+  }
+}
+
+// by[ks] = f times y's values of the tokens 32 ks + 8 g + j, in N parts.
+template <typename T, int N>
+__device__ __forceinline__ void weighted(Parts<T, N>& by, const float* f, const f32x4_t& a, const f32x4_t& b) {
+  float x[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = f[j] * a[j], x[4 + j] = f[4 + j] * b[j];
+  split(by, x);
+}
 
 // Sums over a wave's 16 value channels (lanes n) of a lane's values of its 16 tokens, x[ks][j]
 // of token 32 ks + 8 g + j: halving exchanges, after which lane n has token

@@ -52,6 +52,34 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, ui
   void* p = reinterpret_cast<void*>(((uint64_t)hi << 32) | lo);
   return __builtin_amdgcn_make_buffer_rsrc(p, 0, n, 0x00020000);
 }
+// A buffer resource over `bytes` bytes from `base`, as four scalar registers
+// for the assembly loads below (the same descriptor as make_rsrc).
+__device__ __forceinline__ u32x4_t rsrc_sgprs(const void* base, uint32_t bytes) {
+  const uint64_t ad = reinterpret_cast<uint64_t>(base);
+  return u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)ad),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(ad >> 32)),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+
+// 16 bytes per lane from the buffer into LDS at base + 16 * lane (M0 = base;
+// one wait state after writing M0).  Assembly, so that the compiler neither
+// tracks these loads (the step loop waits for them explicitly, by count) nor
+// moves LDS accesses across them.
+// M is the LDS byte address (wave-uniform).
+__device__ __forceinline__ void dma16(const u32x4_t& r, uint32_t m, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :
+               : "v"(off), "s"(r), "s"(m)
+               : "memory", "m0");
+}
+
+// s_waitcnt vmcnt(N), the other counters left alone (gfx9 encoding).
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
+}
+
 constexpr uint32_t kOutOfRange = 0x80000000u;
 
 // Taps of one tensor (0 = q, 1 = k, 2 = v), head h, channel c, right-aligned

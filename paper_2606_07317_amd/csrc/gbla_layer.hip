@@ -55,27 +55,6 @@ constexpr int kDmaPerTile = kTileBytes / (kProjThreads * 16);
 // rows r and r + 8 collided, and 49% of the LDS cycles were conflicts.)
 __device__ __forceinline__ int tile_off(int r, int c) { return r * kRowBytes + ((c ^ ((r >> 1) & 7)) << 4); }
 
-// A buffer resource over `bytes` bytes from `base`, as four scalar registers
-// for the assembly loads below (the same descriptor as make_rsrc).
-__device__ __forceinline__ u32x4_t rsrc_sgprs(const void* base, uint32_t bytes) {
-  const uint64_t ad = reinterpret_cast<uint64_t>(base);
-  return u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)ad),
-                 (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(ad >> 32)),
-                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
-}
-
-// 16 bytes per lane from the buffer into LDS at base + 16 * lane (M0 = base;
-// one wait state after writing M0).  Assembly, so that the compiler neither
-// tracks these loads (the step loop waits for them explicitly, by count) nor
-// moves LDS accesses across them.
-// M is the LDS byte address (wave-uniform).
-__device__ __forceinline__ void dma16(const u32x4_t& r, uint32_t m, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-               :
-               : "v"(off), "s"(r), "s"(m)
-               : "memory", "m0");
-}
-
 // The lane index, computed where it is used: a volatile statement cannot be
 // hoisted, so addresses formed from it are not held (and spilled) across
 // the tile loop, where each reload's wait would drain the loads in flight.
@@ -87,13 +66,6 @@ __device__ __forceinline__ int lane_now() {
 
 // s_waitcnt lgkmcnt(0), the other counters left alone (gfx9 encoding).
 __device__ __forceinline__ void wait_lgkm0() { __builtin_amdgcn_s_waitcnt(0xC07F); }
-
-// s_waitcnt vmcnt(N), the other counters left alone (gfx9 encoding).
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  static_assert(N >= 0 && N < 64, "vmcnt");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
-}
 
 // Workgroup barrier with no fence: a fence would make each wave wait for all
 // of its loads in flight, the later K steps' too.  Each wave has waited for

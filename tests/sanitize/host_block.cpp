@@ -36,7 +36,6 @@ static void check(const DeltaPlan& p, bool backward) {
   REQUIRE(p.units >= 1 && p.tiles >= p.units && (p.single ? p.grid_units == p.nseq : p.grid_units == p.units));
   const size_t tiles = (size_t)p.tiles * p.value_heads, units = (size_t)p.units * p.value_heads;
   const size_t state = (size_t)p.d * p.d * sizeof(float);
-  REQUIRE(p.off_gates + tiles * kGateBytes <= p.off_pack);
   REQUIRE(p.off_pack + tiles * kPackBytes <= p.off_B);
   REQUIRE(p.off_B + units * state <= p.off_M);
   REQUIRE(p.off_M + units * state <= p.total_bytes);
