@@ -12,7 +12,7 @@
 namespace gbla {
 
 constexpr int kDeltaTile = 64;      // tokens of a tile
-constexpr int kDeltaMaxUnit = 512;  // tokens of a unit, at most
+constexpr int kDeltaMaxUnit = 1024;  // tokens of a unit, at most
 constexpr int kGateBytes = 1792;         // a tile's gates (struct Gates)
 constexpr int kPackBytes = 6 * 64 * 48 + kGateBytes;  // a tile's triangle as operands (Packed), at most, and gates
 
@@ -36,8 +36,9 @@ struct DeltaPlan {
   // Workspace (bytes from its base)
   size_t off_pack;   // [V, tiles] packed triangles and gates
   size_t off_B;      // [V, units, d, d] fp32: what a unit adds; then the state before each unit
-  size_t off_M;      // [V, units, d, d] fp32: what a unit does to the state before it
+  size_t off_M;      // [V, units, d, d] fp32: what a unit does to the state before it, transposed
   // Backward:
+  size_t off_MT;     // [V, units, d, d] fp32: the maps, transposed against off_M
   size_t off_packT;  // ... with the triangles transposed
   size_t off_D;      // [V, units, d, d] fp32: the gradient of the state after each unit
   size_t off_S;      // [V, tiles, d, d] fp32: the state before each tile, [value][key channel]

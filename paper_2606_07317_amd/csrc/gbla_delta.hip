@@ -208,6 +208,7 @@ struct BackOut {
   const void* dout;
   const float* F;     // the gradient of u
   float *S, *E, *do_o, *dbeta;
+  float* M;           // the maps for the gradients' scan
   bool final_gradient;  // the final state has one
 };
 
@@ -247,8 +248,8 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     if (map) S.identity(e0, lane);
     else S.fill(0.0f);
   } else {
-    const float* init = !P.single && (S0 || sp.idx > 0) ? recB + record : S0 ? S0 + pair * (D * D) : nullptr;
-    if (init) S.load(init, e0, lane);
+    if (!P.single && (S0 || sp.idx > 0)) S.load_record(recB + record, e0, lane);
+    else if (S0) S.load(S0 + pair * (D * D), e0, lane);
     else S.fill(0.0f);
   }
 
@@ -500,15 +501,20 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
       }
     }
   }
-  float* to = !Out ? (map ? recM : recB) + record
-              : !Back && final_state && sp.last ? final_state + pair * (D * D) : nullptr;
-  if (to) S.store(to, e0, lane);
+  if constexpr (!Out) {
+    if (!map) S.store_record(recB + record, e0, lane);
+    if (map) S.store_transposed(recM + record, e0, lane);
+    if (map && back.M) S.store_record(back.M + record, e0, lane);
+  } else if (!Back && final_state && sp.last) {
+    S.store(final_state + pair * (D * D), e0, lane);
+  }
 }
 
 // The records become the state before each unit, in place: S -> M S + B from unit to unit.
 // A workgroup takes 16 value channels, wave w the key channels 16 w ..; the state passes from
 // wave to wave through LDS, in fp32, with fp32 products.  Back: from the last unit to the
-// first, with M's transpose, the gradient of the state after each unit.
+// first, with M's transpose, the gradient of the state after each unit.  A step takes the rows
+// 16 w .. of the map (Back: its columns), whose records hold four of their values in 16 bytes.
 template <int D, bool Back>
 __global__ void __launch_bounds__(4 * D)
 scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const float* recM) {
@@ -516,13 +522,16 @@ scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const 
   __shared__ __attribute__((aligned(16))) float lds[2][16 * kPitch];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int s = blockIdx.x / KS, e0 = 16 * (blockIdx.x % KS), h = blockIdx.y;
+  // The workgroups that read the same maps are eight apart: one L2 serves them.
+  const int pair = (int)(blockIdx.x / (8 * KS)) * 8 + (int)(blockIdx.x % 8), e0 = 16 * (int)(blockIdx.x / 8 % KS);
+  if (pair >= P.nseq * P.value_heads) return;
+  const int s = pair / P.value_heads, h = pair % P.value_heads;
   const int64_t len = P.ragged ? (int64_t)cu[s + 1] - cu[s] : P.rows;
   const int first = P.ragged ? first_slot(P, cu[s], s) : s * P.units_per_seq;
   const int units = units_of(len, P.unit);
   const size_t record = ((size_t)h * P.units + first) * (D * D);
-  float* B = recB + record + (16 * w + 4 * g) * D + e0 + n;
-  const float* M = recM + record + (Back ? 4 * g * D + 16 * w + n : (16 * w + n) * D + 4 * g);
+  f32x4_t* B = reinterpret_cast<f32x4_t*>(recB + record + e0 * D) + (4 * w + g) * 16 + n;
+  const f32x4_t* M = reinterpret_cast<const f32x4_t*>(recM + record + 16 * w * D) + g * 16 + n;
   f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
   struct Records {
     f32x4_t b, m[KS];
@@ -532,47 +541,54 @@ scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const 
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[r] = p[r * D];
   }
-  // The i-th unit of the walk.  The last has no record, and the first no map where it starts
-  // from zeros.
+  // The i-th unit of the walk.  What is read of the last, which has no record, is not used;
+  // the first has no map where it starts from zeros.
   auto unit = [&](int i) { return Back ? units - 1 - i : i; };
   auto fetch = [&](int i) {
     Records rec;
-    const bool any = i < units - 1, map = any && (i > 0 || S0);
-    const size_t at = (size_t)unit(min(i, units - 1)) * (D * D);
+    const size_t at = (size_t)unit(min(i, units - 1)) * (D * D / 4);
+    rec.b = B[at];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) rec.b[r] = any ? B[at + r * D] : 0.0f;
-#pragma unroll
-    for (int j = 0; j < KS; ++j) {
-      rec.m[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-      if (map) {
-        if constexpr (Back) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) rec.m[j][r] = M[at + (16 * j + r) * D];
-        } else {
-          rec.m[j] = *reinterpret_cast<const f32x4_t*>(M + at + 16 * j);
-        }
-      }
-    }
+    for (int j = 0; j < KS; ++j) rec.m[j] = M[at + 64 * j];
     return rec;
   };
-  Records rec = fetch(0);
-  for (int i = 0; i < units; ++i) {
-    float* sx = lds[i & 1];
+  if (units == 1) {
+    B[0] = x;
+    return;
+  }
+  // The next units' records are under way while one unit's are multiplied.
+  constexpr int kAhead = 2;
+  Records rec[kAhead];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) B[(size_t)unit(i) * (D * D) + r * D] = x[r];
-    if (i + 1 == units) break;
-    *reinterpret_cast<f32x4_t*>(&sx[n * kPitch + 16 * w + 4 * g]) = x;
-    const Records now = rec;
-    rec = fetch(i + 1);  // under way while this unit's are multiplied
-    lds_barrier();
-    f32x4_t z[2] = {now.b, {0.0f, 0.0f, 0.0f, 0.0f}};
+  for (int z = 0; z < kAhead; ++z)
+    if (z < units - 1) rec[z] = fetch(z);
+  if (!S0) {
 #pragma unroll
-    for (int j = 0; j < KS; ++j) {
-      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&sx[n * kPitch + 16 * j + 4 * g]);
+    for (int j = 0; j < KS; ++j) rec[0].m[j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // (steps behind the last keep the state and store it again: what is loaded and stored under a
+  // condition would be waited for earlier)
+  for (int i0 = 0; i0 < units; i0 += kAhead) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(now.m[j][r], y[r], z[r & 1], 0, 0, 0);
+    for (int a = 0; a < kAhead; ++a) {
+      const int i = i0 + a;
+      float* sx = lds[a & 1];
+      *reinterpret_cast<f32x4_t*>(&sx[n * kPitch + 16 * w + 4 * g]) = x;
+      B[(size_t)unit(min(i, units - 1)) * (D * D / 4)] = x;
+      lds_barrier();
+      f32x4_t y[KS], z[2] = {rec[a].b, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+      for (int j = 0; j < KS; ++j) y[j] = *reinterpret_cast<const f32x4_t*>(&sx[n * kPitch + 16 * j + 4 * g]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < KS; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          z[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(rec[a].m[j][r], y[j][r], z[r & 1], 0, 0, 0);
+      rec[a] = fetch(i + kAhead);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = i + 1 < units ? z[0][r] + z[1][r] : x[r];
     }
-    x = z[0] + z[1];
   }
 }
 
@@ -599,9 +615,10 @@ void launch_walk(const DeltaPlan& p, const void* q, const void* k, const void* v
 }
 template <int D, bool Back>
 void launch_scan(const DeltaPlan& p, const int32_t* cu, const float* S0, unsigned char* base, hipStream_t st) {
-  hipLaunchKernelGGL((scan_kernel<D, Back>), dim3(p.nseq * (D / 16), p.value_heads), dim3(4 * D), 0, st, p, cu, S0,
+  const int pairs = (p.nseq * p.value_heads + 7) / 8 * 8;
+  hipLaunchKernelGGL((scan_kernel<D, Back>), dim3(pairs * (D / 16)), dim3(4 * D), 0, st, p, cu, S0,
                      reinterpret_cast<float*>(base + (Back ? p.off_D : p.off_B)),
-                     reinterpret_cast<const float*>(base + p.off_M));
+                     reinterpret_cast<const float*>(base + (Back ? p.off_MT : p.off_M)));
 }
 
 }  // namespace
@@ -636,7 +653,7 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
     const BackOut back = {dout,         floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_do_o),
-                          dbeta, dfinal != nullptr};
+                          dbeta,        floats(p.off_MT), dfinal != nullptr};
     launch_prep<T, D>(p, k, log_decay, beta, cu, base, true, st);
     if (!p.single) {
       launch_walk<T, D, kRecords>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
@@ -655,7 +672,7 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
     const BackOut back = {dout,         floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_do_o),
-                          dbeta, dfinal != nullptr};
+                          dbeta,        floats(p.off_MT), dfinal != nullptr};
     launch_walk<T, D, kBack>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
   });
   if (done != GBLA_OK) return done;

@@ -57,11 +57,9 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
   const int e0 = 16 * w;
   const size_t record = ((size_t)h * P.units + sp.slot) * (D * D);
   Columns16<T, C> N;
-  const float* init = Records                                ? nullptr
-                      : !P.single && (dfinal || !sp.last) ? a.recD + record
-                      : dfinal                               ? dfinal + pair * (D * D)
-                                                             : nullptr;
-  if (init) N.load(init, e0, lane);
+  if (Records) N.fill(0.0f);
+  else if (!P.single && (dfinal || !sp.last)) N.load_record(a.recD + record, e0, lane);
+  else if (dfinal) N.load(dfinal + pair * (D * D), e0, lane);
   else N.fill(0.0f);
 
   const int64_t krow = first_row(P, sp, P.heads, h / P.group), vrow = first_row(P, sp, P.value_heads, h);
@@ -234,7 +232,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
       }
     }
   }
-  if (Records) N.store(a.recD + record, e0, lane);
+  if (Records) N.store_record(a.recD + record, e0, lane);
   else if (dS0 && sp.idx == 0) N.store(dS0 + pair * (D * D), e0, lane);
 }
 

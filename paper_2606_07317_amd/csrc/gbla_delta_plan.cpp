@@ -13,16 +13,25 @@ namespace {
 constexpr int64_t kMaxGroups = 4294967295LL / 512;
 constexpr int kMaxGridY = 65535;
 
-// Tokens of a unit (a power of two).
+// Tokens of a unit (a power of two): the largest that leaves 256 walks, a workgroup for each
+// compute unit; 1024 only where that leaves four times as many.  Measured (bf16, us): 8192
+// tokens, 8 heads of 64 with units of 128, 256, 512: 81, 69, 80; 16384 tokens, 8 heads of 128
+// with 256, 512, 1024: 279, 233, 268; 178000 packed tokens, 8 heads of 128 with 512, 1024:
+// 1916, 1786; backward, 58000 packed tokens, 8 heads of 128 with 256, 512, 1024: 2327, 2031, 2188.
 int32_t unit_tokens(const DeltaPlan& p) {
-  int32_t unit = kDeltaMaxUnit;
-  while (unit > 2 * kDeltaTile && p.tokens * p.value_heads < (int64_t)unit * 512) unit /= 2;
+  const int64_t all = p.tokens * p.value_heads;
+  int32_t unit = all >= 1024 * kDeltaMaxUnit ? kDeltaMaxUnit : kDeltaMaxUnit / 2;
+  while (unit > kDeltaTile && all < (int64_t)unit * 256) unit /= 2;
   return unit;
 }
 
-// Whether a workgroup walks a whole sequence.
-bool walk_whole(const DeltaPlan& p, int64_t longest) {
-  return longest <= 2 * kDeltaTile || longest * 256 <= p.tokens * p.value_heads;
+// Whether a workgroup walks a whole sequence: all are short, or there are walks enough of the
+// longest's length.  Measured (bf16, heads of 64; split, whole, in us): 1 x 256 tokens, 8 heads
+// 30, 27; 8 x 512 41, 45; 16 x 1024 92, 88; 16 x 4096 296, 315; 32 x 4096 583, 386; backward,
+// where a split sequence takes two launches more: 1 x 256 62, 70; 16 x 512 164, 148; 16 x 1024
+// 288, 278; 8 x 2048, 16 heads 460, 545; 16 x 2048, 16 heads 874, 695.
+bool walk_whole(const DeltaPlan& p, int64_t longest, bool backward) {
+  return longest <= (backward ? 128 : 256) || longest * (longest <= 1024 ? 128 : 256) <= p.tokens * p.value_heads;
 }
 
 }  // namespace
@@ -67,9 +76,9 @@ gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backwar
     q.units_per_seq = pieces(q.unit);
     q.units = q.units_per_seq * q.nseq;
   }
-  q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows) ? 1 : 0;
-  // the split's scan has a workgroup for every 16 value channels of a sequence's states
-  if ((int64_t)q.nseq * (q.d / 16) > kMaxGroups) q.single = 1;
+  q.single = walk_whole(q, ragged && s->max_seqlen < q.rows ? s->max_seqlen : q.rows, backward) ? 1 : 0;
+  // the split's scan has a workgroup for every 16 value channels of a state, in groups of eight
+  if (((int64_t)q.nseq * q.value_heads + 7) * (q.d / 16) > kMaxGroups) q.single = 1;
   q.grid_units = q.single ? q.nseq : q.units;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -85,6 +94,7 @@ gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backwar
     const size_t each = (size_t)most * q.value_heads, state = (size_t)q.d * q.d * sizeof(float);
     const size_t vectors = (size_t)q.d * kDeltaTile * sizeof(float);
     const size_t gate = (size_t)q.tokens * q.value_heads * sizeof(float);
+    q.off_MT = take(states);
     q.off_packT = take(each * kPackBytes);
     q.off_D = take(states);
     q.off_S = take(each * state);

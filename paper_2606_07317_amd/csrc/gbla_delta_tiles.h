@@ -372,6 +372,29 @@ struct Columns16 {
 #pragma unroll
       for (int r = 0; r < 4; ++r) m[row_of(i, 4 * (lane >> 4) + r) * C::D + col0 + (lane & 15)] = s[i][r];
   }
+  // Records between launches hold four rows of a column in 16 bytes, as the waves that load
+  // them have them: [block of 16 columns][row / 4][column][row % 4].
+  __device__ __forceinline__ void load_record(const float* m, int col0, int lane) {
+    const f32x4_t* p = reinterpret_cast<const f32x4_t*>(m + col0 * C::D) + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < C::NB; ++i) s[i] = p[4 * row_of(i, 4 * (lane >> 4))];
+  }
+  __device__ __forceinline__ void store_record(float* m, int col0, int lane) const {
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(m + col0 * C::D) + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < C::NB; ++i) p[4 * row_of(i, 4 * (lane >> 4))] = s[i];
+  }
+  // The transpose's record.
+  __device__ __forceinline__ void store_transposed(float* m, int col0, int lane) const {
+    const int col = col0 + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < C::NB; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = row_of(i, 4 * (lane >> 4) + r);
+        m[(row & ~15) * C::D + ((col >> 2) * 16 + (row & 15)) * 4 + (col & 3)] = s[i][r];
+      }
+  }
   // K step ks as an operand.
   template <int N>
   __device__ __forceinline__ Parts<T, N> operand(int ks) const {

@@ -30,7 +30,7 @@ static bool grid_ok(int64_t x, int64_t y, int threads) {
 static void check(const DeltaPlan& p, bool backward) {
   REQUIRE(grid_ok(p.tiles, p.value_heads, 256));
   REQUIRE(grid_ok(p.grid_units, p.value_heads, 4 * p.d));
-  if (!p.single) REQUIRE(grid_ok((int64_t)p.nseq * (p.d / 16), p.value_heads, 4 * p.d));
+  if (!p.single) REQUIRE(grid_ok(((int64_t)p.nseq * p.value_heads + 7) / 8 * 8 * (p.d / 16), 1, 4 * p.d));
   REQUIRE(p.group * p.heads == p.value_heads);
   REQUIRE(p.unit % kDeltaTile == 0 && p.unit >= kDeltaTile);
   REQUIRE(p.units >= 1 && p.tiles >= p.units && (p.single ? p.grid_units == p.nseq : p.grid_units == p.units));
