@@ -31,26 +31,30 @@ __device__ __forceinline__ double log2_decay(float g) {
   return (double)(g < -1e5f ? -1e5f : g) * 1.4426950408889634074;
 }
 
-// A tile's gates and its M.  Wave w takes the columns 16 w .. of the tile.  M is formed by
-// blocks of 16 rows, from the first on: with X = (I + L_ii beta)^-1, by substitution,
+// A tile's gates and its M.  A wave takes 16 columns of the tile; which, goes around from
+// workgroup to workgroup, as the first have the most rows below them.  M is formed by blocks of
+// 16 rows, from the first on: with X = (I + L_ii beta)^-1, by substitution (one wave's sixteen
+// lanes a block),
 //   M_ij = X (L_ij - sum_{j <= m < i} (L_im beta) M_mj)
 // in fp32 products, whose results are the next one's operands as they lie.  (Powers of L
 // beta would need fewer steps, but cancel: binomial coefficients, where keys are alike.)
 // packsT (backward): M's transpose too.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3)
 prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, const float* beta,
             const int32_t* cu, unsigned char* packs, unsigned char* packsT) {
   using C = DS<T, D, 4>;
   constexpr int kL = 68;  // floats of a row of L
-  __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes];
-  __shared__ __attribute__((aligned(16))) float ldsL[kDeltaTile][kL], ldsX[4][16][20];
+  // the keys; once multiplied, L beta and then M in their place
+  __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes > kDeltaTile * kL * 4 ? C::kTileBytes : kDeltaTile * kL * 4];
+  __shared__ __attribute__((aligned(16))) float ldsX[4][16][20];
+  float (*ldsL)[kL] = reinterpret_cast<float (*)[kL]>(ldsK);
   __shared__ __attribute__((aligned(16))) Gates G;
   __shared__ int bad;
   Span sp;
   if (!find_span<C::NT>(tiles, cu, blockIdx.x, &sp)) return;
   const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = __builtin_amdgcn_readfirstlane(((threadIdx.x >> 6) + blockIdx.x) & 3);
   const int live = sp.end - sp.begin;
   RowsLoad<T, C> lk;
   lk.load(k + (first_row(P, sp, P.heads, h / P.group) + sp.begin) * D, live);
@@ -87,81 +91,74 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
     if (lane == 63) G.whole = G.into[63], G.good = good;
     if (lane < 62) G.pad[lane] = 0.0f;
   }
-  f32x4_t x[4];
+  f32x4_t x[4];  // L's rows 16 b + 4 g + r of the wave's column n; then M's
 #pragma unroll
   for (int b = 0; b < 4; ++b) x[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int ks = 0; ks < C::KS; ++ks) {
     const auto own = row_units<T, C>(ldsK, 16 * w + n, ks, g);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) Num<T>::mma(x[b], row_units<T, C>(ldsK, 16 * b + n, ks, g), own);
+    for (int b = 0; b < 4; ++b)
+      if (b >= w) Num<T>::mma(x[b], row_units<T, C>(ldsK, 16 * b + n, ks, g), own);
   }
   __syncthreads();
   {
     const int s = 16 * w + n;
-    const float hi = G.hi[s], lo = G.lo[s];
+    const float hi = G.hi[s], lo = G.lo[s], strength = -G.beta[s];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
+      if (b < w) continue;
       const int t0 = 16 * b + 4 * g;
       const f32x4_t h4 = *reinterpret_cast<const f32x4_t*>(&G.hi[t0]), l4 = *reinterpret_cast<const f32x4_t*>(&G.lo[t0]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float y = x[b][r] * __builtin_amdgcn_exp2f((h4[r] - hi) + (l4[r] - lo));
-        ldsL[t0 + r][s] = t0 + r > s ? y : 0.0f;
+        x[b][r] = t0 + r > s ? y : 0.0f;
+        ldsL[t0 + r][s] = strength * x[b][r];
       }
     }
   }
   __syncthreads();
-  // X of the wave's diagonal block: lane n its column n, row after row.
-  {
-    float y[16], bb[16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&G.beta[16 * w + 4 * i]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) bb[4 * i + j] = z[j];
-    }
+  // X of the diagonal blocks: lane n of group g column n of block g, row after row.
+  if (w == 3) {
+    float y[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float sum = n == i ? 1.0f : 0.0f;
 #pragma unroll
       for (int s4 = 0; s4 < i; s4 += 4) {
-        const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&ldsL[16 * w + i][16 * w + s4]);
+        const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&ldsL[16 * g + i][16 * g + s4]);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (s4 + j < i) sum = fmaf(-z[j] * bb[s4 + j], y[s4 + j], sum);
+          if (s4 + j < i) sum = fmaf(z[j], y[s4 + j], sum);
       }
       y[i] = sum;
     }
-    if (g == 0) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ldsX[w][i][n] = y[i];
-    }
+    for (int i = 0; i < 16; ++i) ldsX[g][i][n] = y[i];
   }
   __syncthreads();
-  f32x4_t m[4];  // M's rows 16 i + 4 g + r of the wave's column n
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    f32x4_t acc;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] = ldsL[16 * i + 4 * g + r][16 * w + n];
+    if (i < w) continue;
 #pragma unroll
     for (int j = 0; j < i; ++j) {
+      if (j < w) continue;
       const f32x4_t a = *reinterpret_cast<const f32x4_t*>(&ldsL[16 * i + n][16 * j + 4 * g]);
-      const f32x4_t b = *reinterpret_cast<const f32x4_t*>(&G.beta[16 * j + 4 * g]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(-a[r] * b[r], m[j][r], acc, 0, 0, 0);
+      for (int r = 0; r < 4; ++r) x[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], x[j][r], x[i], 0, 0, 0);
     }
     const f32x4_t inv = *reinterpret_cast<const f32x4_t*>(&ldsX[i][n][4 * g]);
-    m[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4_t m = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) m[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(inv[r], acc[r], m[i], 0, 0, 0);
+    for (int r = 0; r < 4; ++r) m = __builtin_amdgcn_mfma_f32_16x16x4f32(inv[r], x[i][r], m, 0, 0, 0);
+    x[i] = m;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) ldsL[16 * i + 4 * g + r][16 * w + n] = -m[i][r];
+    for (int r = 0; r < 4; ++r) ldsL[16 * i + 4 * g + r][16 * w + n] = -x[i][r];
   __syncthreads();
   const size_t slot = (size_t)h * P.tiles + sp.slot;
   using Pack = Packed<T, kParts>;

@@ -108,14 +108,20 @@ __device__ __forceinline__ void split(Parts<T, N>& p, const float* x) {
   if constexpr (sizeof(T) == 4) {
     p.set(x);
   } else {
+    // (part by part: a dot product's result is used several instructions later)
+    float y[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float a = x[2 * j], b = x[2 * j + 1];
+    for (int j = 0; j < 8; ++j) y[j] = x[j];
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const uint32_t h = pack_bf16x2(a, b);
-        p.v[i][j] = h;
-        if (i + 1 < N) a = rest_lo(h, a), b = rest_hi(h, b);
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p.v[i][j] = pack_bf16x2(y[2 * j], y[2 * j + 1]);
+      if (i + 1 < N) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y[2 * j] = rest_lo(p.v[i][j], y[2 * j]);
+          y[2 * j + 1] = rest_hi(p.v[i][j], y[2 * j + 1]);
+        }
       }
     }
   }
