@@ -23,27 +23,35 @@ namespace {
 // gradients that they form.
 constexpr int kParts = 2;
 
-// bf16.  Wave w takes the tokens row_of(w, ..) of a tile as its own.  All that is computed in
-// fp32 enters as two bf16 parts: the states come so from the walks; the vectors u and dv are
+// Wave w takes the tokens row_of(w, ..) of a tile as its own.  All that is computed in fp32
+// enters (bf16) as two parts: the states come so from the walks; the vectors u and dv are
 // weighted and split once for all waves, into LDS as [value channel][token], where both the own
 // tokens' operands and the others' are transposed reads.
 //
-// Half of LDS holds them first (u | dv, each in two parts); after the pairs' products the same
-// place holds keys and queries below, and above the first 32 key channels of both states (in two
-// parts, [value channel][key channel]); the others follow by turns above and below, each loaded
-// while the one before is multiplied.
-template <int D>
-__global__ void __launch_bounds__(kThreads, 2)
-grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k, const uint16_t* dout,
-             const int32_t* cu, const unsigned char* packs, const float* S, const float* N, const float* E,
-             const float* F, uint16_t* dq, uint16_t* dk, uint16_t* dv) {
-  using T = uint16_t;
-  using C = DS<T, D, 4>;            // rows of the operands
-  using V = DS<T, kDeltaTile, 4>;   // rows of the vectors
-  using B = DS<T, 32, 4>;           // rows of 32 key channels of a state
-  constexpr int kPlane = D * V::kRow, kHalf = 2 * kPlane;
-  static_assert(kHalf == 2 * C::kTileBytes && kHalf == 4 * D * B::kRow, "the halves' uses");
-  __shared__ __attribute__((aligned(512))) unsigned char lds[2 * kHalf];
+// LDS holds them first; after the pairs' products the same place holds keys and queries below,
+// and above the first 32 key channels of both states, [value channel][key channel]; the others
+// follow by turns below and above, each loaded while the one before is multiplied.
+template <typename T, int D>
+struct GradSizes {
+  using C = DS<T, D, 4>;           // rows of the operands
+  using V = DS<T, kDeltaTile, 4>;  // rows of the vectors
+  using B = DS<T, 32, 4>;          // rows of 32 key channels of a state
+  static constexpr int kN = Parts<T, kParts>::kN;
+  static constexpr int kPlane = D * V::kPitch, kState = (sizeof(T) == 2 ? 2 : 1) * D * B::kPitch;
+  static constexpr int kUpper = 2 * C::kTileBytes > 2 * kState ? 2 * C::kTileBytes : 2 * kState;
+  static constexpr int kBytes = kUpper + 2 * kState > 2 * kN * kPlane ? kUpper + 2 * kState : 2 * kN * kPlane;
+};
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2)
+grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout, const int32_t* cu,
+             const unsigned char* packs, const float* S, const float* N, const float* E, const float* F, T* dq,
+             T* dk, T* dv) {
+  using Z = GradSizes<T, D>;
+  using C = typename Z::C;
+  using V = typename Z::V;
+  using B = typename Z::B;
+  constexpr bool kDirect = sizeof(T) == 2;
+  __shared__ __attribute__((aligned(512))) unsigned char lds[Z::kBytes];
   __shared__ __attribute__((aligned(16))) Gates G;
   unsigned char *ldsK = lds, *ldsQ = lds + C::kTileBytes;
   Span sp;
@@ -70,7 +78,13 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k,
           reinterpret_cast<const u32x4_t*>(packs + slot * Packed<T, 3>::kBlock + Packed<T, 3>::kBytes)[threadIdx.x];
     auto gradient = [&](int t, int ks) {  // of the outputs
       Parts<T, 1> o;
-      o.v[0] = __builtin_amdgcn_raw_buffer_load_b128(ro, (uint32_t)(t * C::kRow + 64 * ks + 16 * g), 0, 0);
+      const uint32_t at = (uint32_t)(t * C::kRow + (32 * ks + 8 * g) * C::ES);
+      if constexpr (sizeof(T) == 2) {
+        o.v[0] = __builtin_amdgcn_raw_buffer_load_b128(ro, at, 0, 0);
+      } else {
+        o.v[0].a = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, at, 0, 0));
+        o.v[0].b = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, at + 16, 0, 0));
+      }
       return o;
     };
     {
@@ -94,17 +108,23 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k,
         for (int i = 0; i < C::KS; ++i) {
           Parts<T, kParts> p;
           weighted<T>(p, beta, x[z][i][0], x[z][i][1]);
+          const int row = (i * kThreads + id) / 8;
+          if constexpr (sizeof(T) == 2) {
 #pragma unroll
-          for (int j = 0; j < kParts; ++j)
-            *reinterpret_cast<u32x4_t*>(lds + (2 * z + j) * kPlane +
-                                        V::unit_at((i * kThreads + id) / 8, unit)) = p.v[j];
+            for (int j = 0; j < Z::kN; ++j)
+              *reinterpret_cast<u32x4_t*>(lds + (Z::kN * z + j) * Z::kPlane + V::unit_at(row, unit)) = p.v[j];
+          } else {
+            f32x4_t* to = reinterpret_cast<f32x4_t*>(lds + z * Z::kPlane + V::unit_at(row, 2 * unit));
+            to[0] = p.v[0].a;
+            to[1] = p.v[0].b;
+          }
         }
     }
     lds_barrier();
     auto vectors = [&](int z, int b, int ks) {  // u (z = 0) or dv of the tokens row_of(b, ..)
       Parts<T, kParts> p;
 #pragma unroll
-      for (int j = 0; j < kParts; ++j) p.v[j] = key_column<T, V>(lds + (2 * z + j) * kPlane, b, ks, lane);
+      for (int j = 0; j < Z::kN; ++j) p.v[j] = key_column<T, V>(lds + (Z::kN * z + j) * Z::kPlane, b, ks, lane);
       return p;
     };
     // Pairs of an own token and others of the tile, [others][own]; the products of one order
@@ -178,26 +198,66 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k,
     if (own < live) {
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
-        u32x4_t y;
+        T* to = dv + (vrow + own) * D + 32 * ks + 8 * g;
+        if constexpr (sizeof(T) == 2) {
+          u32x4_t y;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          y[j] = pack_bf16x2(bf16_lo(v[ks].v[0][j]) + bf16_lo(v[ks].v[1][j]),
-                             bf16_hi(v[ks].v[0][j]) + bf16_hi(v[ks].v[1][j]));
-        *reinterpret_cast<u32x4_t*>(dv + (vrow + own) * D + 32 * ks + 8 * g) = y;
+          for (int j = 0; j < 4; ++j)
+            y[j] = pack_bf16x2(bf16_lo(v[ks].v[0][j]) + bf16_lo(v[ks].v[1][j]),
+                               bf16_hi(v[ks].v[0][j]) + bf16_hi(v[ks].v[1][j]));
+          *reinterpret_cast<u32x4_t*>(to) = y;
+        } else {
+          reinterpret_cast<f32x4_t*>(to)[0] = v[ks].v[0].a;
+          reinterpret_cast<f32x4_t*>(to)[1] = v[ks].v[0].b;
+        }
       }
     }
     lds_barrier();
     again();
-    auto states = [&](int cc, int to) {
-      const T* from = reinterpret_cast<const T*>(S + slot * (D * D)) + cc * (2 * D * 32);
-      rows_to_lds<T, B, 2 * D>(at_lds + to * kHalf, from, 2 * D, w, lane);
-      from = reinterpret_cast<const T*>(N + slot * (D * D)) + cc * (2 * D * 32);
-      rows_to_lds<T, B, 2 * D>(at_lds + to * kHalf + 2 * D * B::kRow, from, 2 * D, w, lane);
+    // Key channels 32 cc .. of both states, straight into LDS (fp32, whose rows there are
+    // padded: through registers), S's before N's.
+    constexpr int kPieces = D * 16 / kThreads;
+    u32x4_t piece[kDirect ? 1 : kPieces];
+    auto states = [&](int cc, int at) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const float* m = (z ? N : S) + slot * (D * D);
+        if constexpr (kDirect) {
+          rows_to_lds<T, B, 2 * D>(at_lds + at + z * Z::kState, reinterpret_cast<const T*>(m) + cc * (2 * D * 32),
+                                   2 * D, w, lane);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPieces / 2; ++i) {
+            const int p = i * kThreads + (int)threadIdx.x;
+            piece[z * (kPieces / 2) + i] = *reinterpret_cast<const u32x4_t*>(m + (p / 8) * D + 32 * cc + 4 * (p % 8));
+          }
+        }
+      }
     };
-    rows_to_lds<T, C>(at_lds, k + krow * D, live, w, lane);
-    rows_to_lds<T, C>(at_lds + C::kTileBytes, q + krow * D, live, w, lane);
-    states(0, 1);
-    wait_vm<0>();
+    auto arrive = [&](int at) {
+      if constexpr (kDirect) {
+        wait_vm<0>();
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int p = i % (kPieces / 2) * kThreads + (int)threadIdx.x;
+          *reinterpret_cast<u32x4_t*>(lds + at + i / (kPieces / 2) * Z::kState + B::unit_at(p / 8, p % 8)) = piece[i];
+        }
+      }
+    };
+    if constexpr (kDirect) {
+      rows_to_lds<T, C>(at_lds, k + krow * D, live, w, lane);
+      rows_to_lds<T, C>(at_lds + C::kTileBytes, q + krow * D, live, w, lane);
+    }
+    states(0, Z::kUpper);
+    if constexpr (!kDirect) {
+      RowsLoad<T, C> rows;
+      rows.load(k + krow * D, live);
+      rows.store(ldsK);
+      rows.load(q + krow * D, live);
+      rows.store(ldsQ);
+    }
+    arrive(Z::kUpper);
     lds_barrier();
     auto apply = [&](auto kt_, auto before_, auto after_) {
       constexpr int kt = decltype(kt_)::value;
@@ -228,11 +288,11 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k,
     const float into = G.into[own], rest = G.rest[own], scaled = P.scale * into;
 #pragma unroll
     for (int cc = 0; cc < C::KS; ++cc) {
-      if (cc + 1 < C::KS) {
-        lds_barrier();  // nobody reads the half before this one any more
-        states(cc + 1, cc & 1);
-      }
-      const unsigned char* at = lds + ((cc & 1) ^ 1) * kHalf;
+      const int here = cc & 1 ? 0 : Z::kUpper, there = cc & 1 ? Z::kUpper : 0;
+      // what is here has arrived for all waves, and nobody reads what is there any more
+      if (C::KS > 1) lds_barrier();
+      if (cc + 1 < C::KS) states(cc + 1, there);
+      const unsigned char* at = lds + here;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         f32x4_t so = {0.0f, 0.0f, 0.0f, 0.0f}, sv = so, nu = so;
@@ -240,11 +300,11 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k,
         for (int kt = 0; kt < C::KS; ++kt) {
           Parts<T, kParts> a;
 #pragma unroll
-          for (int j = 0; j < kParts; ++j) a.v[j] = key_column<T, B>(at + j * D * B::kRow, i, kt, lane);
+          for (int j = 0; j < Z::kN; ++j) a.v[j] = key_column<T, B>(at + j * D * B::kPitch, i, kt, lane);
           mma_parts<T>(so, a, o[kt]);
           mma_parts<T>(sv, a, v[kt]);
 #pragma unroll
-          for (int j = 0; j < kParts; ++j) a.v[j] = key_column<T, B>(at + (2 + j) * D * B::kRow, i, kt, lane);
+          for (int j = 0; j < Z::kN; ++j) a.v[j] = key_column<T, B>(at + Z::kState + j * D * B::kPitch, i, kt, lane);
           mma_parts<T>(nu, a, u[kt]);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -255,175 +315,25 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const uint16_t* q, const uint16_t* k,
           y[r] = fmaf(rest, nu[r], fmaf(-into, sv[r], y[r]));
         }
       }
-      if (cc + 1 < C::KS) wait_vm<0>();
+      if (cc + 1 < C::KS) arrive(there);
     }
   }
   if (own >= live) return;
 #pragma unroll
   for (int ks = 0; ks < C::KS; ++ks) {
     const int64_t at = (krow + own) * D + 32 * ks + 8 * g;
-    auto rounded = [&](const f32x4_t& a, const f32x4_t& b) {
-      return (u32x4_t){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+    auto put = [&](T* to, const f32x4_t& a, const f32x4_t& b) {
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x4_t*>(to + at) = (u32x4_t){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
+                                                         pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+      } else {
+        reinterpret_cast<f32x4_t*>(to + at)[0] = a;
+        reinterpret_cast<f32x4_t*>(to + at)[1] = b;
+      }
     };
-    *reinterpret_cast<u32x4_t*>(dq + at) = rounded(aq[2 * ks], aq[2 * ks + 1]);
-    *reinterpret_cast<u32x4_t*>(dk + at) = rounded(ak[2 * ks], ak[2 * ks + 1]);
+    put(dq, aq[2 * ks], aq[2 * ks + 1]);
+    put(dk, ak[2 * ks], ak[2 * ks + 1]);
   }
-}
-
-__device__ __forceinline__ float value_at(__amdgpu_buffer_rsrc_t r, int at) {
-  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (uint32_t)(4 * at), 0, 0));
-}
-__device__ __forceinline__ Parts<float, 1> exact(const float* x) {
-  Parts<float, 1> p;
-  p.set(x);
-  return p;
-}
-
-// fp32: the same in its order, operands gathered from memory.
-template <int D>
-__global__ void __launch_bounds__(kThreads)
-grads_kernel(DeltaPlan P, TileSpans tiles, const float* q, const float* k, const float* dout, const int32_t* cu,
-             const unsigned char* packs, const float* S, const float* N, const float* E, const float* F, float* dq,
-             float* dk, float* dv) {
-  using T = float;
-  using C = DS<T, D, 4>;
-  using Pack = Packed<T, 3>;
-  __shared__ __attribute__((aligned(16))) Gates G;
-  Span sp;
-  if (!find_span<kThreads>(tiles, cu, blockIdx.x, &sp)) return;
-  const int hk = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), own = row_of(w, n);
-  const int live = sp.end - sp.begin;
-  if (live <= 0) return;
-  const int64_t krow = first_row(P, sp, P.heads, hk) + sp.begin;
-  const uint32_t bytes = (uint32_t)(live * C::kRow);
-  const __amdgpu_buffer_rsrc_t rk = make_rsrc(k + krow * D, bytes), rq = make_rsrc(q + krow * D, bytes);
-  f32x4_t aq[C::NB], ak[C::NB];  // channels 16 c + 4 g + r of the own token
-#pragma unroll
-  for (int c = 0; c < C::NB; ++c) aq[c] = ak[c] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-  for (int gi = 0; gi < P.group; ++gi) {
-    const int h = hk * P.group + gi;
-    const size_t slot = (size_t)h * P.tiles + sp.slot;
-    const int64_t vrow = first_row(P, sp, P.value_heads, h) + sp.begin;
-    const __amdgpu_buffer_rsrc_t ro = make_rsrc(dout + vrow * D, bytes);
-    __syncthreads();
-    if (threadIdx.x < kGateBytes / 16)
-      reinterpret_cast<u32x4_t*>(&G)[threadIdx.x] = 
-          reinterpret_cast<const u32x4_t*>(packs + slot * Pack::kBlock + Pack::kBytes)[threadIdx.x];
-    __syncthreads();
-    const float *St = S + slot * (D * D), *Nt = N + slot * (D * D);
-    const float *Et = E + slot * (D * kDeltaTile), *Ft = F + slot * (D * kDeltaTile);
-    auto vectors = [&](const float* X, int t, int ks, float f, float* x) {  // f X[32 ks + 8 g + j][t]
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = f * X[(32 * ks + 8 * g + j) * kDeltaTile + t];
-    };
-    auto gradient = [&](int t, int ks, float* x) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = value_at(ro, t * D + 32 * ks + 8 * g + j);
-    };
-    Parts<T, 1> u[C::KS], v[C::KS];
-    Parts<T, 1> o[C::KS];
-    const float beta = G.beta[own];
-#pragma unroll
-    for (int ks = 0; ks < C::KS; ++ks) {
-      float x[8];
-      vectors(Et, own, ks, beta, x);
-      split(u[ks], x);
-      vectors(Ft, own, ks, beta, x);
-      split(v[ks], x);
-      if (own < live) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dv[(vrow + own) * D + 32 * ks + 8 * g + j] = x[j];
-      }
-      gradient(own, ks, x);
-      o[ks] = exact(x);
-    }
-    const float into = G.into[own], rest = G.rest[own];
-#pragma unroll
-    for (int c = 0; c < C::NB; ++c) {
-      f32x4_t so = {0.0f, 0.0f, 0.0f, 0.0f}, sv = so, nu = so;
-#pragma unroll
-      for (int ks = 0; ks < C::KS; ++ks) {
-        float x[8];
-        Parts<T, 1> a;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = St[(32 * ks + 8 * g + j) * D + 16 * c + n];
-        split(a, x);
-        mma_parts<T>(so, a, o[ks]);
-        mma_parts<T>(sv, a, v[ks]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = Nt[(32 * ks + 8 * g + j) * D + 16 * c + n];
-        split(a, x);
-        mma_parts<T>(nu, a, u[ks]);
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        aq[c][r] = fmaf(P.scale * into, so[r], aq[c][r]);
-        ak[c][r] = fmaf(rest, nu[r], fmaf(-into, sv[r], ak[c][r]));
-      }
-    }
-    // Pairs of an own token and another of the tile, [others][own].
-    const float hi = G.hi[own], lo = G.lo[own];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      float x[8], y[8], z[8];
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int b = 2 * kt + half, other = row_of(b, n);
-        f32x4_t ou = {0.0f, 0.0f, 0.0f, 0.0f}, uo = ou, vu = ou, uv = ou;
-        const float bo = G.beta[other];
-#pragma unroll
-        for (int ks = 0; ks < C::KS; ++ks) {
-          float f[8];
-          Parts<T, 1> a;
-          vectors(Et, other, ks, bo, f);
-          split(a, f);
-          mma_parts<T>(uo, a, o[ks]);
-          mma_parts<T>(uv, a, v[ks]);
-          vectors(Ft, other, ks, bo, f);
-          split(a, f);
-          mma_parts<T>(vu, a, u[ks]);
-          gradient(other, ks, f);
-          mma_parts<T>(ou, exact(f), u[ks]);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = row_of(b, 4 * g + r), j = 4 * half + r;
-          const float away = (hi - G.hi[t]) + (lo - G.lo[t]);
-          const float f = __builtin_amdgcn_exp2f(t <= own ? away : -away);
-          x[j] = t <= own ? P.scale * f * uo[r] : 0.0f;
-          y[j] = t >= own ? P.scale * f * ou[r] : 0.0f;
-          z[j] = t < own ? -f * uv[r] : t > own ? -f * vu[r] : 0.0f;
-        }
-      }
-      Parts<T, 1> xp, yp, zp;
-      split(xp, x);
-      split(yp, y);
-      split(zp, z);
-#pragma unroll
-      for (int c = 0; c < C::NB; ++c) {
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = value_at(rk, (32 * kt + 8 * g + j) * D + 16 * c + n);
-        const Parts<T, 1> kc = exact(f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = value_at(rq, (32 * kt + 8 * g + j) * D + 16 * c + n);
-        const Parts<T, 1> qc = exact(f);
-        mma_parts<T>(aq[c], kc, xp);
-        mma_parts<T>(ak[c], kc, zp);
-        mma_parts<T>(ak[c], qc, yp);
-      }
-    }
-  }
-  if (own >= live) return;
-#pragma unroll
-  for (int c = 0; c < C::NB; ++c)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t at = (krow + own) * D + 16 * c + 4 * g + r;
-      dq[at] = aq[c][r];
-      dk[at] = ak[c][r];
-    }
 }
 
 // The decays' gradient of a span: from that of its first token, <gradient of the state before
@@ -484,7 +394,7 @@ gbla_status launch_delta_grads(const DeltaPlan& p, const void* q, const void* k,
   return by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    hipLaunchKernelGGL((grads_kernel<D>), dim3(p.tiles, p.heads), dim3(kThreads), 0, st, p, tile_spans(p),
+    hipLaunchKernelGGL((grads_kernel<T, D>), dim3(p.tiles, p.heads), dim3(kThreads), 0, st, p, tile_spans(p),
                        (const T*)q, (const T*)k, (const T*)dout, cu, base + p.off_pack,
                        floats(p.off_S), floats(p.off_N), floats(p.off_E), floats(p.off_F), (T*)dq, (T*)dk, (T*)dv);
     hipLaunchKernelGGL(decay_kernel, dim3(p.grid_units, p.value_heads), dim3(kThreads), 0, st, p, cu, S0, dS0,
