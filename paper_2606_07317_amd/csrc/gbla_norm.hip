@@ -305,15 +305,17 @@ gbla_status launch_norm(const NormPlan& p, const void* x, const void* residual, 
 gbla_status launch_norm_backward(const NormPlan& p, const void* sum, const float* w,
                                  const void* dout, const void* dsum, void* ws, void* dx, float* dw,
                                  hipStream_t st) {
-  float* part = static_cast<float*>(ws);
+  const bool one = p.rows > 0 && p.blocks == 1;  // whose partial sum is all there is
+  float* part = one ? dw : static_cast<float*>(ws);
   return by_size(p, [&](auto t, auto lanes, auto pieces) {
     using T = decltype(t);
     constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
     if (p.rows > 0)
       hipLaunchKernelGGL((norm_back_kernel<T, L, N>), dim3(p.blocks), dim3(kThreads), 0, st, p, (const T*)sum, w,
                          (const T*)dout, (const T*)dsum, (T*)dx, part);
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((p.width + 63) / 64), dim3(kSumThreads), 0, st,
-                       p.rows > 0 ? p.blocks : 0, p.width, part, dw);
+    if (!one)
+      hipLaunchKernelGGL(norm_sum_kernel, dim3((p.width + 63) / 64), dim3(kSumThreads), 0, st,
+                         p.rows > 0 ? p.blocks : 0, p.width, part, dw);
   });
 }
 

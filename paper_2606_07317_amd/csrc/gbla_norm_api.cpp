@@ -44,9 +44,11 @@ gbla_status make_norm_plan(const gbla_norm_shape* s, bool backward, NormPlan* p)
   while (q.lanes * q.pieces < eights) q.pieces *= 2;
   const int32_t each = 256 / q.lanes;
   const int64_t groups = (q.rows + each - 1) / each;
-  // The backward's workgroups leave a partial sum each.
+  // The backward's workgroups leave a partial sum each.  One workgroup for up to four groups of
+  // rows writes its sum as the gradient and saves the launch that adds them (a call from Python
+  // with 4 rows of 1024: 13.9 us with it, 10.9 without).
   const int64_t most = backward ? (q.lanes == 256 ? 512 : 1024) : kMaxBlocks;
-  q.blocks = (int32_t)(groups < most ? groups : most);
+  q.blocks = (int32_t)(backward && groups <= 4 ? groups > 0 : groups < most ? groups : most);
   *p = q;
   return GBLA_OK;
 }
