@@ -284,8 +284,16 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   }
   if (threadIdx.x == 0) bad[0] = kDeltaTile;
   __syncthreads();
-  // (addresses in LDS are worked out phase by phase: held over the loop they cost registers)
-  auto again = [&] { lane = fresh(lane), n = lane & 15, g = lane >> 4; };
+  // Phases do not mix, and addresses in LDS, which cost registers held over the loop, are worked
+  // out in each: needed where four waves a SIMD share the registers, and faster where a tile is
+  // short (backward, 8 x 2048 tokens, 16 heads of 64: 92 us with it, 102 without; 58000 tokens, 8
+  // heads of 128: 430, 421; fp32, 8 x 2048 tokens, 8 heads of 64: 69, 66).
+  auto again = [&] {
+    if constexpr (kWalkWaves<T, D, Mode> > 2 || D * sizeof(T) < 256) {
+      __builtin_amdgcn_sched_barrier(0);
+      lane = fresh(lane), n = lane & 15, g = lane >> 4;
+    }
+  };
   for (int t0 = sp.begin, flip = 0; t0 < sp.end; t0 += kDeltaTile, flip ^= 1) {
     const int live = min(kDeltaTile, sp.end - t0);
     lk.store(ldsK);
@@ -336,7 +344,6 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
     again();
     // What the state predicts for the tile's keys; the values less that, y; and what of that
     // stays as the tile is read token by token, e.
@@ -372,7 +379,6 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
       }
       triangle<T, kParts, false>(y, ldsM, by, lane);
     }
-    __builtin_amdgcn_sched_barrier(0);
     again();
     if constexpr (Back) {
       float x[2][8];
@@ -462,7 +468,6 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
     again();
     Parts<T, kParts> u[2];
 #pragma unroll

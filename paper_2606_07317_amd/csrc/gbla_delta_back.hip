@@ -48,7 +48,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
   const Gates& G = *reinterpret_cast<const Gates*>(ldsM + M::kBytes);
   __shared__ float sums[All ? C::NW : 1][kDeltaTile];
   const int h = blockIdx.y;
-  int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Span sp;
   if (!find_span<C::NT>(P, cu, blockIdx.x, &sp)) return;
@@ -77,8 +77,6 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
   };
   const int last = sp.begin < sp.end ? sp.begin + (sp.end - 1 - sp.begin) / kDeltaTile * kDeltaTile : sp.begin - 1;
   if (sp.begin < sp.end) fetch(last);
-  // (addresses in LDS are worked out phase by phase: held over the loop they cost registers)
-  auto again = [&] { lane = fresh(lane), n = lane & 15, g = lane >> 4; };
   for (int t0 = last; t0 >= sp.begin; t0 -= kDeltaTile) {
     const int live = min(kDeltaTile, sp.end - t0);
     const size_t slot = slot0 + t0 / kDeltaTile;
@@ -88,7 +86,6 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
     if (All) lv.store(ldsV);
     lm.store(ldsM);
     lds_barrier();
-    again();
     // Scores [later tokens][own earlier token] as operands for all waves.
     {
       constexpr int NP = C::NW < 4 ? 4 / C::NW : 1, PG = C::NW == 8 ? 1 : 2;
@@ -118,8 +115,6 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    again();
     // The gradient of u: from the states after the tile, from the tile's outputs; f is that
     // without the tile's later ones.
     f32x4_t x[4];
@@ -142,7 +137,6 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[b][r] *= G.rest[row_of(b, 4 * g + r)];
     lds_barrier();  // the scores
-    again();
     {
       typename Num<T>::V8 o[2];
 #pragma unroll
@@ -168,8 +162,6 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
 #pragma unroll
         for (int ks = b >> 1; ks < 2; ++ks) mma_parts<T>(x[b], M::get(ldsM, upper_pair(b, ks), lane), y[ks]);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    again();
     if constexpr (All) {
       float part[2][8];
 #pragma unroll
@@ -185,9 +177,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
       const float sum = token_sums(part, lane);
       sums[w][token_of(lane)] = sum;
     }
-    __builtin_amdgcn_sched_barrier(0);
     fetch(t0 - kDeltaTile);
-    again();
     {
       Parts<T, kParts> up[2], down[2];
 #pragma unroll
