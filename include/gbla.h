@@ -499,8 +499,9 @@ size_t gbla_delta_backward_ragged_workspace_bytes(const gbla_delta_shape* shape)
  *   out              like v
  *   final_state      fp32 [N,V,d,d] or NULL (not wanted); may be initial_state.
  *                    An empty sequence's is its initial state.
- * States are sums in fp32.  In bf16 what is computed in fp32 enters the products in two
- * bf16 parts, 2^-17 of a term; fp32 products are fp32 throughout.
+ * States are sums in fp32.  In bf16 what is computed in fp32 enters the products that form
+ * states in three bf16 parts (fp32's accuracy) and those that form only the output in two,
+ * 2^-16 of a term; fp32 products are fp32 throughout.
  */
 gbla_status gbla_delta_forward(const gbla_delta_shape* shape, const void* q, const void* k,
                                const void* v, const float* log_decay, const float* beta,

