@@ -179,3 +179,15 @@ def test_delta_on_two_streams_at_once():
     for got in grads:
         for x in gw:
             assert torch.equal(got[x], gw[x]), x
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_delta_of_no_tokens(ragged):
+    """The states pass through, whatever the scratch holds."""
+    t = delta_case([0, 0], ragged, 2, 4, 32, BF16, True, (-5, -6, -7, -8))
+    args = _dev(*(t[x] for x in NAMES + ("dout",)))
+    S0, dS, cu = _dev(t["S0"], t["dS"], t["cu"])
+    out, S = gbla.delta_attention(*args[:5], initial_state=S0, final_state=True, cu_seqlens=cu)
+    assert out.shape == args[2].shape and torch.equal(S, S0)
+    got = gbla.delta_attention_backward(*args, initial_state=S0, dfinal_state=dS, cu_seqlens=cu)
+    assert torch.equal(got["dinitial_state"], dS) and got["dq"].shape == args[0].shape
