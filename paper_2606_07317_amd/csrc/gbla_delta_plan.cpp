@@ -25,13 +25,16 @@ int32_t unit_tokens(const DeltaPlan& p) {
   return unit;
 }
 
-// Whether a workgroup walks a whole sequence: all are short, or there are walks enough of the
-// longest's length.  Measured (bf16, heads of 64; split, whole, in us): 1 x 256 tokens, 8 heads
-// 30, 27; 8 x 512 41, 45; 16 x 1024 92, 88; 16 x 4096 296, 315; 32 x 4096 583, 386; backward,
-// where a split sequence takes two launches more: 1 x 256 62, 70; 16 x 512 164, 148; 16 x 1024
-// 288, 278; 8 x 2048, 16 heads 460, 545; 16 x 2048, 16 heads 874, 695.
+// Whether a workgroup walks a whole sequence: all are of a few tiles, or there are walks enough
+// of the longest's length.  Measured (split, whole, in us; 8 heads of 64 in bf16 where nothing
+// else is said): 1 x 192 tokens 28, 23; 1 x 256 28, 27; 1 x 320 27, 30; 1 x 128 in fp32 28, 23
+// (heads of 32); 1 x 192 in fp32 31, 34; 8 x 512 41, 45; 16 x 1024 92, 88; 16 x 4096 296, 315;
+// 32 x 4096 583, 386; backward, where a split sequence takes two launches more: 1 x 192 64, 57;
+// 1 x 256 62, 70; 16 x 512 164, 148; 16 x 1024 288, 278; 8 x 2048, 16 heads 460, 545; 16 x 2048,
+// 16 heads 874, 695.
 bool walk_whole(const DeltaPlan& p, int64_t longest, bool backward) {
-  return longest <= (backward ? 128 : 256) || longest * (longest <= 1024 ? 128 : 256) <= p.tokens * p.value_heads;
+  const int few = p.dtype == GBLA_F32 ? 2 : backward ? 3 : 4;
+  return longest <= few * kDeltaTile || longest * (longest <= 1024 ? 128 : 256) <= p.tokens * p.value_heads;
 }
 
 }  // namespace
