@@ -146,11 +146,19 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
       f32x4_t ou[2], uo[2], vu[2], uv[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) ou[i] = uo[i] = vu[i] = uv[i] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+      // (the next step's rows from memory are under way while this one's are multiplied)
+      Parts<T, 1> o, others[2], next, next_others[2];
+      auto ahead = [&](int ks) {
+        if constexpr (Before) next = gradient(own, ks);
+        if constexpr (After) next_others[0] = gradient(row_of(2 * kt, n), ks), next_others[1] = gradient(row_of(2 * kt + 1, n), ks);
+      };
+      ahead(0);
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
+        o = next, others[0] = next_others[0], others[1] = next_others[1];
+        if (ks + 1 < C::KS) ahead(ks + 1);
         Parts<T, kParts> u, v;
-        Parts<T, 1> o;
-        if constexpr (Before) o = gradient(own, ks), v = vectors(1, w, ks);
+        if constexpr (Before) v = vectors(1, w, ks);
         if constexpr (After) u = vectors(0, w, ks);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -162,7 +170,7 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
           }
           if constexpr (After) {
             mma_parts<T>(vu[i], vectors(1, b, ks), u);
-            mma_parts<T>(ou[i], gradient(row_of(b, n), ks), u);
+            mma_parts<T>(ou[i], others[i], u);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
