@@ -275,10 +275,17 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   BlockLoad<C, M::kBytes> lm;
   BlockLoad<C, kGateBytes> lg;
   const uint32_t atV = lds_address(ldsV), atM = lds_address(ldsM);
+  // Outputs at four waves a SIMD hold too much to have keys and queries under way from a tile's
+  // start (spilled registers: 833 us for 178000 packed tokens, 8 heads of 128; from the outputs
+  // on 779.  Heads of 64 the other way round: 58 and 59).
+  constexpr bool kLate = Mode == kOutputs && kWalkWaves<T, D, Mode> > 2 && D == 128;
+  auto rows = [&](int t) {
+    lk.load(k + (krow + t) * D, sp.end - t);
+    if (Out) lq.load(q + (krow + t) * D, sp.end - t);
+  };
   auto fetch = [&](int t) {
     const int left = sp.end - t;
-    lk.load(k + (krow + t) * D, left);
-    if (Out) lq.load(q + (krow + t) * D, left);
+    if (!kLate) rows(t);
     lg.load(packs + (slot0 + t / kDeltaTile) * M::kBlock + M::kBytes, left > 0);
   };
   auto fetch_direct = [&](int t) {
@@ -296,6 +303,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   if (sp.begin < sp.end) {
     fetch(sp.begin);
     fetch_direct(sp.begin);
+    if (kLate) rows(sp.begin);
   }
   if (threadIdx.x == 0) bad[0] = kDeltaTile;
   __syncthreads();
@@ -413,6 +421,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     lds_barrier();  // the scores are there; nobody reads the values and the triangle any more
     const int good = min(min(bad[flip], G.good), live);
     if (t0 + kDeltaTile < sp.end) fetch_direct(t0 + kDeltaTile);
+    if (kLate) rows(t0 + kDeltaTile);
     if constexpr (Out) {
       again();
       f32x4_t o[4];
