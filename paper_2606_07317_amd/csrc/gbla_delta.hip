@@ -206,9 +206,9 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
 // its registers; only the scores, which all waves need, go through LDS.  The matrix unit, vector
 // instructions (the splits into parts) and reads of operands from LDS take 0.4 to 0.5 of the
 // cycles each, and dependent steps between barriers the rest: 0.38 and 0.48 of the matrix unit
-// at 178000 packed tokens, 8 heads of 128 (outputs 811 us, records 706), 0.28 and 0.37 at 32768
-// tokens, 8 heads of 64 (57 and 55 us).  Without any loads of a later tile the same walks take
-// 715 and 681.  Two column blocks a wave, which halve the reads of LDS, took as long (half the
+// at 178000 packed tokens, 8 heads of 128 (outputs 811 us, 0.1 ms less since, and records 706),
+// 0.28 and 0.37 at 32768 tokens, 8 heads of 64 (57 and 55 us).  Without any loads of a later tile
+// the records take 681.  Two column blocks a wave, which halve the reads of LDS, took as long (half the
 // waves); scores in the place of the values, for a third workgroup at heads of 64, as well.
 enum WalkMode { kOutputs, kRecords, kBack };
 template <typename T, int D>
@@ -275,18 +275,14 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   BlockLoad<C, M::kBytes> lm;
   BlockLoad<C, kGateBytes> lg;
   const uint32_t atV = lds_address(ldsV), atM = lds_address(ldsM);
-  // Outputs at four waves a SIMD hold too much to have keys and queries under way from a tile's
-  // start (spilled registers: 833 us for 178000 packed tokens, 8 heads of 128; from the outputs
-  // on 779.  Heads of 64 the other way round: 58 and 59).
+  // Outputs at four waves a SIMD hold too much to have keys, queries and gates under way from a
+  // tile's start (spilled registers: 833 us for 178000 packed tokens, 8 heads of 128; from before
+  // the outputs on 779, behind them 729.  Heads of 64 the other way round: 58 and 59).
   constexpr bool kLate = Mode == kOutputs && kWalkWaves<T, D, Mode> > 2 && D == 128;
-  auto rows = [&](int t) {
+  auto fetch = [&](int t) {
     lk.load(k + (krow + t) * D, sp.end - t);
     if (Out) lq.load(q + (krow + t) * D, sp.end - t);
-  };
-  auto fetch = [&](int t) {
-    const int left = sp.end - t;
-    if (!kLate) rows(t);
-    lg.load(packs + (slot0 + t / kDeltaTile) * M::kBlock + M::kBytes, left > 0);
+    lg.load(packs + (slot0 + t / kDeltaTile) * M::kBlock + M::kBytes, sp.end - t > 0);
   };
   auto fetch_direct = [&](int t) {
     const int left = sp.end - t;
@@ -303,7 +299,6 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   if (sp.begin < sp.end) {
     fetch(sp.begin);
     fetch_direct(sp.begin);
-    if (kLate) rows(sp.begin);
   }
   if (threadIdx.x == 0) bad[0] = kDeltaTile;
   __syncthreads();
@@ -329,7 +324,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
       lm.store(ldsM);
     }
     lds_barrier();
-    fetch(t0 + kDeltaTile);
+    if (!kLate) fetch(t0 + kDeltaTile);
     if (threadIdx.x == 0) bad[flip ^ 1] = kDeltaTile;
     if (G.good < live) {
       clear_rows<C>(ldsK, G.good);
@@ -421,7 +416,6 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     lds_barrier();  // the scores are there; nobody reads the values and the triangle any more
     const int good = min(min(bad[flip], G.good), live);
     if (t0 + kDeltaTile < sp.end) fetch_direct(t0 + kDeltaTile);
-    if (kLate) rows(t0 + kDeltaTile);
     if constexpr (Out) {
       again();
       f32x4_t o[4];
@@ -493,6 +487,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
       }
     }
     again();
+    if (kLate) fetch(t0 + kDeltaTile);
     Parts<T, kParts> u[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
