@@ -204,10 +204,10 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
 //
 // A wave holds 16 value channels of the state, so that a tile's products follow one another in
 // its registers; only the scores, which all waves need, go through LDS.  The matrix unit, vector
-// instructions (the splits into parts) and reads of operands from LDS take 0.4 to 0.5 of the
-// cycles each, and dependent steps between barriers the rest: 0.38 and 0.48 of the matrix unit
-// at 178000 packed tokens, 8 heads of 128 (outputs 811 us, 0.1 ms less since, and records 706),
-// 0.28 and 0.37 at 32768 tokens, 8 heads of 64 (57 and 55 us).  Without any loads of a later tile
+// instructions (the splits into parts) and reads of operands from LDS take 0.4 to 0.6 of the
+// cycles each, and dependent steps between barriers the rest: 0.46 and 0.48 of the matrix unit
+// at 178000 packed tokens, 8 heads of 128 (outputs 695 us, records 719), 0.28 and 0.37 at 32768
+// tokens, 8 heads of 64 (57 us each).  Without any loads of a later tile
 // the records take 681.  Two column blocks a wave, which halve the reads of LDS, took as long (half the
 // waves); scores in the place of the values, for a third workgroup at heads of 64, as well.
 enum WalkMode { kOutputs, kRecords, kBack };
