@@ -71,7 +71,8 @@ gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void
                                    float* dS0, hipStream_t st);
 gbla_status launch_delta_grads(const DeltaPlan& p, const void* q, const void* k, const float* S0,
                                const int32_t* cu, const void* dout, void* ws, void* dq, void* dk,
-                               void* dv, float* dlog_decay, const float* dS0, hipStream_t st);
+                               void* dv, float* dlog_decay, const float* dS0, bool final_gradient,
+                               hipStream_t st);
 gbla_status launch_delta_step(const gbla_delta_shape& s, const void* q, const void* k,
                               const void* v, const float* log_decay, const float* beta,
                               const int32_t* indices, int32_t slots, float* state, void* out,

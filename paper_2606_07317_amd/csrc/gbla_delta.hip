@@ -702,7 +702,8 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
     launch_walk<T, D, kBack>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
   });
   if (done != GBLA_OK) return done;
-  return launch_delta_grads(p, q, k, S0, cu, dout, ws, dq, dk, dv, dlog_decay, dS0, st);
+  return launch_delta_grads(p, q, k, S0, cu, dout, ws, dq, dk, dv, dlog_decay, dS0,
+                            dfinal != nullptr, st);
 }
 
 }  // namespace gbla
