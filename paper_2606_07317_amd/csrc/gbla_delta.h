@@ -45,10 +45,21 @@ struct DeltaPlan {
   size_t off_N;      // ... the gradient of the state after each tile
   size_t off_E;      // [V, tiles, d, 64] fp32: the tiles' e, [value channel][token]
   size_t off_F;      // ... the gradient of u
-  size_t off_do_o;   // fp32, like the gates: do o of each token
-  size_t off_dv_v;   // ... dv v
+  size_t off_X;      // ... its part from the state after the tile
+  size_t off_from;   // fp32, like the gates: what of the decays' gradient ends at each token and
+                     // comes from the state before its tile
+  size_t off_on;     // ... begins at each token and goes on to the state after its tile
+  size_t off_sums;   // [V, tiles] DeltaTileSums
   size_t off_dS0;    // [N, V, d, d] fp32: dinitial_state where the caller wants none
   size_t total_bytes;
+};
+
+// What a tile has of its decays' gradient (gbla_delta_grads.hip).
+struct DeltaTileSums {
+  double from, on;  // sums of off_from's and off_on's tokens
+  double over;      // what passes over the whole tile
+  float steps;      // tiles from where the sum that `over` comes of is known
+  int32_t direct;   // `over` was formed of the states themselves
 };
 
 gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backward, DeltaPlan* p);
@@ -66,9 +77,9 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
 // walk; and its last launches (gbla_delta_grads.hip): the gradients of q, k, v and log_decay.
 gbla_status launch_delta_back_records(const DeltaPlan& p, const void* q, const void* k, const int32_t* cu,
                                       const void* dout, void* ws, hipStream_t st);
-gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void* k, const void* v,
-                                   const int32_t* cu, const void* dout, const float* dfinal, void* ws,
-                                   float* dS0, hipStream_t st);
+gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void* k, const int32_t* cu,
+                                   const void* dout, const float* dfinal, void* ws, float* dS0,
+                                   hipStream_t st);
 gbla_status launch_delta_grads(const DeltaPlan& p, const void* q, const void* k, const float* S0,
                                const int32_t* cu, const void* dout, void* ws, void* dq, void* dk,
                                void* dv, float* dlog_decay, const float* dS0, bool final_gradient,

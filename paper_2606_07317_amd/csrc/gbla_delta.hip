@@ -200,7 +200,9 @@ prep_kernel(DeltaPlan P, TileSpans tiles, const T* k, const float* log_decay, co
 
 // What walk_kernel makes: outputs; a unit's records, which are what the unit adds to the state
 // (from zeros) and what it does to the state before it (from the identity, without values);
-// or what the backward needs of the forward, and the strengths' gradient.
+// or what the backward needs of the forward, the strengths' gradient, and what of the decays' ends
+// at each token from the state before its tile, or begins there for the state after it
+// (gbla_delta_grads.hip).  The last forms no scores.
 //
 // A wave holds 16 value channels of the state, so that a tile's products follow one another in
 // its registers; only the scores, which all waves need, go through LDS.  The matrix unit, vector
@@ -218,8 +220,8 @@ template <typename T, int D, WalkMode Mode>
 constexpr int kWalkWaves = sizeof(T) == 4 || D == 32 || Mode == kBack ? 2 : 4;
 struct BackOut {
   const void* dout;
-  const float* F;     // the gradient of u
-  float *S, *E, *do_o, *dbeta;
+  const float *F, *X;  // the gradient of u, and its part from the state after the tile
+  float *S, *E, *from, *on, *dbeta;
   float* M;           // the maps for the gradients' scan
   bool final_gradient;  // the final state has one
 };
@@ -234,13 +236,13 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   constexpr int kOut = Mode == kBack ? 3 : kOutParts;
   using M = Packed<T, kParts>;
   using Pk = Packed<T, kOut>;
-  constexpr bool Out = Mode != kRecords, Back = Mode == kBack;
+  constexpr bool Out = Mode != kRecords, Back = Mode == kBack, Scores = Mode == kOutputs;
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes], ldsV[C::kTileBytes],
       ldsQ[Out ? C::kTileBytes : 16];
-  __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBytes], ldsP[Out ? Pk::kBytes : 16];
+  __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBytes], ldsP[Scores ? Pk::kBytes : 16];
   __shared__ __attribute__((aligned(16))) Gates G;
   __shared__ int bad[2];  // of this tile and the next
-  __shared__ float sums[2][Back ? C::NW : 1][kDeltaTile];
+  __shared__ float sums[Back ? 4 : 1][Back ? C::NW : 1][kDeltaTile];
   const int h = blockIdx.y;
   int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -334,7 +336,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     again();
     // Scores [own token][earlier tokens] as operands for all waves: a wave forms NP blocks of 16
     // own tokens with PG groups of 32 earlier ones.
-    if constexpr (Out) {
+    if constexpr (Scores) {
       constexpr int NP = C::NW < 4 ? 4 / C::NW : 1, PG = C::NW == 8 ? 1 : 2;
       const int pg0 = C::NW == 8 ? w >> 2 : 0;
 #pragma unroll
@@ -380,6 +382,15 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
 #pragma unroll
         for (int b = 0; b < 4; ++b) Num<T>::mma(y[b], kk[b], s.v[i]);
     }
+    // (Back: what the walk needs of the gradient of u, at the wave's tokens 32 ks + 8 g + j)
+    auto vector = [&](const float* m, int ks, float* x) {
+      eight(m + (slot * D + e0 + n) * kDeltaTile + 32 * ks + 8 * g, x);
+    };
+    float part[2][8], f[2][8];
+    auto add_up = [&](int i) {
+      const float sum = token_sums(part, lane);
+      sums[i][w][token_of(lane)] = sum;
+    };
     {
       Parts<T, kParts> by[2];
 #pragma unroll
@@ -391,27 +402,37 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
         auto v8 = value_column<T, C>(ldsV, w, ks, lane);
         drop_bad<T>(v8, 32 * ks + 8 * g, &bad[flip]);
         Num<T>::widen(v8, x);
+        if constexpr (Back) {  // dv times what the state before the tile predicts
+          vector(back.F, ks, f[ks]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) part[ks][j] = beta[j] * f[ks][j] * (-into[j] * y[2 * ks + (j >> 2)][j & 3]);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[2 * ks + (j >> 2)][j & 3] = fmaf(-into[j], y[2 * ks + (j >> 2)][j & 3], x[j]);
         weighted<T>(by[ks], beta, y[2 * ks], y[2 * ks + 1]);
       }
       triangle<T, kParts, false>(y, ldsM, by, lane);
+      if constexpr (Back) add_up(0);
     }
     again();
     if constexpr (Back) {
-      float x[2][8];
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        float* at = back.E + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g);
-        *reinterpret_cast<f32x4_t*>(at) = y[b];
-        const f32x4_t f = *reinterpret_cast<const f32x4_t*>(back.F + (at - back.E));
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<f32x4_t*>(back.E + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g)) = y[b];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[b >> 1][4 * (b & 1) + r] = y[b][r] * f[r];
-        }
+      for (int ks = 0; ks < 2; ++ks) {
+        float x[8], beta[8];
+        vector(back.X, ks, x);
+        eight(&G.beta[32 * ks + 8 * g], beta);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[ks][j] = x[j] * (beta[j] * y[2 * ks + (j >> 2)][j & 3]);
       }
-      const float sum = token_sums(x, lane);
-      sums[0][w][token_of(lane)] = sum;
+      add_up(1);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[ks][j] = f[ks][j] * y[2 * ks + (j >> 2)][j & 3];
+      add_up(2);
     }
     lds_barrier();  // the scores are there; nobody reads the values and the triangle any more
     const int good = min(min(bad[flip], G.good), live);
@@ -438,7 +459,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[b][r] *= f;
       }
-      {
+      if constexpr (Scores) {
         Parts<T, kOut> u[2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
@@ -466,7 +487,7 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
           }
           x += __shfl_xor(x, 16);
           x += __shfl_xor(x, 32);
-          sums[1][w][row_of(b, n)] = x;
+          sums[3][w][row_of(b, n)] = x;
         }
       } else {
         const __amdgpu_buffer_rsrc_t ro = make_rsrc(out + (vrow + t0) * D, (uint32_t)(live * C::kRow));
@@ -511,14 +532,17 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     if (good < live) S.fill(__builtin_nanf(""));
     lds_barrier();
     if constexpr (Back) {
-      // (the next tile's are written behind two more barriers)
+      // (the next tile's are written behind one more barrier)
       if ((int)threadIdx.x < live) {
         const int64_t at = gate_row(P, sp, h) + t0 + threadIdx.x;
-        float a = 0.0f, b = 0.0f;
+        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < C::NW; ++i) a += sums[0][i][threadIdx.x], b += sums[1][i][threadIdx.x];
-        back.dbeta[at] = a;
-        back.do_o[at] = b;
+        for (int i = 0; i < C::NW; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] += sums[j][i][threadIdx.x];
+        back.from[at] = x[0] + x[3];
+        back.on[at] = x[1];
+        back.dbeta[at] = x[2];
       }
     }
   }
@@ -675,11 +699,11 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
   // (the decays' gradient takes it too)
   if (!dS0 && S0) dS0 = floats(p.off_dS0);
+  const BackOut back = {dout, floats(p.off_F), floats(p.off_X), floats(p.off_S), floats(p.off_E), floats(p.off_from),
+                        floats(p.off_on), dbeta, floats(p.off_MT), dfinal != nullptr};
   gbla_status done = by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    const BackOut back = {dout,         floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_do_o),
-                          dbeta,        floats(p.off_MT), dfinal != nullptr};
     launch_prep<T, D>(p, k, log_decay, beta, cu, base, true, st);
     if (!p.single) {
       launch_walk<T, D, kRecords>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
@@ -692,13 +716,11 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
     constexpr int D = decltype(dim)::value;
     if (!p.single) launch_scan<D, true>(p, cu, dfinal, base, st);
   });
-  if (done == GBLA_OK) done = launch_delta_back_walk(p, q, k, v, cu, dout, dfinal, ws, dS0, st);
+  if (done == GBLA_OK) done = launch_delta_back_walk(p, q, k, cu, dout, dfinal, ws, dS0, st);
   if (done != GBLA_OK) return done;
   done = by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
-    const BackOut back = {dout,         floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_do_o),
-                          dbeta,        floats(p.off_MT), dfinal != nullptr};
     launch_walk<T, D, kBack>(p, q, k, v, S0, cu, base, nullptr, nullptr, back, st);
   });
   if (done != GBLA_OK) return done;

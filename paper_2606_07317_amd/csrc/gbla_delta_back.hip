@@ -4,7 +4,7 @@
 // With N the gradient of the state after a tile, and P, M, c as in the forward
 // (gbla_delta.hip; P the tile's scaled and decayed scores):
 //   du = P^T do + e^(c_L - c) K N
-//   f  = du - M^T (beta du),    dv = beta f,    dbeta = f e   (e from the forward's tiles)
+//   f  = du - M^T (beta du),    dv = beta f
 //   N_in = e^c_L N + scale (e^c Q)^T do - (e^c K)^T dv
 // which needs nothing of the forward's states.  As there, a wave owns 16 value channels and
 // all that one product hands to the next stays in its registers; units run at the same time,
@@ -36,22 +36,21 @@ constexpr int kBackWaves = 2;
 struct BackArrays {
   const unsigned char* packs;  // M's transposes and the gates
   float* recD;                 // the gradient of the state after each unit; what it adds (Records)
-  float *N, *F, *dv_v;
+  float *N, *F, *X;
 };
 
 // Records: what the unit's own tokens add to the gradient of the state before it, into recD.
 template <typename T, int D, bool Records>
 __global__ void __launch_bounds__((BackSizes<T, D>::NT), (kBackWaves<T, D, Records>))
-back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, const int32_t* cu, const float* dfinal,
+back_kernel(DeltaPlan P, const T* q, const T* k, const T* dout, const int32_t* cu, const float* dfinal,
             BackArrays a, float* dS0) {
   using C = BackSizes<T, D>;
   using M = Packed<T, kParts>;
   constexpr bool All = !Records;
   __shared__ __attribute__((aligned(512))) unsigned char ldsK[C::kTileBytes], ldsQ[C::kTileBytes],
-      ldsO[C::kTileBytes], ldsV[All ? C::kTileBytes : 16];
+      ldsO[C::kTileBytes];
   __shared__ __attribute__((aligned(16))) unsigned char ldsM[M::kBlock], ldsP[M::kBytes];
   const Gates& G = *reinterpret_cast<const Gates*>(ldsM + M::kBytes);
-  __shared__ float sums[All ? C::NW : 1][kDeltaTile];
   const int h = blockIdx.y;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -69,7 +68,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
 
   const int64_t krow = first_row(P, sp, P.heads, h / P.group), vrow = first_row(P, sp, P.value_heads, h);
   const size_t slot0 = (size_t)h * P.tiles + tile_slot(P, sp.row0, sp.s);
-  RowsLoad<T, C> lk, lq, lo, lv;
+  RowsLoad<T, C> lk, lq, lo;
   BlockLoad<C, M::kBlock> lm;
   auto fetch = [&](int t) {  // (none before the unit's first tile)
     const int left = t < sp.begin ? 0 : sp.end - t;
@@ -77,18 +76,15 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
     lk.load(k + (krow + row) * D, left);
     lq.load(q + (krow + row) * D, left);
     lo.load(dout + (vrow + row) * D, left);
-    if (All) lv.load(v + (vrow + row) * D, left);
     lm.load(a.packs + (slot0 + row / kDeltaTile) * M::kBlock, left > 0);
   };
   const int last = sp.begin < sp.end ? sp.begin + (sp.end - 1 - sp.begin) / kDeltaTile * kDeltaTile : sp.begin - 1;
   if (sp.begin < sp.end) fetch(last);
   for (int t0 = last; t0 >= sp.begin; t0 -= kDeltaTile) {
-    const int live = min(kDeltaTile, sp.end - t0);
     const size_t slot = slot0 + t0 / kDeltaTile;
     lk.store(ldsK);
     lq.store(ldsQ);
     lo.store(ldsO);
-    if (All) lv.store(ldsV);
     lm.store(ldsM);
     lds_barrier();
     // Scores [later tokens][own earlier token] as operands for all waves.
@@ -141,6 +137,12 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
     for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[b][r] *= G.rest[row_of(b, 4 * g + r)];
+    auto put = [&](float* m) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<f32x4_t*>(m + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g)) = x[b];
+    };
+    if constexpr (All) put(a.X);
     lds_barrier();  // the scores
     {
       typename Num<T>::V8 o[2];
@@ -167,21 +169,7 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
 #pragma unroll
         for (int ks = b >> 1; ks < 2; ++ks) mma_parts<T>(x[b], M::get(ldsM, upper_pair(b, ks), lane), y[ks]);
     }
-    if constexpr (All) {
-      float part[2][8];
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        float z[8];
-        Num<T>::widen(value_column<T, C>(ldsV, w, ks, lane), z);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) part[ks][j] = G.beta[32 * ks + 8 * g + j] * x[2 * ks + (j >> 2)][j & 3] * z[j];
-      }
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-        *reinterpret_cast<f32x4_t*>(a.F + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g)) = x[b];
-      const float sum = token_sums(part, lane);
-      sums[w][token_of(lane)] = sum;
-    }
+    if constexpr (All) put(a.F);
     fetch(t0 - kDeltaTile);
     {
       Parts<T, kParts> up[2], down[2];
@@ -217,15 +205,6 @@ back_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const T* dout, cons
       }
     }
     lds_barrier();
-    if constexpr (All) {
-      // (the next tile's are written behind two more barriers)
-      if ((int)threadIdx.x < live) {
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < C::NW; ++i) sum += sums[i][threadIdx.x];
-        a.dv_v[gate_row(P, sp, h) + t0 + threadIdx.x] = sum;
-      }
-    }
   }
   if (Records) N.store_record(a.recD + record, e0, lane);
   else if (dS0 && sp.idx == 0) N.store(dS0 + pair * (D * D), e0, lane);
@@ -235,7 +214,7 @@ BackArrays arrays(const DeltaPlan& p, void* ws) {
   unsigned char* base = static_cast<unsigned char*>(ws);
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
   return {base + p.off_packT, floats(p.off_D), floats(p.off_N),
-          floats(p.off_F), floats(p.off_dv_v)};
+          floats(p.off_F), floats(p.off_X)};
 }
 
 }  // namespace
@@ -247,19 +226,19 @@ gbla_status launch_delta_back_records(const DeltaPlan& p, const void* q, const v
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
     hipLaunchKernelGGL((back_kernel<T, D, true>), dim3(p.grid_units, p.value_heads), dim3((BackSizes<T, D>::NT)), 0,
-                       st, p, (const T*)q, (const T*)k, (const T*)nullptr, (const T*)dout, cu, (const float*)nullptr,
+                       st, p, (const T*)q, (const T*)k, (const T*)dout, cu, (const float*)nullptr,
                        arrays(p, ws), (float*)nullptr);
   });
 }
 
-gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void* k, const void* v,
-                                   const int32_t* cu, const void* dout, const float* dfinal, void* ws,
-                                   float* dS0, hipStream_t st) {
+gbla_status launch_delta_back_walk(const DeltaPlan& p, const void* q, const void* k, const int32_t* cu,
+                                   const void* dout, const float* dfinal, void* ws, float* dS0,
+                                   hipStream_t st) {
   return by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;
     hipLaunchKernelGGL((back_kernel<T, D, false>), dim3(p.grid_units, p.value_heads), dim3((BackSizes<T, D>::NT)), 0,
-                       st, p, (const T*)q, (const T*)k, (const T*)v, (const T*)dout, cu, dfinal, arrays(p, ws), dS0);
+                       st, p, (const T*)q, (const T*)k, (const T*)dout, cu, dfinal, arrays(p, ws), dS0);
   });
 }
 

@@ -8,9 +8,7 @@
 //          - sum_{s < t} D_ts (dv_t u_s) k_s - sum_{r > t} D_rt (dv_r u_t) k_r
 // summed over the value heads that share the query and key head.
 //
-// The decay's gradient <dZ_t, Z_t> (Z_t = e^g_t S_{t-1}, dZ_t its gradient) goes on from token
-// to token: dg_{t+1} = dg_t + dv_t v_t - do_t o_t.  It is anchored where both states are at
-// hand, at the start of every unit, and summed from there in 64 bits.
+// and of log_decay, by tiles (pairs_kernel) and joined over them (decay_kernel).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -349,18 +347,248 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
   }
 }
 
-// The decays' gradient of a span: from that of its first token, <gradient of the state before
-// the span, that state>, on, to what it comes to behind the last, where the next span has it or
-// nothing has a gradient any more.  What the sum misses that end by is the roundings of its
-// terms; spread over the tokens it leaves 0.6 of their error (8 packed sequences of up to 12000
-// tokens, heads of 32 in fp32: 1.4e-6 of the norm without).
+// The decays' gradient, dg_t = <dZ_t, Z_t>, as the sum of the terms that pass token t's decay and
+// of no others, so that it is as accurate where the decay is strong as where it is not:
+//   sum_{s < t <= r} A_rs + sum_{r >= t} B_r + sum_{s < t} C_s + W
+//   A_rs = D_rs (scale (q_r k_s) (do_r u_s) - (k_r k_s) (dv_r u_s))          within the tile
+//   B_r  = e^c_r (scale do_r S^T q_r - dv_r S^T k_r)     from the state before it (the walk's)
+//   C_s  = e^(c_L - c_s) k_s^T N u_s                      to the state after it (the walk's)
+//   W    = e^c_L <S, N>                                   over all of it
+// (The difference of neighbours, dv_t v_t - do_t o_t, holds the token's own pair, which no decay
+// makes smaller: summed over the tokens its roundings were 3e-4 of the gradient at decays of
+// e^-8, and all of it at e^-30.)
+//
+// W comes of <S, N> at the ends of a span of tiles (decay_kernel), off by 2^-24 of the gradients
+// about it.  That is little beside what a token of the tile has of its neighbours, which is of the
+// size of its own decay, unless that is below 2^-8: then the tile's W is the product of the states
+// as the walks left them (bf16: in two parts, 2^-17 of it each).  Without such a token a W below
+// 2^-64 is taken as nothing.  (The states of every tile would be 128 KB more to read at heads of
+// 128: 58000 packed tokens, 8 heads, 2425 us a backward; 2547 with a forgetting token among 50.)
+//
+// Bound by HBM and the wait for it: 56 KB a tile at heads of 64, 8 x 2048 tokens, 16 heads: 70 us
+// (3.3 TB/s); 112 KB at heads of 128, 58000 packed tokens, 8 heads: 215 us (3.8).  E and F both in
+// LDS: 78 and 282; neither, with branches between the blocks: 88 and 281; as a phase of the
+// gradients' kernel, which has both: 72 and 370 more.
+constexpr float kDirectStep = -8.0f;  // log2
+constexpr float kNothing = 0x1p-64f;
+
+// Thread's share of <S, N> of two states as store_columns leaves them.
+template <typename T, int D>
+__device__ __forceinline__ float states_product(const float* S, const float* N) {
+  const u32x4_t *s = reinterpret_cast<const u32x4_t*>(S), *n = reinterpret_cast<const u32x4_t*>(N);
+  float sum = 0.0f;
+  if constexpr (sizeof(T) == 2) {
+    for (int i = threadIdx.x; i < D * D / 8; i += kThreads) {
+      const int at = i / (4 * D) * (8 * D) + i % (4 * D);  // of the first parts; 4 D on, the second
+      const u32x4_t a = s[at], b = s[at + 4 * D], c = n[at], d = n[at + 4 * D];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sum = fmaf(bf16_lo(a[j]) + bf16_lo(b[j]), bf16_lo(c[j]) + bf16_lo(d[j]), sum);
+        sum = fmaf(bf16_hi(a[j]) + bf16_hi(b[j]), bf16_hi(c[j]) + bf16_hi(d[j]), sum);
+      }
+    }
+  } else {
+    for (int i = threadIdx.x; i < D * D / 4; i += kThreads) {
+      const u32x4_t a = s[i], c = n[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum = fmaf(__uint_as_float(a[j]), __uint_as_float(c[j]), sum);
+    }
+  }
+  return sum;
+}
+
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// A tile of a value head: what its tokens have but W.  Wave w has the later tokens 16 w .. (which
+// wave that is goes around, as in prep_kernel) and sums over the earlier ones in its registers.  E,
+// which all waves need, goes straight into LDS in fp32, [value channel][token] (16-byte units of a
+// row at u ^ (row / 8 % 4 * 4): the four rows that a wave reads at once lie in different banks);
+// E and F enter the products in three parts (bf16).
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 3)
+pairs_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout, const int32_t* cu,
+             const unsigned char* packs, const float* S, const float* N, const float* E, const float* F,
+             const float* from, const float* on, DeltaTileSums* sums, float* dg) {
+  using C = DS<T, D, 4>;
+  __shared__ __attribute__((aligned(512))) float lds[D][kDeltaTile];
+  __shared__ __attribute__((aligned(16))) float gates[3][kDeltaTile];
+  __shared__ float passing[4][kDeltaTile];
+  __shared__ double product[4];
+  Span sp;
+  if (!find_span<kThreads>(tiles, cu, blockIdx.x, &sp)) return;
+  const int live = sp.end - sp.begin;
+  if (live <= 0) return;
+  const int h = blockIdx.y, lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(((threadIdx.x >> 6) + blockIdx.x) & 3);
+  const size_t slot = (size_t)h * P.tiles + sp.slot;
+  const Gates& G = *reinterpret_cast<const Gates*>(packs + slot * Packed<T, 3>::kBlock + Packed<T, 3>::kBytes);
+  const int64_t at = gate_row(P, sp, h) + sp.begin + lane;
+  const float hi = G.hi[lane], lo = G.lo[lane], beta = G.beta[lane], whole = G.whole;
+  const float last_hi = __shfl_up(hi, 1), last_lo = __shfl_up(lo, 1);
+  const float step = lane > 0 ? (hi - last_hi) + (lo - last_lo) : hi;
+  const bool multiply = __ballot(step < kDirectStep) != 0 && whole > 0.0f;
+  float ends = 0.0f, begins = 0.0f;
+  if (lane < live) ends = from[at], begins = on[at];
+  {
+    const uint32_t at_lds = lds_address(lds);
+    const u32x4_t r = rsrc_sgprs(E + slot * (D * kDeltaTile), D * kDeltaTile * 4);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const int piece = 4 * i + w, row = 4 * piece + g;
+      dma16(r, at_lds + 1024 * piece, (uint32_t)(row * 256 + ((n ^ ((row >> 3 & 3) << 2)) * 16)));
+    }
+  }
+  const int64_t krow = first_row(P, sp, P.heads, h / P.group) + sp.begin,
+                vrow = first_row(P, sp, P.value_heads, h) + sp.begin;
+  const uint32_t bytes = (uint32_t)(live * C::kRow);
+  const __amdgpu_buffer_rsrc_t rq = make_rsrc(q + krow * D, bytes), rk = make_rsrc(k + krow * D, bytes),
+                               ro = make_rsrc(dout + vrow * D, bytes);
+  auto row = [&](const __amdgpu_buffer_rsrc_t& r, int t, int ks) {
+    Parts<T, 1> o;
+    const uint32_t at = (uint32_t)(t * C::kRow + (32 * ks + 8 * g) * C::ES);
+    if constexpr (sizeof(T) == 2) {
+      o.v[0] = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+    } else {
+      o.v[0].a = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+      o.v[0].b = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, at + 16, 0, 0));
+    }
+    return o;
+  };
+  const int own = 16 * w + n;
+  f32x4_t qk[4], kk[4], ou[4], vu[4];  // products with the earlier tokens 16 b + 4 g + r
+#pragma unroll
+  for (int b = 0; b < 4; ++b) qk[b] = kk[b] = ou[b] = vu[b] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+  Parts<T, 1> own_o[C::KS];
+  float own_f[C::KS][8];
+#pragma unroll
+  for (int ks = 0; ks < C::KS; ++ks) {
+    own_o[ks] = row(ro, own, ks);
+    const float* p = F + slot * (D * kDeltaTile) + (32 * ks + 8 * g) * kDeltaTile + own;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) own_f[ks][j] = p[j * kDeltaTile];
+  }
+  // (Each wave's row blocks without branches between them: their loads are under way at once.  The
+  // last product's result is waited for here: the compiler left one wait state too few behind the
+  // branches.)
+  auto by_wave = [&](auto products) {
+    auto f = [&](auto blocks) {
+      products(blocks);
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_nop 10");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if (w == 0) f(std::integral_constant<int, 1>{});
+    else if (w == 1) f(std::integral_constant<int, 2>{});
+    else if (w == 2) f(std::integral_constant<int, 3>{});
+    else f(std::integral_constant<int, 4>{});
+  };
+  by_wave([&](auto blocks) {
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) {
+      const Parts<T, 1> own_q = row(rq, own, ks), own_k = row(rk, own, ks);
+#pragma unroll
+      for (int b = 0; b < decltype(blocks)::value; ++b) {
+        const Parts<T, 1> keys = row(rk, 16 * b + n, ks);
+        mma_parts<T>(qk[b], keys, own_q);
+        mma_parts<T>(kk[b], keys, own_k);
+      }
+    }
+  });
+  if (threadIdx.x < kDeltaTile) gates[0][lane] = hi, gates[1][lane] = lo, gates[2][lane] = beta;
+  wait_vm<0>();
+  lds_barrier();
+  by_wave([&](auto blocks) {
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) {
+      Parts<T, 3> f, e;
+      split(f, own_f[ks]);
+#pragma unroll
+      for (int b = 0; b < decltype(blocks)::value; ++b) {
+        const float* p = &lds[32 * ks + 8 * g][(16 * b + n) ^ (16 * g)];
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = p[j * kDeltaTile];
+        split(e, x);
+        mma_parts<T>(ou[b], e, own_o[ks]);
+        mma_parts<T>(vu[b], e, f);
+      }
+    }
+  });
+  const float own_hi = gates[0][own], own_lo = gates[1][own], own_beta = gates[2][own];
+  // Of the own token r: sums of A_rs up to s, which are what token s + 1 has from r > s on.
+  float x[16], before = 0.0f;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const int s = 16 * b + 4 * g;
+    const f32x4_t h4 = *reinterpret_cast<const f32x4_t*>(&gates[0][s]), l4 = *reinterpret_cast<const f32x4_t*>(&gates[1][s]),
+                  b4 = *reinterpret_cast<const f32x4_t*>(&gates[2][s]);
+    float part[4], sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float f = __builtin_amdgcn_exp2f((own_hi - h4[r]) + (own_lo - l4[r])) * b4[r];
+      const float a = f * (P.scale * qk[b][r] * ou[b][r] - own_beta * kk[b][r] * vu[b][r]);
+      sum += s + r < own ? a : 0.0f;
+      part[r] = sum;
+    }
+    // over the groups of lanes, which have the tokens in order
+    float up = __shfl_up(sum, 16);
+    sum += g >= 1 ? up : 0.0f;
+    up = __shfl_up(sum, 32);
+    sum += g >= 2 ? up : 0.0f;
+    up = __shfl_up(sum, 16);
+    const float first = before + (g >= 1 ? up : 0.0f);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[4 * b + r] = s + r < own ? first + part[r] : 0.0f;
+    before += __shfl(sum, 48 + n);
+  }
+  halve<8, 8>(x, lane);
+  halve<4, 4>(x, lane);
+  halve<2, 2>(x, lane);
+  halve<1, 1>(x, lane);
+  passing[w][16 * (n >> 2) + 4 * g + (n & 3)] = x[0];
+  if (multiply) {
+    const double share = wave_sum(states_product<T, D>(S + slot * (D * D), N + slot * (D * D)));
+    if (lane == 0) product[w] = share;
+  }
+  __syncthreads();
+  if (threadIdx.x >= kDeltaTile) return;
+  double b = ends, c = begins;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_down(b, o), z = __shfl_up(c, o);
+    b += lane + o < 64 ? y : 0.0;
+    c += lane >= o ? z : 0.0;
+  }
+  const double all_b = __shfl(b, 0), all_c = __shfl(c, 63), up = __shfl_up(c, 1);
+  double sum = b + (lane > 0 ? up : 0.0);
+  if (lane > 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += passing[i][lane - 1];
+  if (lane < live) dg[at] = (float)sum;
+  if (lane == 0) {
+    double over = 0.0;
+    if (multiply) over = (double)whole * ((product[0] + product[1]) + (product[2] + product[3]));
+    sums[slot] = {all_b, all_c, over, 0.0f, multiply || whole < kNothing};
+  }
+}
+
+// W of a span's tiles, into their tokens' gradients.  With a_j = <S, N> at a tile's start, W_j =
+// a_j - sum B and a_{j+1} = W_j + sum C: from the span's start on, where both states are at hand,
+// and from every tile on whose W is known; and back from the span's end, where the next one
+// has both (or nothing has a gradient any more).  Where both ways reach, either's error grows with
+// its steps, and they are joined in that measure.
 __global__ void __launch_bounds__(kThreads)
 decay_kernel(DeltaPlan P, const int32_t* cu, const float* S0, const float* dS0, const float* recB, const float* recD,
-             const float* do_o, const float* dv_v, bool final_gradient, float* dg) {
-  __shared__ double red[4][kThreads / 64];
+             bool final_gradient, DeltaTileSums* sums, float* dg) {
+  __shared__ double red[2][kThreads / 64];
   const int h = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6, size = P.d * P.d;
   Span sp;
   if (!find_span<kThreads>(P, cu, blockIdx.x, &sp)) return;
+  if (sp.begin >= sp.end) return;
   const int64_t pair = (int64_t)sp.s * P.value_heads + h;
   const size_t record = ((size_t)h * P.units + sp.slot) * size;
   auto product = [&](const float* a, const float* b) {  // this thread's share
@@ -371,47 +599,77 @@ decay_kernel(DeltaPlan P, const int32_t* cu, const float* S0, const float* dS0, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum += (double)x[r] * (double)y[r];
       }
-    return sum;
+    return wave_sum(sum);
   };
+  const double shares[2] = {product(sp.idx > 0 ? recB + record : S0 ? S0 + pair * size : nullptr,
+                                    sp.idx > 0 ? recD + record - size : S0 ? dS0 + pair * size : nullptr),
+                            product(sp.last ? nullptr : recB + record + size, recD + record)};
+  if (lane == 0) red[0][w] = shares[0], red[1][w] = shares[1];
+  __syncthreads();
+  const int count = (sp.end - sp.begin + kDeltaTile - 1) / kDeltaTile;
+  DeltaTileSums* mine =
+      sums + (size_t)h * P.tiles + tile_slot(P, sp.row0, sp.s) + sp.begin / kDeltaTile;
+  if (w == 0) {
+    // Sums that start anew at direct tiles, 64 tiles at a time, a lane a tile.
+    double carry = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+    float steps = 0.0f;
+    for (int j0 = 0; j0 < count; j0 += 64) {
+      const bool in = j0 + lane < count;
+      DeltaTileSums t = {};
+      if (in) t = mine[j0 + lane];
+      bool anew = in && t.direct;
+      double v = anew ? t.over + t.on : t.on - t.from;
+      float m = in && !anew ? 1.0f : 0.0f;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(v, o);
+        const float z = __shfl_up(m, o);
+        const bool other = __shfl_up((int)anew, o);
+        if (lane >= o && !anew) v += y, m += z, anew = other;
+      }
+      if (!anew) v += carry, m += steps;
+      double start = __shfl_up(v, 1);
+      float from = __shfl_up(m, 1);
+      if (lane == 0) start = carry, from = steps;
+      if (!t.direct) t.over = start - t.from;
+      t.steps = from;
+      if (in) mine[j0 + lane] = t;
+      carry = __shfl(v, 63), steps = __shfl(m, 63);
+    }
+    bool known = !(sp.last && final_gradient);
+    carry = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    steps = 0.0f;
+    for (int j0 = (count - 1) / 64 * 64; j0 >= 0; j0 -= 64) {
+      const bool in = j0 + lane < count;
+      DeltaTileSums t = {};
+      if (in) t = mine[j0 + lane];
+      bool anew = in && t.direct;
+      double v = anew ? t.over + t.from : t.from - t.on;
+      float m = in && !anew ? 1.0f : 0.0f;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_down(v, o);
+        const float z = __shfl_down(m, o);
+        const bool other = __shfl_down((int)anew, o);
+        if (lane + o < 64 && !anew) v += y, m += z, anew = other;
+      }
+      if (!anew) v += carry, m += steps;
+      const bool there = anew || known;
+      double end = __shfl_down(v, 1);
+      float to = __shfl_down(m, 1);
+      bool reached = __shfl_down((int)there, 1);
+      if (lane == 63) end = carry, to = steps, reached = known;
+      if (in && !t.direct && reached) {
+        const double a = t.steps + 0.5f, b = to + 0.5f;
+        mine[j0 + lane].over = (t.over * b + (end - t.on) * a) / (a + b);
+      }
+      carry = __shfl(v, 0), steps = __shfl(m, 0), known = __shfl((int)there, 0);
+    }
+  }
+  __syncthreads();
   const int64_t row = gate_row(P, sp, h);
-  auto step_of = [&](int t) { return (double)dv_v[row + t] - (double)do_o[row + t]; };
-  double sums[3] = {product(sp.idx > 0 ? recB + record : S0 ? S0 + pair * size : nullptr,
-                            sp.idx > 0 ? recD + record - size : S0 ? dS0 + pair * size : nullptr),
-                    product(sp.last ? nullptr : recB + record + size, recD + record), 0.0};
-  for (int t = sp.begin + (int)threadIdx.x; t < sp.end; t += kThreads) sums[2] += step_of(t);
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sums[k] += __shfl_xor(sums[k], o);
-    if (lane == 0) red[k][w] = sums[k];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    sums[k] = 0.0;
-    for (int i = 0; i < kThreads / 64; ++i) sums[k] += red[k][i];
-  }
-  __syncthreads();
-  double at = sums[0];
-  const double miss = sp.last && final_gradient ? 0.0 : (sums[1] - (at + sums[2])) / max(sp.end - sp.begin, 1);
-  for (int t0 = sp.begin, flip = 0; t0 < sp.end; t0 += kThreads, flip ^= 1) {
-    const int t = t0 + (int)threadIdx.x;
-    const double step = t < sp.end ? step_of(t) : 0.0;
-    double c = step;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double x = __shfl_up(c, o);
-      if (lane >= o) c += x;
-    }
-    if (lane == 63) red[flip][w] = c;
-    __syncthreads();
-    double before = at;
-    for (int i = 0; i < kThreads / 64; ++i) {
-      if (i < w) before += red[flip][i];
-      at += red[flip][i];
-    }
-    if (t < sp.end) dg[row + t] = (float)(before + (c - step) + miss * (t - sp.begin));
-  }
+  for (int t = sp.begin + (int)threadIdx.x; t < sp.end; t += kThreads)
+    dg[row + t] = (float)(dg[row + t] + mine[(t - sp.begin) / kDeltaTile].over);
 }
 
 }  // namespace
@@ -429,9 +687,13 @@ gbla_status launch_delta_grads(const DeltaPlan& p, const void* q, const void* k,
     hipLaunchKernelGGL((grads_kernel<T, D>), dim3(p.tiles, p.heads), dim3(kThreads), 0, st, p, tile_spans(p),
                        (const T*)q, (const T*)k, (const T*)dout, cu, base + p.off_pack,
                        floats(p.off_S), floats(p.off_N), floats(p.off_E), floats(p.off_F), (T*)dq, (T*)dk, (T*)dv);
-    hipLaunchKernelGGL(decay_kernel, dim3(p.grid_units, p.value_heads), dim3(kThreads), 0, st, p, cu, S0, dS0,
-                       floats(p.off_B), floats(p.off_D), floats(p.off_do_o), floats(p.off_dv_v), final_gradient,
+    DeltaTileSums* sums = reinterpret_cast<DeltaTileSums*>(base + p.off_sums);
+    hipLaunchKernelGGL((pairs_kernel<T, D>), dim3(p.tiles, p.value_heads), dim3(kThreads), 0, st, p, tile_spans(p),
+                       (const T*)q, (const T*)k, (const T*)dout, cu, base + p.off_pack, floats(p.off_S),
+                       floats(p.off_N), floats(p.off_E), floats(p.off_F), floats(p.off_from), floats(p.off_on), sums,
                        dlog_decay);
+    hipLaunchKernelGGL(decay_kernel, dim3(p.grid_units, p.value_heads), dim3(kThreads), 0, st, p, cu, S0, dS0,
+                       floats(p.off_B), floats(p.off_D), final_gradient, sums, dlog_decay);
   });
 }
 

@@ -104,8 +104,10 @@ gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backwar
     q.off_N = take(each * state);
     q.off_E = take(each * vectors);
     q.off_F = take(each * vectors);
-    q.off_do_o = take(gate);
-    q.off_dv_v = take(gate);
+    q.off_X = take(each * vectors);
+    q.off_from = take(gate);
+    q.off_on = take(gate);
+    q.off_sums = take(each * sizeof(DeltaTileSums));
     q.off_dS0 = take((size_t)q.nseq * q.value_heads * state);
   }
   q.total_bytes = off;
