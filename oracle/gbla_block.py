@@ -98,11 +98,14 @@ def delta_sizes(q, k, v, g, beta, scale, S0=None, tile=64):
 
 def delta_backward_sizes(q, k, v, g, beta, do, scale, S0=None, dS=None, tile=64):
     """The like of ``delta_sizes`` for (dq, dk, dv, dg, dbeta, dS0).  A token's map of the state's
-    gradient is the transpose of the forward's and makes no column longer either.  Per token and
-    value channel: A bounds an error in reading the state, Bu one in u, G one in reading the
-    state's gradient, Bf one in f = D^T k (from the tile's do, the gradient after the tile and
-    the tile's later f).  dk = D u - Z dv takes both factors' errors of both products, dbeta = f
-    miss likewise; dg adds up those of do o and dv v over the sequence and of one <D, S>."""
+    gradient is the transpose of the forward's and makes no column longer either, so of an error
+    in f = D^T k only what arises at the token adds to W, the error that the state's gradient
+    carries.  Per token and value channel: A bounds an error in reading the state, Bu one in u, G
+    one in reading the state's gradient, Bf one in f (from the tile's do, the gradient after the
+    tile and the tile's later f).  dk = D u - Z dv takes both factors' errors of both products,
+    dbeta = f miss likewise; dg adds up, over the sequence, those of what a token's do and dv take of the
+    past (the state before its tile and the tile's earlier u) and of what its u gives to the
+    gradient after the tile, and of one <D, S>, the largest of those where tiles meet."""
     V, n, d = v.shape
     H = q.shape[0]
     q, k, v, beta, do = _shared(q, V), _shared(k, V), v.double(), beta.double(), do.double()
@@ -110,9 +113,10 @@ def delta_backward_sizes(q, k, v, g, beta, do, scale, S0=None, dS=None, tile=64)
     norm = lambda X: X.norm(dim=1)
     S = torch.zeros(V, d, d, dtype=torch.float64) if S0 is None else S0.double().clone()
     Z = norm(S)
-    past = []
+    past, starts = [], {}
     for t in range(n):
         if t % tile == 0:
+            starts[t] = (norm(S), Z)
             head, inner, added = norm(S), torch.zeros(V, d), torch.zeros(V, d)
             Z = Z + head
         P = lam[:, t, :, None] * S
@@ -120,28 +124,32 @@ def delta_backward_sizes(q, k, v, g, beta, do, scale, S0=None, dS=None, tile=64)
         u = beta[:, t, None] * miss
         S = P + k[:, t, :, None] * u[:, None, :]
         y = v[:, t].abs() + head
+        reach = head + added  # of what the token's key finds
         inner, added = inner + beta[:, t, None] * y, added + u.abs()
         wrong = Z + y + inner + added  # of miss
         Z = lam[:, t] * Z + beta[:, t, None] * (y + inner + added) + u.abs()
-        past.append((P, miss, u, S, Z + head + added, wrong))
+        past.append((P, miss, u, S, Z + head + added, wrong, reach))
     D = torch.zeros_like(S) if dS is None else dS.double().clone()
     W = norm(D)
     out = {x: torch.zeros(V, n, d, dtype=torch.float64) for x in ("dq", "dk", "dv")}
     db = torch.zeros(V, n, dtype=torch.float64)
     flow = torch.zeros(V, dtype=torch.float64)
+    meet = (norm(S) * W + Z * norm(D)).sum(-1)
     for t in reversed(range(n)):
         if t == n - 1 or t % tile == tile - 1:
             tail, given, later = norm(D), torch.zeros(V, d), torch.zeros(V, d)
             W = W + tail
-        P, miss, u, S, A, wrong = past[t]
+        P, miss, u, S, A, wrong, reach = past[t]
         o = abs(scale) * do[:, t].abs()
         D = D + scale * q[:, t, :, None] * do[:, t, None, :]
         f = torch.matmul(k[:, t, None, :], D)[:, 0]
         dv = beta[:, t, None] * f
         given = given + o
         W = W + q[:, t].norm(dim=-1, keepdim=True) * o
-        G = W + tail + given + later
-        Bf = G + beta[:, t, None] * (tail + given)
+        near = tail + given + later
+        G = W + near
+        near = near + beta[:, t, None] * (tail + given)
+        Bf = W + near
         later = later + dv.abs() + beta[:, t, None] * (tail + given)
         out["dq"][:, t] = (A * o).sum(-1, keepdim=True)
         out["dv"][:, t] = beta[:, t, None] * Bf
@@ -149,12 +157,13 @@ def delta_backward_sizes(q, k, v, g, beta, do, scale, S0=None, dS=None, tile=64)
         out["dk"][:, t] = (G * u.abs() + (norm(D) + tail + given + later) * Bu + A * dv.abs()
                            + (norm(P) + A) * out["dv"][:, t]).sum(-1, keepdim=True)
         db[:, t] = (Bf * miss.abs() + f.abs() * wrong).sum(-1)
-        flow = flow + (A * o + out["dv"][:, t] * v[:, t].abs()).sum(-1)
+        flow = flow + (A * o + dv.abs() * wrong + out["dv"][:, t] * reach + u.abs() * (W + tail) + tail * Bu).sum(-1)
         D = D - k[:, t, :, None] * dv[:, None, :]
-        W = lam[:, t] * (W + out["dv"][:, t] + dv.abs())
+        W = lam[:, t] * (W + beta[:, t, None] * near + dv.abs())
         D = lam[:, t, :, None] * D
-    start = torch.zeros(V, d, d, dtype=torch.float64) if S0 is None else S0.double()
-    dg = flow[:, None] + ((W * norm(start)) + norm(D) * Z).sum(-1)[:, None]
+        if t in starts:
+            meet = torch.maximum(meet, (starts[t][0] * W + starts[t][1] * norm(D)).sum(-1))
+    dg = (flow + meet)[:, None]
     fold = lambda x: x.view(H, V // H, n, d).sum(1)
     return fold(out["dq"]), fold(out["dk"]), out["dv"], dg.expand(V, n), db, W[:, None, :].expand(V, d, d)
 

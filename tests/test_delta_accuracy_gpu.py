@@ -26,13 +26,19 @@ GRADS = ("dq", "dk", "dv", "dlog_decay", "dbeta")
 
 
 def per_head(got, want, name, tol=2.0 ** -17):
-    """Heads first: the error's norm within tol of the head's own."""
-    if got.dtype == BF16:
+    """Heads first: the error's norm within tol of the head's own; in bf16, where a wrong entry
+    among many is less than the roundings of all, every entry within half a step and 2^-8 of the
+    head's root mean square (parts of 2^-16 of terms up to 2^5 times their sum, six deviations)."""
+    half = got.dtype == BF16
+    if half:
         tol = 2.0 ** -8 * (1 + 2.0 ** -4)
     got, want = got.cpu().double().flatten(1), want.flatten(1)
     off, size = (got - want).norm(dim=1), want.norm(dim=1)
     assert torch.isfinite(got).all() and (off <= tol * size + 1e-30).all(), "%s: off by %s of the heads' norms" % (
         name, ["%.3g" % x for x in off / size])
+    if half:
+        over = (got - want).abs() - 2.0 ** -8 * (want.abs() * 1.01 + want.square().mean(dim=1, keepdim=True).sqrt())
+        assert (over <= 0).all(), "%s: an entry off by %.3g more" % (name, over.max())
 
 
 def fast(lengths, d, dtype, rates, seed=5):
