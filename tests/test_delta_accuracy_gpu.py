@@ -17,7 +17,8 @@ from oracle import gbla_block as ref
 from paper_2606_07317_amd import gbla
 from tests.test_decoder_gpu import BF16, F32, _dev, _gen, _pieces, _randn
 from tests.test_delta_backward_gpu import grads_of
-from tests.test_delta_gpu import NAMES, delta_case, own, pieces_of
+from tests.test_delta_gpu import BOUNDED, BOUNDED_IDS, NAMES, _MANY, delta_case, own, pieces_of, unit
+from tests.test_delta_large_gpu import LONG, LONG_IDS
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +90,73 @@ def test_decays_gradient_of_single_tokens_that_forget(dtype, d, n):
     for x, at in kinds.items():
         off = (got[at].double() - want[at]).norm() / want[at].norm()
         assert off <= 2.0 ** -14, "tokens of decay exp(%g): off by %.3g of their norm" % (x, off)
+
+
+def by_heads(pieces):
+    """The sequences' [heads, ..] next to each other."""
+    return torch.cat([x.flatten(1) for x in pieces], dim=1)
+
+
+def check_case(case, tight, directions):
+    """Every result of a case, head by head over its sequences."""
+    lengths, ragged, H, V, d, dtype, states, _ = case
+    t = delta_case(*case)
+    how = dict(initial_state=_dev(t["S0"])[0], cu_seqlens=_dev(t["cu"])[0], max_seqlen=max(lengths) if tight else None)
+    start = lambda s: t["S0"][s] if states else None
+    if "forward" in directions:
+        out, S = own(t, final_state=True, **how)
+        want = [ref.delta(*args, d ** -0.5, start(s)) for s, args in enumerate(pieces_of(t, NAMES, lengths, ragged))]
+        per_head(by_heads(_pieces(out, lengths, ragged)), by_heads(w[0] for w in want), "out")
+        per_head(by_heads(S), by_heads(w[1] for w in want), "final_state")
+    if "backward" in directions:
+        got = grads_of(t, dfinal_state=_dev(t["dS"])[0], **how)
+        want = [ref.delta_backward(*args, d ** -0.5, start(s), t["dS"][s] if states else None)
+                for s, args in enumerate(pieces_of(t, NAMES + ("dout",), lengths, ragged))]
+        have = list(pieces_of(got, GRADS, lengths, ragged))
+        for i, x in enumerate(GRADS):
+            per_head(by_heads(h[i] for h in have), by_heads(w[i] for w in want), x)
+        if states:
+            per_head(by_heads(got["dinitial_state"]), by_heads(w[5] for w in want), "dinitial_state")
+
+
+MANY = [(lengths, True, 1, 1, d, dtype, True, (-7,)) for lengths in _MANY for dtype, d in ((BF16, 32), (F32, 64))]
+
+
+@pytest.mark.parametrize("case,tight", BOUNDED, ids=BOUNDED_IDS)
+def test_gradients_of_each_head(case, tight):
+    check_case(case, tight, ("backward",))
+
+
+@pytest.mark.parametrize("case", LONG, ids=LONG_IDS)
+def test_gradients_of_each_head_in_units_of_several_tiles(case):
+    check_case(case, False, ("backward",))
+
+
+@pytest.mark.parametrize("case", MANY[1:], ids=lambda c: "%d-%d" % (len(c[0]), c[4]))
+def test_gradients_of_each_head_of_many_sequences(case):
+    check_case(case, True, ("backward",))
+
+
+def test_gradients_past_two_to_the_31_elements():
+    """Of the last sequence of a packed batch whose v ends past element 2^31."""
+    H, V, d, last = 2, 4, 128, 300
+    T = 2 ** 22 + 333
+    gen = torch.Generator("cuda").manual_seed(4)
+
+    def act(heads, one):
+        x = torch.empty(heads, T, d, dtype=BF16, device="cuda").normal_(generator=gen)
+        if one:
+            for h in range(heads):
+                x[h] = unit(x[h]).to(BF16)
+        return x
+
+    q, k, v, dout = act(H, True), act(H, True), act(V, False), act(V, False)
+    g = -torch.exp2(torch.tensor([-6.0, -3.0, 1.0, 3.0], device="cuda"))[:, None] * torch.rand(V, T, generator=gen, device="cuda")
+    b = torch.rand(V, T, generator=gen, device="cuda")
+    cu = torch.tensor([0, 2 ** 21, T - last, T], device="cuda", dtype=torch.int32)
+    got = gbla.delta_attention_backward(q, k, v, g, b, dout, cu_seqlens=cu)
+    tail = [x[:, -last:].cpu() for x in (q, k, v, g, b, dout)]
+    for x, w in zip(GRADS, ref.delta_backward(*tail, d ** -0.5)):
+        per_head(got[x][:, -last:], w, x)
+    del got
+    torch.cuda.empty_cache()
