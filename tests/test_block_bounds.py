@@ -78,3 +78,24 @@ def test_wrong_gradients_are_refused(dtype, d):
         for bad in wrong:
             with pytest.raises(AssertionError):
                 per_head(bad.to(kind), want, name)
+
+
+@pytest.mark.parametrize("parts,ok", [(1, False), (3, True)])
+def test_states_of_too_few_parts_are_refused(parts, ok):
+    """The recurrence with u cut to bf16 parts before it enters the state, as a tile's products are."""
+    n, d = 300, 64
+    (q, k, v, g, b, _), (S0, _) = _case(n, d, BF16)
+    _, want = ref.delta(q, k, v, g, b, d ** -0.5, S0)
+    S = S0.double()
+    for t in range(n):
+        S = torch.exp(g[:, t, None, None].double()) * S
+        u = b[:, t, None] * (v[:, t].double() - torch.matmul(k[:, t, None, :].double(), S)[:, 0])
+        kept = torch.zeros_like(u)
+        for _ in range(parts):
+            kept = kept + (u - kept).to(BF16).double()
+        S = S + k[:, t, :, None].double() * kept[:, None, :]
+    if ok:
+        per_head(S.float(), want, "state")
+    else:
+        with pytest.raises(AssertionError):
+            per_head(S.float(), want, "state")

@@ -160,3 +160,54 @@ def test_gradients_past_two_to_the_31_elements():
         per_head(got[x][:, -last:], w, x)
     del got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("case,tight", BOUNDED, ids=BOUNDED_IDS)
+def test_outputs_and_states_of_each_head(case, tight):
+    """States are fp32 whatever the type: one bf16 part of what forms them, in place of three, would
+    leave 2^-9 of their norm."""
+    check_case(case, tight, ("forward",))
+
+
+@pytest.mark.parametrize("case", LONG, ids=LONG_IDS)
+def test_outputs_and_states_of_each_head_in_units_of_several_tiles(case):
+    check_case(case, False, ("forward",))
+
+
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "%d-%d" % (len(c[0]), c[4]))
+def test_outputs_and_states_of_each_head_of_many_sequences(case):
+    check_case(case, True, ("forward",))
+
+
+def test_outputs_and_states_past_two_to_the_31_elements():
+    H, V, d, last = 2, 4, 128, 300
+    T = 2 ** 22 + 333
+    gen = torch.Generator("cuda").manual_seed(5)
+    q, k = (torch.empty(H, T, d, dtype=BF16, device="cuda").normal_(generator=gen) for _ in range(2))
+    for h in range(H):
+        q[h], k[h] = unit(q[h]).to(BF16), unit(k[h]).to(BF16)
+    v = torch.empty(V, T, d, dtype=BF16, device="cuda").normal_(generator=gen)
+    g = -2.0 ** -6 * torch.rand(V, T, generator=gen, device="cuda")
+    b = torch.rand(V, T, generator=gen, device="cuda")
+    cu = torch.tensor([0, 2 ** 21, T - last, T], device="cuda", dtype=torch.int32)
+    out, S = gbla.delta_attention(q, k, v, g, b, final_state=True, cu_seqlens=cu)
+    want, final = ref.delta(*(x[:, -last:].cpu() for x in (q, k, v, g, b)), d ** -0.5)
+    per_head(out[:, -last:], want, "out")
+    per_head(S[2], final, "final_state")
+    del out, S
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("rows", [1, 7])
+def test_a_step_of_each_head(rows, dtype, d):
+    H, V = 2, 4
+    t = delta_case([rows], True, H, V, d, dtype, False, (-3, -4, -5, -6), seed=rows)
+    step = _dev(*(t[x].transpose(0, 1).contiguous() for x in NAMES))
+    state = _randn(_gen(7), rows, V, d, d)
+    S, = _dev(state.clone())
+    out = gbla.delta_step(*step, S)
+    for n in range(rows):
+        want, new = ref.delta(*(t[x][:, n:n + 1] for x in NAMES), d ** -0.5, state[n])
+        per_head(out[n], want, "out")
+        per_head(S[n], new, "state")
