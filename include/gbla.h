@@ -494,7 +494,9 @@ size_t gbla_delta_backward_ragged_workspace_bytes(const gbla_delta_shape* shape)
  *   log_decay, beta  fp32 [B,V,n] or [V,T]; log_decay <= 0 (-inf: the past is forgotten).
  *                    Keys of length one and beta within [0, 2] keep the state bounded;
  *                    nothing is normalised here (gbla_qk_norm_rope with weights d^-1/2 and
- *                    no rotation does).
+ *                    no rotation does).  Where the decays are near 1, the keys of 64 tokens
+ *                    nearly alike and their beta nearly 2, roundings add up undamped:
+ *                    results are then at 2^-11 of their norm, not at fp32's accuracy.
  *   initial_state    fp32 [N,V,d,d] ([c][e]: key channel, value channel) or NULL
  *   out              like v
  *   final_state      fp32 [N,V,d,d] or NULL (not wanted); may be initial_state.

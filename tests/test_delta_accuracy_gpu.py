@@ -211,3 +211,64 @@ def test_a_step_of_each_head(rows, dtype, d):
         want, new = ref.delta(*(t[x][:, n:n + 1] for x in NAMES), d ** -0.5, state[n])
         per_head(out[n], want, "out")
         per_head(S[n], new, "state")
+
+
+def strong(lengths, d, dtype, beta, alike, decay, seed=6):
+    """A packed batch with states and strengths from 1 to 2 (or 2 throughout); `alike`: keys a few
+    degrees from one another, where a token written with strength 2 is reflected by the next."""
+    t = delta_case(lengths, True, 2, 4, d, dtype, True, (0,) * 4, seed=seed)
+    gen = _gen(seed + 1)
+    t["beta"] = torch.full(t["beta"].shape, 2.0) if beta == 2 else 1.0 + torch.rand(t["beta"].shape, generator=gen)
+    t["g"] = -decay * torch.rand(t["g"].shape, generator=gen)
+    if alike:
+        k = _randn(gen, 2, 1, d) + 0.05 * _randn(gen, *t["k"].shape)
+        t["k"] = unit(k).to(dtype)
+    return t
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("beta", ["1 to 2", 2])
+@pytest.mark.parametrize("decay", [0.0, 2.0 ** -5])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_strengths_above_one(dtype, d, decay, beta, alike):
+    """fp32 results to 2^-17 of their norms, as elsewhere; with keys alike and strengths from 1 to 2 to
+    2^-14, since a row of the tile's triangle then adds up 64 entries of up to 2, each off by 2^-24, to
+    2^-17 of y, y itself is of up to four times the values' size (what the state predicts is), and
+    the gradients take two such sums.
+
+    Keys alike and strengths of 2 throughout: 2^-11.  (I + L beta)^-1 then has entries of 2 with signs
+    in turn, so that e = (I + L beta)^-1 y is a sum of the tile's tokens that nothing damps, and its
+    norm is 2 * 2 * 64 / pi = 81.  L's entries are rounded at least once, 2^-24 of about 1; as a
+    matrix of independent entries of that size L's error has a norm of at most 2 sqrt(64) 2^-24 =
+    2^-20, and that of e is 81 * 2^-20 * 2 = 2^-12.7 of e.  The triangle that is stored, which
+    substitution rounds entry by entry just so, doubles it, 2^-11.7; the reverse's f = du - M^T
+    (beta du) takes the transpose of the same with e already off: 2^-10.7 for products of both.
+    Their errors are independent: sqrt(2) 2^-11.7, 2^-11.2."""
+    lengths = [130, 1, 700]
+    t = strong(lengths, d, dtype, beta, alike, decay)
+    tol = 2.0 ** (-17 if not alike else -11 if beta == 2 else -14)
+    how = dict(initial_state=_dev(t["S0"])[0], cu_seqlens=_dev(t["cu"])[0], max_seqlen=max(lengths))
+    out, S = own(t, final_state=True, **how)
+    got = grads_of(t, dfinal_state=_dev(t["dS"])[0], **how)
+    cut = lambda x, names: list(pieces_of(x, names, lengths, True))
+    ins = cut(t, NAMES + ("dout",))
+    want = [ref.delta(*a[:5], d ** -0.5, t["S0"][s]) for s, a in enumerate(ins)]
+    back = [ref.delta_backward(*a, d ** -0.5, t["S0"][s], t["dS"][s]) for s, a in enumerate(ins)]
+    per_head(by_heads(_pieces(out, lengths, True)), by_heads(w[0] for w in want), "out", tol)
+    per_head(by_heads(S), by_heads(w[1] for w in want), "final_state", tol)
+    have = cut(got, GRADS)
+    for i, x in enumerate(GRADS):
+        per_head(by_heads(h[i] for h in have), by_heads(w[i] for w in back), x, tol)
+    per_head(by_heads(got["dinitial_state"]), by_heads(w[5] for w in back), "dinitial_state", tol)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_steps_of_strength_above_one(dtype, d):
+    """Sixty tokens of keys alike and strength 2, one after the other in place."""
+    n = 60
+    t = strong([n], d, dtype, 2, True, 2.0 ** -5)
+    S, = _dev(t["S0"].clone())
+    outs = [gbla.delta_step(*_dev(*(t[x][:, i][None].contiguous() for x in NAMES)), S)[0] for i in range(n)]
+    want, final = ref.delta(*(t[x] for x in NAMES), d ** -0.5, t["S0"][0])
+    per_head(torch.stack(outs, 1), want, "out")
+    per_head(S[0], final, "state")
