@@ -43,9 +43,9 @@ struct DeltaPlan {
   size_t off_D;      // [V, units, d, d] fp32: the gradient of the state after each unit
   size_t off_S;      // [V, tiles, d, d] fp32: the state before each tile, [value][key channel]
   size_t off_N;      // ... the gradient of the state after each tile
-  size_t off_E;      // [V, tiles, d, 64] fp32: the tiles' e, [value channel][token]
+  size_t off_E;      // [V, tiles, d, 64] fp32: the tiles' e, [value channel][token]; before that, what
+                     // of the gradient of u comes from the state after the tile
   size_t off_F;      // ... the gradient of u
-  size_t off_X;      // ... its part from the state after the tile
   size_t off_from;   // fp32, like the gates: what of the decays' gradient ends at each token and
                      // comes from the state before its tile
   size_t off_on;     // ... begins at each token and goes on to the state after its tile

@@ -220,8 +220,10 @@ template <typename T, int D, WalkMode Mode>
 constexpr int kWalkWaves = sizeof(T) == 4 || D == 32 || Mode == kBack ? 2 : 4;
 struct BackOut {
   const void* dout;
-  const float *F, *X;  // the gradient of u, and its part from the state after the tile
-  float *S, *E, *from, *on, *dbeta;
+  const float* F;  // the gradient of u
+  float* S;
+  float* E;        // holds F's part from the state after the tile, which e takes the place of
+  float *from, *on, *dbeta;
   float* M;           // the maps for the gradients' scan
   bool final_gradient;  // the final state has one
 };
@@ -417,12 +419,12 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
     again();
     if constexpr (Back) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
-        *reinterpret_cast<f32x4_t*>(back.E + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g)) = y[b];
-#pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         float x[8], beta[8];
-        vector(back.X, ks, x);
+        vector(back.E, ks, x);
+#pragma unroll
+        for (int b = 2 * ks; b < 2 * ks + 2; ++b)
+          *reinterpret_cast<f32x4_t*>(back.E + (slot * D + e0 + n) * kDeltaTile + row_of(b, 4 * g)) = y[b];
         eight(&G.beta[32 * ks + 8 * g], beta);
 #pragma unroll
         for (int j = 0; j < 8; ++j) part[ks][j] = x[j] * (beta[j] * y[2 * ks + (j >> 2)][j & 3]);
@@ -699,8 +701,8 @@ gbla_status launch_delta_backward(const DeltaPlan& p, const void* q, const void*
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
   // (the decays' gradient takes it too)
   if (!dS0 && S0) dS0 = floats(p.off_dS0);
-  const BackOut back = {dout, floats(p.off_F), floats(p.off_X), floats(p.off_S), floats(p.off_E), floats(p.off_from),
-                        floats(p.off_on), dbeta, floats(p.off_MT), dfinal != nullptr};
+  const BackOut back = {dout, floats(p.off_F), floats(p.off_S), floats(p.off_E), floats(p.off_from), floats(p.off_on),
+                        dbeta, floats(p.off_MT), dfinal != nullptr};
   gbla_status done = by_type(p, [&](auto t, auto dim) {
     using T = decltype(t);
     constexpr int D = decltype(dim)::value;

@@ -36,7 +36,7 @@ constexpr int kBackWaves = 2;
 struct BackArrays {
   const unsigned char* packs;  // M's transposes and the gates
   float* recD;                 // the gradient of the state after each unit; what it adds (Records)
-  float *N, *F, *X;
+  float *N, *F, *X;             // X: f's part from the state after the tile
 };
 
 // Records: what the unit's own tokens add to the gradient of the state before it, into recD.
@@ -214,7 +214,7 @@ BackArrays arrays(const DeltaPlan& p, void* ws) {
   unsigned char* base = static_cast<unsigned char*>(ws);
   auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
   return {base + p.off_packT, floats(p.off_D), floats(p.off_N),
-          floats(p.off_F), floats(p.off_X)};
+          floats(p.off_F), floats(p.off_E)};
 }
 
 }  // namespace

@@ -104,7 +104,6 @@ gbla_status make_delta_plan(const gbla_delta_shape* s, bool ragged, bool backwar
     q.off_N = take(each * state);
     q.off_E = take(each * vectors);
     q.off_F = take(each * vectors);
-    q.off_X = take(each * vectors);
     q.off_from = take(gate);
     q.off_on = take(gate);
     q.off_sums = take(each * sizeof(DeltaTileSums));
