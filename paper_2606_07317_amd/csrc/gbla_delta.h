@@ -1,5 +1,5 @@
-// gbla_delta.h -- host-side plans and launchers of the gated delta rule and of the
-// residual stream's norm.  Internal to libgbla.so; not part of the public boundary.
+// gbla_delta.h -- host-side plans and launchers of the gated delta rule.  Internal to
+// libgbla.so; not part of the public boundary.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -29,9 +29,7 @@ constexpr int kParts = 3;
 template <typename T, int D>
 using BackSizes = DS<T, D, D / 16>;
 
-// Waves a SIMD that the registers are kept to.
-template <typename T, int D, bool Records>
-constexpr int kBackWaves = 2;
+constexpr int kBackWaves = 2;  // a SIMD, that the registers are kept to
 
 struct BackArrays {
   const unsigned char* packs;  // M's transposes and the gates
@@ -41,7 +39,7 @@ struct BackArrays {
 
 // Records: what the unit's own tokens add to the gradient of the state before it, into recD.
 template <typename T, int D, bool Records>
-__global__ void __launch_bounds__((BackSizes<T, D>::NT), (kBackWaves<T, D, Records>))
+__global__ void __launch_bounds__((BackSizes<T, D>::NT), kBackWaves)
 back_kernel(DeltaPlan P, const T* q, const T* k, const T* dout, const int32_t* cu, const float* dfinal,
             BackArrays a, float* dS0) {
   using C = BackSizes<T, D>;
