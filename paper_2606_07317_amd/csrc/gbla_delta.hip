@@ -306,12 +306,12 @@ walk_kernel(DeltaPlan P, const T* q, const T* k, const T* v, const float* S0, co
   }
   if (threadIdx.x == 0) bad[0] = kDeltaTile;
   __syncthreads();
-  // Phases do not mix, and addresses in LDS, which cost registers held over the loop, are worked
-  // out in each: needed where four waves a SIMD share the registers, and faster where a tile is
-  // short (backward, 8 x 2048 tokens, 16 heads of 64: 92 us with it, 102 without; 58000 tokens, 8
-  // heads of 128: 430, 421; fp32, 8 x 2048 tokens, 8 heads of 64: 69, 66).
+  // Where four waves a SIMD share the registers, phases do not mix, and addresses in LDS, which
+  // cost registers held over the loop, are worked out in each.  (Elsewhere it takes longer: backward,
+  // 8 x 2048 tokens, 16 heads of 64 96 us without it, 100 with; 58000 tokens, 8 heads of 128 409, 429;
+  // forward, 8 x 4096 tokens, 8 heads of 32 100.5, 102.7.)
   auto again = [&] {
-    if constexpr (kWalkWaves<T, D, Mode> > 2 || D * sizeof(T) < 256) {
+    if constexpr (kWalkWaves<T, D, Mode> > 2) {
       __builtin_amdgcn_sched_barrier(0);
       lane = fresh(lane), n = lane & 15, g = lane >> 4;
     }
