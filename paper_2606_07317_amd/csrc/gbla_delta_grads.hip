@@ -426,13 +426,10 @@ pairs_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
   const int w = __builtin_amdgcn_readfirstlane(((threadIdx.x >> 6) + blockIdx.x) & 3);
   const size_t slot = (size_t)h * P.tiles + sp.slot;
   const Gates& G = *reinterpret_cast<const Gates*>(packs + slot * Packed<T, 3>::kBlock + Packed<T, 3>::kBytes);
-  const int64_t at = gate_row(P, sp, h) + sp.begin + lane;
+  // (loaded without a condition, under which they would be waited for)
+  const int64_t at = gate_row(P, sp, h) + sp.begin + min(lane, live - 1);
   const float hi = G.hi[lane], lo = G.lo[lane], beta = G.beta[lane], whole = G.whole;
-  const float last_hi = __shfl_up(hi, 1), last_lo = __shfl_up(lo, 1);
-  const float step = lane > 0 ? (hi - last_hi) + (lo - last_lo) : hi;
-  const bool multiply = __ballot(step < kDirectStep) != 0 && whole > 0.0f;
-  float ends = 0.0f, begins = 0.0f;
-  if (lane < live) ends = from[at], begins = on[at];
+  const float ends = from[at], begins = on[at];
   {
     const uint32_t at_lds = lds_address(lds);
     const u32x4_t r = rsrc_sgprs(E + slot * (D * kDeltaTile), D * kDeltaTile * 4);
@@ -550,13 +547,16 @@ pairs_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
   halve<2, 2>(x, lane);
   halve<1, 1>(x, lane);
   passing[w][16 * (n >> 2) + 4 * g + (n & 3)] = x[0];
+  const float last_hi = __shfl_up(hi, 1), last_lo = __shfl_up(lo, 1);
+  const float step = lane > 0 ? (hi - last_hi) + (lo - last_lo) : hi;
+  const bool multiply = __ballot(step < kDirectStep) != 0 && whole > 0.0f;
   if (multiply) {
     const double share = wave_sum(states_product<T, D>(S + slot * (D * D), N + slot * (D * D)));
     if (lane == 0) product[w] = share;
   }
   __syncthreads();
   if (threadIdx.x >= kDeltaTile) return;
-  double b = ends, c = begins;
+  double b = lane < live ? ends : 0.0f, c = lane < live ? begins : 0.0f;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const double y = __shfl_down(b, o), z = __shfl_up(c, o);
