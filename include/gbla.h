@@ -478,7 +478,10 @@ typedef struct {
 } gbla_delta_shape;
 
 /* Scratch bytes of gbla_delta_forward / gbla_delta_backward (the larger of the dense and the
- * ragged reading, for every max_seqlen); 0 if neither is accepted. */
+ * ragged reading, for every max_seqlen); 0 if neither is accepted.  A backward keeps the states
+ * before and after every 64 tokens: with long sequences about 1.1, 1.8 and 4.3 KB a token and value
+ * head at head dims 32, 64 and 128 (a forward 0.3, 0.4 and 0.6), 2.0 GB for 58,000 packed tokens
+ * of 8 heads of 128. */
 size_t gbla_delta_workspace_bytes(const gbla_delta_shape* shape);
 size_t gbla_delta_backward_workspace_bytes(const gbla_delta_shape* shape);
 /* What the ragged reading alone needs; 0 if it is not accepted. */

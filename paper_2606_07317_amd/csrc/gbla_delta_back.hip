@@ -10,10 +10,10 @@
 // all that one product hands to the next stays in its registers; units run at the same time,
 // joined by the transposes of the forward's maps.
 //
-// Bound by dependent steps at two waves a SIMD (LDS holds keys, queries, gradients, values,
-// scores and triangle: one workgroup a compute unit at heads of 128): the matrix unit works 0.31
-// of the cycles, LDS 0.38.  58000 packed tokens, 8 heads of 128: 318 us, records 230; 8 x 2048
-// tokens, 16 heads of 64: 72 and 55.  Barriers for the order of the phases cost 7 %.
+// Bound by dependent steps at two waves a SIMD (LDS holds keys, queries, gradients, scores and
+// triangle: one workgroup a compute unit at heads of 128): the matrix unit works 0.29 of the
+// cycles, LDS 0.32.  58000 packed tokens, 8 heads of 128: 333 us, records 222; 8 x 2048 tokens, 16
+// heads of 64: 80 and 56.  Barriers for the order of the phases cost 7 %.
 //
 // All sums here form fp32 results of both signs (the gradients of the gates): everything that
 // is computed in fp32 enters its products in three parts.

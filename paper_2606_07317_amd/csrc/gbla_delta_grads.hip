@@ -32,7 +32,7 @@ constexpr int kParts = 2;
 //
 // Bound by dependent steps at two waves a SIMD (registers): the matrix unit works 0.2 of the
 // cycles, LDS 0.25, and 192 KB a tile of heads of 128 come at 3.2 TB/s.  8 x 2048 tokens, 16
-// heads of 64: 106 us; 58000 packed tokens, 8 heads of 128: 445.  (Every wave gathering and
+// heads of 64: 103 us; 58000 packed tokens, 8 heads of 128: 450.  (Every wave gathering and
 // splitting the states and vectors by itself: 491 and 2175.)
 template <typename T, int D>
 struct GradSizes {
@@ -363,10 +363,10 @@ grads_kernel(DeltaPlan P, TileSpans tiles, const T* q, const T* k, const T* dout
 // size of its own decay, unless that is below 2^-8: then the tile's W is the product of the states
 // as the walks left them (bf16: in two parts, 2^-17 of it each).  Without such a token a W below
 // 2^-64 is taken as nothing.  (The states of every tile would be 128 KB more to read at heads of
-// 128: 58000 packed tokens, 8 heads, 2425 us a backward; 2547 with a forgetting token among 50.)
+// 128: 60000 packed tokens, 8 heads, 2395 us a backward; 2505 with a forgetting token among 50.)
 //
-// Bound by HBM and the wait for it: 56 KB a tile at heads of 64, 8 x 2048 tokens, 16 heads: 70 us
-// (3.3 TB/s); 112 KB at heads of 128, 58000 packed tokens, 8 heads: 215 us (3.8).  E and F both in
+// Bound by HBM and the wait for it: 56 KB a tile at heads of 64, 8 x 2048 tokens, 16 heads: 62 us
+// (3.7 TB/s); 112 KB at heads of 128, 58000 packed tokens, 8 heads: 186 us (4.4).  E and F both in
 // LDS: 78 and 282; neither, with branches between the blocks: 88 and 281; as a phase of the
 // gradients' kernel, which has both: 72 and 370 more.
 constexpr float kDirectStep = -8.0f;  // log2
