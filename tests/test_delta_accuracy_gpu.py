@@ -272,3 +272,30 @@ def test_steps_of_strength_above_one(dtype, d):
     want, final = ref.delta(*(t[x] for x in NAMES), d ** -0.5, t["S0"][0])
     per_head(torch.stack(outs, 1), want, "out")
     per_head(S[0], final, "state")
+
+
+@pytest.mark.parametrize("dtype,d", [(F32, 32), (BF16, 64)])
+@pytest.mark.parametrize("with_states", [False, True])
+def test_gradients_of_many_long_sequences(dtype, d, with_states):
+    """Sequences of more than 64 tiles that a workgroup walks whole (256 heads' sequences in all), with
+    heads that forget fast and single tokens that do; three of them against 64 bits."""
+    B, V, n = 32, 8, 4200
+    gen = torch.Generator("cuda").manual_seed(8)
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    q, k = (unit(randn(B, 2, n, d)).to(dtype) for _ in range(2))
+    v, dout = randn(B, V, n, d).to(dtype), randn(B, V, n, d).to(dtype)
+    rate = torch.exp2(torch.tensor([-8.0, -6.0, -4.0, -3.0, -6.0, 0.0, 2.0, -9.0], device="cuda"))
+    g = -rate[:, None] * torch.rand(B, V, n, generator=gen, device="cuda")
+    pick = torch.rand(B, V, n, generator=gen, device="cuda")
+    g[:, 4][pick[:, 4] < 0.005] = -9.0
+    g[:, 7][pick[:, 7] < 0.001] = -float("inf")
+    b = torch.rand(B, V, n, generator=gen, device="cuda")
+    S0, dS = (randn(B, V, d, d), randn(B, V, d, d)) if with_states else (None, None)
+    got = gbla.delta_attention_backward(q, k, v, g, b, dout, initial_state=S0, dfinal_state=dS)
+    at = (0, 17, B - 1)
+    want = [ref.delta_backward(*(x[s].cpu() for x in (q, k, v, g, b, dout)), d ** -0.5,
+                               *((S0[s].cpu(), dS[s].cpu()) if with_states else (None, None))) for s in at]
+    for i, x in enumerate(GRADS):
+        per_head(by_heads(got[x][s].cpu() for s in at), by_heads(w[i] for w in want), x)
+    dg = got["dlog_decay"]
+    assert (dg[torch.isneginf(g)] == 0.0).all()
