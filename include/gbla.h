@@ -523,9 +523,9 @@ gbla_status gbla_delta_forward(const gbla_delta_shape* shape, const void* q, con
  * The states are formed again from the inputs.  Gradients are sums in fp32, of products with
  * fp32's accuracy for the gates' and the states' in both types; in bf16 those of q, k and v
  * enter fp32 values in two or three bf16 parts before they are rounded once.  A token's
- * dlog_decay is a sum of terms of the size of its own exp(log_decay), so it keeps that accuracy
- * where a head forgets fast (2^-14 of it at least for a token that forgets among others that do
- * not), and is 0 where exp(log_decay) is.  Reductions run
+ * dlog_decay is a sum of terms of the size of its own exp(log_decay): it keeps fp32's accuracy in
+ * heads that forget fast, is within 2^-14 of itself for tokens that forget among others that do
+ * not, and is 0 where exp(log_decay) is.  Reductions run
  * in an order fixed by the shape: repeated calls give the same bits.  A value that is not
  * finite may reach every gradient of its sequence and of the heads that read it, but none of
  * another sequence or another query and key head.
